@@ -332,6 +332,103 @@ void abs_batch_destroy(abs_batch* b);
 int abs_calibrate_mfma(int32_t data_mode, int32_t iters, int32_t workgroups, float* d_scratch,
                        void* hip_stream, double* h_ms, double* h_tflops);
 
+/*
+ * Operators of a network's hidden layers: the product of a layer with bias, activation and residual in one
+ * pass, group normalisation with an activation behind it, and dropout whose mask is a function of a counter;
+ * each with its gradient.  They need no handle: sizes travel in a small struct, matrices are row-major DEVICE
+ * arrays owned by the caller with a row pitch in elements (ld*, at least the row's length), in the dtype the
+ * struct names (ABS_X_FP32 or ABS_X_BF16; biases, gamma, beta, saved statistics and their gradients are always
+ * fp32).  Any size, pitch and alignment that the elements allow is taken; rows whose length, pitch and start are
+ * multiples of 16 bytes are read in place, others cost a copy (linear) or narrower loads.  What lies between a
+ * row's end and the next row is neither read nor written.  Sums, statistics and products are held in fp32 and
+ * rounded once to the output's dtype; they have a fixed order (no float atomics): two calls give the same bits.
+ *
+ * Every call enqueues on hip_stream (of the device that is current) and returns; nothing is allocated, copied to
+ * the host or waited for, so calls can be captured into a HIP graph.  d_workspace: at least *_workspace_size()
+ * bytes, 256-byte aligned (NULL where that is 0), used until the call's work is done: calls that may overlap in
+ * time - other streams, graphs replayed side by side - need one each.  Outputs must not overlap inputs unless
+ * said.  A negative return value is an error, abs_last_error(NULL) its text, and nothing has been enqueued
+ * unless it is ABS_E_HIP.
+ */
+enum { ABS_ACT_NONE = 0, ABS_ACT_RELU = 1, ABS_ACT_SILU = 2, ABS_ACT_GELU = 3 };   /* gelu: z (1 + erf(z / sqrt 2)) / 2 */
+
+/*
+ * z = x W + b,  y = act(z) + r, with x [rows, d_in], W [d_in, d_out], b [d_out] (may be NULL), r [rows, d_out]
+ * (may be NULL), y and z [rows, d_out] (z may be NULL; a backward pass of a layer with an activation needs it).
+ * rows >= 0, 1 <= d_in, d_out <= 2^20, rows < 2^31.
+ * The backward pass, for a gradient dy [rows, d_out] of y:  dz = dy act'(z) (relu: 0 where z is not positive;
+ * d_z may be NULL for ABS_ACT_NONE),  dx = dz W^T, dW = x^T dz, db = sum of dz over the rows; the residual's
+ * gradient is dy itself.  d_dx, d_dw, d_db: any of them may be NULL, then it is not computed.  With bf16
+ * operands dz is rounded to bf16 once, for the matrix cores; db is summed from the unrounded values.  d_y may be d_r (each element is read before it is written).
+ */
+typedef struct abs_linear {
+  int32_t dtype;
+  int32_t act;
+  int64_t rows;
+  int32_t d_in, d_out;
+  int64_t ldx, ldw, ldy, ldz, ldr;    /* forward; ldz also backward, ldx / ldw of d_x / d_w there too */
+  int64_t lddy, lddx, lddw;           /* backward */
+} abs_linear;
+size_t abs_linear_workspace_size(const abs_linear* p, int32_t backward, int32_t aligned);   /* aligned: all pointers are, to 16 bytes */
+int abs_linear_forward(const abs_linear* p, const void* d_x, const void* d_w, const float* d_b, const void* d_r,
+                       void* d_y, void* d_z, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+int abs_linear_backward(const abs_linear* p, const void* d_x, const void* d_w, const void* d_z, const void* d_dy,
+                        void* d_dx, void* d_dw, float* d_db, void* d_workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
+/*
+ * Group normalisation, channels last: x [n, spatial, channels], a position's channels contiguous, positions
+ * ldx elements apart (a sample's first position follows the last sample's last one at that pitch), channels in
+ * `groups` equal groups.  Per sample and group, over its m = spatial channels / groups values:
+ *   mean, rstd = 1 / sqrt(variance + eps) (variance: mean of the squared distances from the mean),
+ *   h = (x - mean) rstd gamma + beta,  y = act(h).
+ * d_gamma, d_beta fp32 [channels] (both may be NULL: 1 and 0); d_mean, d_rstd fp32 [n, groups] are outputs (both may
+ * be NULL).  groups = 1 with spatial = 1 is layer normalisation.  n >= 0, spatial >= 1, n spatial < 2^31,
+ * 1 <= channels <= 2^20; d_y may be d_x with the same pitch.
+ * The backward pass, for a gradient dy of y, with mean and rstd of the forward pass:  dh = dy act'(h),
+ *   dx = rstd (dh gamma - mean_m(dh gamma) - xhat mean_m(dh gamma xhat)) + dres,
+ *   dgamma = sum over samples and positions of dh xhat, dbeta = the same of dh,
+ * d_dres (may be NULL): the gradient that reaches x past the normalised branch, pitch lddres.  d_dgamma, d_dbeta may be
+ * NULL (both).  d_dx may be d_dres with the same pitch.
+ */
+typedef struct abs_group_norm {
+  int32_t dtype;
+  int32_t act;
+  int64_t n, spatial;
+  int32_t channels, groups;
+  float   eps;
+  int32_t reserved;                   /* must be 0 */
+  int64_t ldx, ldy, lddy, lddx, lddres;
+} abs_group_norm;
+size_t abs_group_norm_workspace_size(const abs_group_norm* p, int32_t backward);
+int abs_group_norm_forward(const abs_group_norm* p, const void* d_x, const float* d_gamma, const float* d_beta,
+                           void* d_y, float* d_mean, float* d_rstd, void* d_workspace, size_t workspace_bytes,
+                           void* hip_stream);
+int abs_group_norm_backward(const abs_group_norm* p, const void* d_x, const float* d_gamma, const float* d_beta,
+                            const float* d_mean, const float* d_rstd, const void* d_dy, const void* d_dres,
+                            void* d_dx, float* d_dgamma, float* d_dbeta, void* d_workspace, size_t workspace_bytes,
+                            void* hip_stream);
+
+/*
+ * Dropout: y = (kept ? x 65536 / (65536 - drop) : 0) + r, r [rows, cols] may be NULL.  Element e = row cols + col is
+ * dropped where the e % 4-th 16-bit part (from the low end) of the draw with index e / 4 is below `drop`
+ * (0 <= drop < 65536, the probability in 65536ths): the simulation's counter-based draws, stream 2 of `seed` at
+ * `offset`, so the mask depends on nothing but (seed, offset, e) - not on pitches, launch or device - and is
+ * never stored.  The gradient is the same call on dy without r.  Needs no workspace; d_y may be d_x or d_r with the same
+ * pitch.  rows >= 0, 1 <= cols, rows cols < 2^40.
+ */
+typedef struct abs_dropout {
+  int32_t dtype;
+  int32_t drop;
+  int64_t rows, cols;
+  int64_t ldx, ldy, ldr;
+  uint64_t seed, offset;
+} abs_dropout;
+int abs_dropout_forward(const abs_dropout* p, const void* d_x, const void* d_r, void* d_y, void* hip_stream);
+int abs_dropout_backward(const abs_dropout* p, const void* d_dy, void* d_dx, void* hip_stream);
+/* The draws themselves, on the host: kept[i] = 1 where element first + i stays (for checking a binding). */
+int abs_dropout_kept(const abs_dropout* p, int64_t first, int64_t count, uint8_t* h_kept);
+
 /* Host-side helpers exposing the simulation's counter-based draws (for checking a
  * binding or planning a run; no device work): execution time of job j of worker n in
  * ticks, and the B dataset rows of that job's minibatch (h_rows_out: B entries). */

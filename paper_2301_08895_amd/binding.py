@@ -43,6 +43,26 @@ class AbsKernelStat(C.Structure):
                 ("timed_flops", C.c_double), ("timed_bytes", C.c_double)]
 
 
+class AbsLinear(C.Structure):
+    """Mirror of `abs_linear` in include/abs.h."""
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("d_in", C.c_int32), ("d_out", C.c_int32),
+                ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldy", C.c_int64), ("ldz", C.c_int64), ("ldr", C.c_int64),
+                ("lddy", C.c_int64), ("lddx", C.c_int64), ("lddw", C.c_int64)]
+
+
+class AbsGroupNorm(C.Structure):
+    """Mirror of `abs_group_norm` in include/abs.h."""
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("n", C.c_int64), ("spatial", C.c_int64), ("channels", C.c_int32),
+                ("groups", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64),
+                ("lddy", C.c_int64), ("lddx", C.c_int64), ("lddres", C.c_int64)]
+
+
+class AbsDropout(C.Structure):
+    """Mirror of `abs_dropout` in include/abs.h."""
+    _fields_ = [("dtype", C.c_int32), ("drop", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("ldx", C.c_int64),
+                ("ldy", C.c_int64), ("ldr", C.c_int64), ("seed", C.c_uint64), ("offset", C.c_uint64)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -97,6 +117,25 @@ def _load():
     lib.abs_draw_time_ticks.argtypes = [cfgp, i32, i64]
     lib.abs_draw_batch_rows.restype = C.c_int
     lib.abs_draw_batch_rows.argtypes = [cfgp, i32, i64, C.POINTER(i64)]
+    linp, normp, dropp = C.POINTER(AbsLinear), C.POINTER(AbsGroupNorm), C.POINTER(AbsDropout)
+    lib.abs_linear_workspace_size.restype = sz
+    lib.abs_linear_workspace_size.argtypes = [linp, i32, i32]
+    lib.abs_linear_forward.restype = C.c_int
+    lib.abs_linear_forward.argtypes = [linp] + [vp] * 7 + [sz, vp]
+    lib.abs_linear_backward.restype = C.c_int
+    lib.abs_linear_backward.argtypes = [linp] + [vp] * 8 + [sz, vp]
+    lib.abs_group_norm_workspace_size.restype = sz
+    lib.abs_group_norm_workspace_size.argtypes = [normp, i32]
+    lib.abs_group_norm_forward.restype = C.c_int
+    lib.abs_group_norm_forward.argtypes = [normp] + [vp] * 7 + [sz, vp]
+    lib.abs_group_norm_backward.restype = C.c_int
+    lib.abs_group_norm_backward.argtypes = [normp] + [vp] * 11 + [sz, vp]
+    lib.abs_dropout_forward.restype = C.c_int
+    lib.abs_dropout_forward.argtypes = [dropp, vp, vp, vp, vp]
+    lib.abs_dropout_backward.restype = C.c_int
+    lib.abs_dropout_backward.argtypes = [dropp, vp, vp, vp]
+    lib.abs_dropout_kept.restype = C.c_int
+    lib.abs_dropout_kept.argtypes = [dropp, i64, i64, vp]
     if lib.abs_config_bytes() != C.sizeof(AbsConfig):
         raise ImportError("abs_config layout mismatch between binding and library")
     return lib

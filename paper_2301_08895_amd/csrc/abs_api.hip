@@ -17,6 +17,7 @@
 
 #include "host_pool.h"
 #include "kernels.h"
+#include "operators.h"
 #include "sched.h"
 
 using namespace abs_impl;
@@ -168,6 +169,16 @@ struct Stat {
 };
 
 }  // namespace
+
+int abs_impl::op_fail(int code, const char* text) noexcept {
+  try { g_create_error = text; } catch (...) {}
+  return code;
+}
+int abs_impl::op_hip(const char* what, hipError_t e) noexcept {
+  if (e == hipSuccess) return ABS_OK;
+  try { g_create_error = std::string(what) + ": " + hipGetErrorString(e); } catch (...) {}
+  return ABS_E_HIP;
+}
 
 const char* abs_impl::kernel_kind_name(int kind) {
   static const char* names[KK_COUNT] = {

@@ -1,0 +1,685 @@
+// The product of a layer with its epilogue, and its gradients (abs_linear_*):
+//   forward   z = x W + b, y = act(z) + r       rows of x times columns of W (W's contraction runs down its rows)
+//   backward  dz = dy act'(z);  dx = dz W^T     rows of dz times rows of W
+//             dW = x^T dz                       columns of x times columns of dz, contraction over the rows
+// One tile kernel serves the three: an operand whose contraction index is contiguous arrives as [row][k], the others as
+// [k][row], and only the fragment reads differ (bf16: the transposing LDS read).
+#include "operators.h"
+
+#include <algorithm>
+
+namespace abs_impl {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);      // elements of a 16-byte piece
+template <typename T> constexpr int kStep = 128 / (int)sizeof(T);      // contraction elements of a k-step: 128 bytes of a row
+
+// What a request reads beyond an operand's end.
+__device__ uint4 g_zero_piece;
+
+// Global -> LDS requests by hand, counted by hand (see ring_wait): the compiler would make every LDS read wait for all of them.
+__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+__device__ __forceinline__ void lds_request16(const void* gsrc, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gsrc), "{m0}"(lds) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void ring_wait() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory"); }
+
+// What is done with a result: y = act(acc + bias) + r, or a share of the contraction to be added up later.
+template <typename T>
+struct Epilogue {
+  const float* bias; const T* r; T* y; T* z; float* part;
+  int64_t ldr, ldy, ldz, ldpart, part_stride;
+  int act, vec;                      // vec: a 16-byte piece of columns is one access for every array
+};
+
+template <typename T>
+struct GemmArgs {
+  const T* A; const T* B;
+  int64_t lda, ldb;
+  int64_t M, N, K;                   // result rows and columns, contraction
+  int64_t mc, nc;                    // contiguous extents of operands stored [k][.]: whole pieces
+  int mt, nt, nsplit, steps_per_split;
+  Epilogue<T> e;
+};
+
+// V neighbouring columns of a row, V the elements of a 16-byte piece.  (Called from loops that are not unrolled: the activations are long.)
+template <typename T>
+__device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t n, int64_t N, float* v) {
+  constexpr int V = kPiece<T>;
+  if (e.part) {
+    if (n < N) {                                  // (rows of shares are padded to whole quads)
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q)
+        if (n + 4 * q < N) *(f32x4_t*)(e.part + m * e.ldpart + n + 4 * q) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    }
+  } else if (e.vec) {
+    if (n >= N) return;                           // (N is whole pieces)
+    typedef OpVec<T, V> Vec;
+    Vec r, o;
+    if (e.r) r = *(const Vec*)(e.r + m * e.ldr + n);
+    if (e.bias) {
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) {
+        const f32x4_t b = *(const f32x4_t*)(e.bias + n + 4 * q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * q + i] += b[i];
+      }
+    }
+    if (e.z) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) op_narrow(v[i], o.e[i]);
+      *(Vec*)(e.z + m * e.ldz + n) = o;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float h = op_act(v[i], e.act);
+      if (e.r) h += op_widen(r.e[i]);
+      op_narrow(h, o.e[i]);
+    }
+    *(Vec*)(e.y + m * e.ldy + n) = o;
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < V; ++i)
+      if (n + i < N) {
+        float h = v[i];
+        if (e.bias) h += e.bias[n + i];
+        if (e.z) op_narrow(h, e.z[m * e.ldz + n + i]);
+        h = op_act(h, e.act);
+        if (e.r) h += op_widen(e.r[m * e.ldr + n + i]);
+        op_narrow(h, e.y[m * e.ldy + n + i]);
+      }
+  }
+}
+
+// ---------------------------------------------------------------------- the tile kernel
+// 128 x 128 of the result per workgroup, 4 wavefronts of 64 x 64 (2 x 2 blocks of 32 x 32), a k-step of 128 bytes per row.
+// Tiles travel global -> LDS through a ring of RING steps.  An operand [row][k]: a row of a step is 128 bytes, its
+// 16-byte piece c at position c ^ ((row >> 1) & 7).  An operand [k][row]: rows of 128 elements, bf16 with the 64-byte blocks
+// at b ^ (k & 3) (the four rows of a transposing read then cover all banks), fp32 with the 128-byte blocks at
+// b ^ ((k >> 2) & 1) (the two halves of a wavefront read rows 4 apart).  The operands of the matrix instruction are swapped
+// (columns first), so that a lane ends up with four neighbouring columns of one row.
+constexpr int kTile = 128;
+constexpr int kOutPitch = 64 + 4;           // floats of a row of a wavefront's staged results
+
+template <typename T, bool TR>
+struct TileOperand {
+  static constexpr int RPR = TR ? 1024 / (kTile * (int)sizeof(T)) : 8;      // tile rows of a request (1 KB)
+  const char* src[4];                                                       // a lane's piece of requests 0..3, k-step 0
+  int k[4];                                                                 // its (first) contraction index there
+  int64_t step;                                                             // bytes to the next k-step
+
+  __device__ __forceinline__ void init(const T* base, int64_t ld, int64_t r0, int64_t rows, int64_t contiguous, int64_t k0, int wave, int lane) {
+    step = TR ? (int64_t)kStep<T> * ld * (int64_t)sizeof(T) : 128;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (TR) {
+        constexpr int per = 64 / RPR;                     // pieces of a row
+        const int row = (wave * 4 + i) * RPR + lane / per, pos = lane % per;
+        int c;
+        if (sizeof(T) == 2) c = ((((pos >> 2) ^ (row & 3)) << 2) | (pos & 3));
+        else                c = ((((pos >> 3) ^ ((row >> 2) & 1)) << 3) | (pos & 7));
+        const int64_t col = min(r0 + (int64_t)c * kPiece<T>, contiguous - kPiece<T>);
+        k[i] = row;
+        src[i] = (const char*)(base + (k0 + row) * ld + col);
+      } else {
+        const int row = (wave * 4 + i) * 8 + (lane >> 3);
+        const int c = (lane & 7) ^ ((row >> 1) & 7);
+        k[i] = c * kPiece<T>;
+        src[i] = (const char*)(base + min(r0 + row, rows - 1) * ld + k0 + k[i]);
+      }
+    }
+  }
+  // left: contraction elements from this step's first one to the end
+  __device__ __forceinline__ void request(int64_t j, int64_t left, uint32_t lds) const {
+    if (left >= kStep<T>) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lds_request16(src[i] + j * step, lds + i * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lds_request16(k[i] < left ? (const void*)(src[i] + j * step) : (const void*)&g_zero_piece, lds + i * 1024);
+    }
+  }
+};
+
+// Fragment of 32 rows (block blk of the tile's four) for the contraction's part `sub`: bf16: 16 elements, fp32: 8 elements as
+// four instructions' operands (a lane's four values belong to one instruction each).
+template <bool TR>
+__device__ __forceinline__ bf16x8_t fragment(const uint16_t* tile, int blk, int sub, int lane) {
+  const int lk = lane >> 5;
+  if (TR) {
+    const int t16 = lane & 15, th = (lane >> 4) & 1, row = sub * 16 + lk * 8 + (t16 >> 2);
+    const uint16_t* q = tile + row * kTile + (blk ^ (row & 3)) * 32 + th * 16 + (t16 & 3) * 4;
+    union { s16x4_t h[2]; bf16x8_t v; } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(q));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(q + 4 * kTile));
+    return u.v;
+  }
+  const int row = blk * 32 + (lane & 31);
+  return *(const bf16x8_t*)(tile + row * 64 + (((sub << 1) | lk) ^ ((row >> 1) & 7)) * 8);
+}
+template <bool TR>
+__device__ __forceinline__ f32x4_t fragment(const float* tile, int blk, int sub, int lane) {
+  const int lk = lane >> 5;
+  if (TR) {
+    const float* q = tile + (sub * 8 + lk * 4) * kTile + (blk ^ lk) * 32 + (lane & 31);
+    return f32x4_t{q[0], q[kTile], q[2 * kTile], q[3 * kTile]};
+  }
+  const int row = blk * 32 + (lane & 31);
+  return *(const f32x4_t*)(tile + row * 32 + (((sub << 1) | lk) ^ ((row >> 1) & 7)) * 4);
+}
+__device__ __forceinline__ f32x16_t multiply(bf16x8_t a, bf16x8_t b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16_t multiply(f32x4_t a, f32x4_t b, f32x16_t c) {
+#pragma unroll
+  for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[s], b[s], c, 0, 0, 0);
+  return c;
+}
+
+template <typename T, bool ATR, bool BTR, int RING>
+__global__ __launch_bounds__(256, RING <= 2 ? 2 : 1) void linear_tile_kernel(GemmArgs<T> g) {
+  constexpr int kOperand = kTile * kStep<T>;                // elements of an operand's step (16 KB)
+  __shared__ __attribute__((aligned(1024))) T smem[RING * 2 * kOperand];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  // workgroups go round the eight XCDs: each takes a run of neighbouring tiles, columns fastest
+  const int total = g.mt * g.nt * g.nsplit, per = (total + 7) / 8;
+  const int id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+  if (((int)blockIdx.x >> 3) >= per || id >= total) return;
+  const int split = id / (g.mt * g.nt), tile = id - split * (g.mt * g.nt);
+  const int64_t m0 = (int64_t)(tile / g.nt) * kTile, n0 = (int64_t)(tile % g.nt) * kTile;
+  const int64_t k0 = (int64_t)split * g.steps_per_split * kStep<T>;
+  const int64_t kend = min(g.K, k0 + (int64_t)g.steps_per_split * kStep<T>);
+  const int nks = (int)((kend - k0 + kStep<T> - 1) / kStep<T>);
+
+  TileOperand<T, ATR> oa;
+  TileOperand<T, BTR> ob;
+  oa.init(g.A, g.lda, m0, g.M, g.mc, k0, wave, lane);
+  ob.init(g.B, g.ldb, n0, g.N, g.nc, k0, wave, lane);
+  const uint32_t lds = lds_at(smem) + (uint32_t)wave * 4096u;
+  auto request = [&](int j, int stage) {
+    const int64_t left = g.K - k0 - (int64_t)j * kStep<T>;
+    oa.request(j, left, lds + (uint32_t)stage * 32768u);
+    ob.request(j, left, lds + (uint32_t)stage * 32768u + 16384u);
+  };
+  f32x16_t acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+#pragma unroll
+  for (int j = 0; j < RING - 1; ++j)
+    if (j < nks) request(j, j);
+  int stage = 0;
+  for (int ks = 0; ks < nks; ++ks) {
+    if (RING > 2 && ks + RING - 1 <= nks) ring_wait<(RING - 2) * 8>();   // step ks is there for every wavefront, and everybody
+    else                                  ring_wait<0>();                // is done with step ks - 1
+    if (ks + RING - 1 < nks) request(ks + RING - 1, stage == 0 ? RING - 1 : stage - 1);
+    const T* const sa = smem + stage * 2 * kOperand;
+    const T* const sb = sa + kOperand;
+    stage = stage + 1 == RING ? 0 : stage + 1;
+#pragma unroll
+    for (int sub = 0; sub < 4; ++sub) {
+      const auto a0 = fragment<ATR>(sa, wm * 2, sub, lane), a1 = fragment<ATR>(sa, wm * 2 + 1, sub, lane);
+      const auto b0 = fragment<BTR>(sb, wn * 2, sub, lane), b1 = fragment<BTR>(sb, wn * 2 + 1, sub, lane);
+      acc[0][0] = multiply(b0, a0, acc[0][0]);
+      acc[0][1] = multiply(b1, a0, acc[0][1]);
+      acc[1][0] = multiply(b0, a1, acc[1][0]);
+      acc[1][1] = multiply(b1, a1, acc[1][1]);
+    }
+  }
+  // Register r of a lane: column 8 (r / 4) + 4 (lane / 32) + r % 4, row lane % 32 of its block.  Each wavefront's 32 x 64 results
+  // pass through LDS, so that they leave as whole 16-byte pieces of rows.
+  __syncthreads();
+  float* const stage_out = (float*)smem + wave * (32 * kOutPitch);
+  Epilogue<T> e = g.e;
+  if (e.part) e.part += split * e.part_stride;
+  constexpr int V = kPiece<T>, LPR = 64 / V;              // lanes of a row
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4_t*)&stage_out[(lane & 31) * kOutPitch + j * 32 + 8 * q + 4 * (lane >> 5)] =
+            f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int r = lane / LPR; r < 32; r += 64 / LPR) {
+      const int64_t m = m0 + wm * 64 + i * 32 + r, n = n0 + wn * 64 + (lane % LPR) * V;
+      float v[V];
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) *(f32x4_t*)&v[4 * q] = *(const f32x4_t*)&stage_out[r * kOutPitch + (lane % LPR) * V + 4 * q];
+      if (m < g.M) finish(e, m, n, g.N, v);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// ---------------------------------------------------------------------- shares of the contraction, added in their order
+template <typename T>
+__global__ __launch_bounds__(256) void linear_join_kernel(Epilogue<T> e, int64_t M, int64_t N, int shares) {
+  constexpr int V = kPiece<T>;
+  const float* const part = e.part;
+  e.part = nullptr;
+  const int64_t pieces = (N + V - 1) / V, total = M * pieces;
+#pragma unroll 1
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+    const int64_t m = q / pieces, n = (q - m * pieces) * V;
+    float v[V];
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) {
+      if (n + 4 * h >= N) { v[4 * h] = v[4 * h + 1] = v[4 * h + 2] = v[4 * h + 3] = 0.f; continue; }
+      const float* p = part + m * e.ldpart + n + 4 * h;
+      f32x4_t s = *(const f32x4_t*)p;
+      for (int k = 1; k < shares; ++k) s += *(const f32x4_t*)(p + k * e.part_stride);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * h + i] = s[i];
+    }
+    finish(e, m, n, N, v);
+  }
+}
+
+// ---------------------------------------------------------------------- few rows: the weights' bytes are what counts
+// A workgroup takes 8 pieces of columns (128 bytes of a weight row) and a run of the contraction, 32 weight rows at a time;
+// every weight is read once, for all R rows of x.  The runs' sums go to shares that linear_join_kernel adds.
+template <typename T, int V, int R>
+__global__ __launch_bounds__(256) void linear_rows_kernel(const T* x, int64_t ldx, const T* w, int64_t ldw, int rows, int K, int N, int run,
+                                                          float* part, int64_t ldpart, int64_t part_stride) {
+  typedef OpVec<T, V> Vec;
+  __shared__ float red[32][8 * V + 1];
+  const int t = threadIdx.x, c = t & 7, kl = t >> 3;
+  const int n = (int)blockIdx.x * 8 * V + c * V, k0 = (int)blockIdx.y * run, k1 = min(K, k0 + run);
+  float acc[R][V];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[r][e] = 0.f;
+  if (n < N) {
+#pragma unroll 4
+    for (int k = k0 + kl; k < k1; k += 32) {
+      const Vec v = *(const Vec*)(w + (int64_t)k * ldw + n);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float xv = r < rows ? op_widen(x[r * ldx + k]) : 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[r][e] = fmaf(xv, op_widen(v.e[e]), acc[r][e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < V; ++e) red[kl][c * V + e] = acc[r][e];
+    __syncthreads();
+    const int col = (int)blockIdx.x * 8 * V + t;
+    if (t < 8 * V && col < N && r < rows) {
+      float s = 0.f;
+      for (int k = 0; k < 32; ++k) s += red[k][t];
+      part[blockIdx.y * part_stride + r * ldpart + col] = s;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------- dz = dy act'(z), and its column sums
+// 256 threads: 32 pieces of columns, 8 rows at a time; a workgroup's shares of the column sums leave in `sums` [gridDim.y][N].
+template <typename T, int V>
+__global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t lddy, const T* z, int64_t ldz, T* dz, int64_t lddz, int64_t rows,
+                                                        int N, int act, float* sums) {
+  typedef OpVec<T, V> Vec;
+  __shared__ float red[8][32 * V + 1];
+  const int t = threadIdx.x, c = t & 31, rl = t >> 5;
+  const int n = ((int)blockIdx.x * 32 + c) * V;
+  float s[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) s[e] = 0.f;
+  if (n < N) {
+    for (int64_t m = (int64_t)blockIdx.y * 8 + rl; m < rows; m += (int64_t)gridDim.y * 8) {
+      const Vec d = *(const Vec*)(dy + m * lddy + n);
+      Vec zv, o;
+      if (act != ABS_ACT_NONE) zv = *(const Vec*)(z + m * ldz + n);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float v = op_widen(d.e[e]);
+        if (act != ABS_ACT_NONE) v *= op_act_slope(op_widen(zv.e[e]), act);
+        s[e] += v;
+        op_narrow(v, o.e[e]);
+      }
+      if (dz) *(Vec*)(dz + m * lddz + n) = o;
+    }
+  }
+  if (!sums) return;
+#pragma unroll
+  for (int e = 0; e < V; ++e) red[rl][c * V + e] = s[e];
+  __syncthreads();
+  for (int j = t; j < 32 * V; j += 256) {
+    const int col = (int)blockIdx.x * 32 * V + j;
+    if (col < N) {
+      float v = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += red[k][j];
+      sums[(int64_t)blockIdx.y * N + col] = v;
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void linear_db_kernel(const float* sums, int shares, int N, float* db) {
+  __shared__ float red[8][33];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
+  float v = 0.f;
+  if (n < N)
+    for (int k = r; k < shares; k += 8) v += sums[(int64_t)k * N + n];
+  red[r][c] = v;
+  __syncthreads();
+  if (r == 0 && n < N) {
+    for (int k = 1; k < 8; ++k) v += red[k][c];
+    db[n] = v;
+  }
+}
+
+// ---------------------------------------------------------------------- an operand whose rows are not whole 16-byte pieces: a copy that is
+// (columns beyond the end are zero: they meet zeros or leave through columns that are not stored)
+template <typename T>
+__global__ __launch_bounds__(256) void linear_pack_kernel(const T* src, int64_t ld, int64_t rows, int64_t cols, T* dst, int64_t ldd) {
+  constexpr int V = kPiece<T>;
+  const int64_t pieces = ldd / V, total = rows * pieces;
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+    const int64_t m = q / pieces, c = (q - m * pieces) * V;
+    OpVec<T, V> o;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o.e[e] = c + e < cols ? src[m * ld + c + e] : T(0);
+    *(OpVec<T, V>*)(dst + m * ldd + c) = o;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void linear_zero_kernel(T* p, int64_t ld, int64_t rows, int64_t cols) {
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < rows * cols; q += (int64_t)gridDim.x * 256) p[q / cols * ld + q % cols] = T(0);
+}
+
+unsigned few_blocks(int64_t threads) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((threads + 255) / 256, 1 << 16)); }
+
+// ---------------------------------------------------------------------- the plan
+constexpr int kFewRows = 8;                  // up to here linear_rows_kernel
+
+struct Product {                              // one product on the tile kernel
+  int mt, nt, nsplit, steps_per_split;
+  size_t part_bytes;
+};
+Product plan_product(int64_t M, int64_t N, int64_t K, int step) {
+  Product q{};
+  q.mt = (int)((M + kTile - 1) / kTile);
+  q.nt = (int)((N + kTile - 1) / kTile);
+  const int64_t tiles = (int64_t)q.mt * q.nt, steps = (K + step - 1) / step;
+  // few tiles: shares of the contraction, at least four k-steps each, until every CU has one
+  int64_t split = 1;
+  if (tiles < 256 && steps >= 8) split = std::max<int64_t>(1, std::min<int64_t>({16, 256 / tiles, steps / 4}));
+  q.steps_per_split = (int)((steps + split - 1) / split);
+  q.nsplit = std::max(1, (int)((steps + q.steps_per_split - 1) / q.steps_per_split));
+  if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
+  return q;
+}
+
+struct LinearPlan {
+  bool pack_x, pack_w, few, dz;
+  int V, run, runs, sum_rows;
+  Product fwd, dx, dw;
+  int64_t in8, out8;                          // d_in, d_out in whole pieces
+  size_t off_x, off_w, off_dz, off_sums, off_part, bytes;
+};
+
+// aligned: the pointers are; need_copy of x / w and, for the backward pass, of dy into dz
+LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok, bool dy_ok) {
+  LinearPlan q{};
+  const int size = op_size(p.dtype), piece = 16 / size, step = 128 / size;
+  q.in8 = (int64_t)op_round_up(p.d_in, piece);
+  q.out8 = (int64_t)op_round_up(p.d_out, piece);
+  const bool x_whole = x_ok && p.d_in % piece == 0 && p.ldx % piece == 0;
+  const bool w_whole = w_ok && p.d_out % piece == 0 && p.ldw % piece == 0;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o = op_round_up(o + bytes, 256); return at; };
+  if (!backward) {
+    q.few = p.rows <= kFewRows;
+    if (q.few) {
+      q.V = w_whole ? piece : 1;
+      // runs of the contraction: about two workgroups per CU
+      const int blocks = (p.d_out + 8 * q.V - 1) / (8 * q.V);
+      const int want = std::max(1, 512 / blocks);
+      q.run = std::max(64, (int)op_round_up((p.d_in + want - 1) / want, 32));
+      q.runs = (p.d_in + q.run - 1) / q.run;
+      q.off_part = take((size_t)q.runs * p.rows * op_round_up(p.d_out, 4) * 4);
+    } else {
+      q.pack_x = !x_whole;
+      q.pack_w = !w_whole;
+      if (q.pack_x) q.off_x = take((size_t)p.rows * q.in8 * size);
+      if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
+      q.fwd = plan_product(p.rows, p.d_out, p.d_in, step);
+      q.off_part = take(q.fwd.part_bytes);
+    }
+  } else {
+    q.pack_x = !x_whole;
+    q.pack_w = !w_whole;
+    if (q.pack_x) q.off_x = take((size_t)p.rows * q.in8 * size);
+    if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
+    q.dz = p.act != ABS_ACT_NONE || !(dy_ok && p.d_out % piece == 0 && p.lddy % piece == 0);
+    if (q.dz) q.off_dz = take((size_t)p.rows * q.out8 * size);
+    const int cols = (p.d_out + 31) / 32;
+    q.sum_rows = (int)std::max<int64_t>(1, std::min<int64_t>((p.rows + 31) / 32, std::max(1, 4096 / cols)));
+    q.off_sums = take((size_t)q.sum_rows * p.d_out * 4);
+    q.dx = plan_product(p.rows, p.d_in, p.d_out, step);
+    q.dw = plan_product(p.d_in, p.d_out, p.rows, step);
+    q.off_part = take(std::max(q.dx.part_bytes, q.dw.part_bytes));
+  }
+  q.bytes = o;
+  return q;
+}
+
+const char* linear_problem(const abs_linear* p, bool backward) {
+  if (!p) return "linear: the description is NULL";
+  if (p->dtype != ABS_X_FP32 && p->dtype != ABS_X_BF16) return "linear: dtype must be ABS_X_FP32 or ABS_X_BF16";
+  if (p->act < ABS_ACT_NONE || p->act > ABS_ACT_GELU) return "linear: act must be 0..3";
+  if (p->rows < 0 || p->rows > 0x7FFFFFFF) return "linear: rows must be in [0, 2^31)";
+  if (p->d_in < 1 || p->d_out < 1 || p->d_in > 1 << 20 || p->d_out > 1 << 20) return "linear: d_in and d_out must be in [1, 2^20]";
+  constexpr int64_t most = 1ll << 32;
+  if (p->ldx < p->d_in || p->ldw < p->d_out || p->ldx >= most || p->ldw >= most) return "linear: a pitch is below the row's length, or 2^32 or more";
+  const int64_t wide = std::max(p->d_in, p->d_out) / kTile + 1, narrow = std::min(p->d_in, p->d_out) / kTile + 1;
+  if (std::max(p->rows / kTile + 1, narrow) * wide > 1 << 22) return "linear: the result has more than 2^22 tiles of 128 x 128";
+  (void)backward;
+  return nullptr;
+}
+bool bad_pitch(int64_t ld, int64_t cols) { return ld < cols || ld >= 1ll << 32; }
+
+template <typename T>
+hipError_t pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd, hipStream_t s) {
+  linear_pack_kernel<T><<<few_blocks(rows * (ldd / kPiece<T>)), 256, 0, s>>>((const T*)src, ld, rows, cols, (T*)dst, ldd);
+  return hipGetLastError();
+}
+
+template <typename T, bool ATR, bool BTR>
+hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, hipStream_t s) {
+  g.mt = q.mt; g.nt = q.nt; g.nsplit = q.nsplit; g.steps_per_split = q.steps_per_split;
+  const int total = q.mt * q.nt * q.nsplit;
+  Epilogue<T> join = g.e;
+  join.ldpart = (int64_t)op_round_up(g.N, 4);
+  join.part_stride = g.M * join.ldpart;
+  join.part = part;
+  if (q.nsplit > 1) g.e = join;
+  else g.e.part = nullptr;
+  const dim3 grid((unsigned)((total + 7) / 8 * 8));
+  if (total > 256) linear_tile_kernel<T, ATR, BTR, 2><<<grid, 256, 0, s>>>(g);
+  else             linear_tile_kernel<T, ATR, BTR, 4><<<grid, 256, 0, s>>>(g);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && q.nsplit > 1) {
+    linear_join_kernel<T><<<few_blocks(g.M * ((g.N + kPiece<T> - 1) / kPiece<T>)), 256, 0, s>>>(join, g.M, g.N, q.nsplit);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+// a 16-byte piece of columns as one access, in every array
+template <typename T>
+bool pieces_ok(int64_t N, std::initializer_list<std::pair<const void*, int64_t>> arrays) {
+  if (N % kPiece<T>) return false;
+  for (const auto& a : arrays)
+    if (a.first && (a.second % kPiece<T> || !op_aligned(a.first, 16))) return false;
+  return true;
+}
+
+template <typename T, int V>
+hipError_t launch_rows(const abs_linear& p, const LinearPlan& q, const void* x, const void* w, float* part, hipStream_t s) {
+  const dim3 grid((unsigned)((p.d_out + 8 * V - 1) / (8 * V)), (unsigned)q.runs);
+  const int64_t ldpart = (int64_t)op_round_up(p.d_out, 4);
+#define ABS_ROWS(R_) linear_rows_kernel<T, V, R_><<<grid, 256, 0, s>>>((const T*)x, p.ldx, (const T*)w, p.ldw, (int)p.rows, p.d_in, p.d_out, q.run, \
+                                                                       part, ldpart, p.rows * ldpart)
+  if (p.rows == 1) ABS_ROWS(1);
+  else if (p.rows <= 2) ABS_ROWS(2);
+  else if (p.rows <= 4) ABS_ROWS(4);
+  else ABS_ROWS(8);
+#undef ABS_ROWS
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, const void* w, const float* b, const void* r, void* y, void* z,
+                       char* ws, hipStream_t s) {
+  Epilogue<T> e{};
+  e.bias = b; e.r = (const T*)r; e.y = (T*)y; e.z = (T*)z;
+  e.ldr = p.ldr; e.ldy = p.ldy; e.ldz = p.ldz; e.act = p.act;
+  e.vec = pieces_ok<T>(p.d_out, {{r, p.ldr}, {y, p.ldy}, {z, p.ldz}}) && (!b || op_aligned(b, 16));
+  float* part = (float*)(ws + q.off_part);
+  if (q.few) {
+    hipError_t err = q.V == kPiece<T> ? launch_rows<T, kPiece<T>>(p, q, x, w, part, s) : launch_rows<T, 1>(p, q, x, w, part, s);
+    if (err != hipSuccess) return err;
+    e.part = part;
+    e.ldpart = (int64_t)op_round_up(p.d_out, 4);
+    e.part_stride = p.rows * e.ldpart;
+    linear_join_kernel<T><<<few_blocks(p.rows * ((p.d_out + kPiece<T> - 1) / kPiece<T>)), 256, 0, s>>>(e, p.rows, p.d_out, q.runs);
+    return hipGetLastError();
+  }
+  GemmArgs<T> g{};
+  g.A = (const T*)x; g.lda = p.ldx; g.B = (const T*)w; g.ldb = p.ldw;
+  hipError_t err = hipSuccess;
+  if (q.pack_x) { g.A = (const T*)(ws + q.off_x); g.lda = q.in8; err = pack<T>(x, p.ldx, p.rows, p.d_in, ws + q.off_x, q.in8, s); }
+  if (err == hipSuccess && q.pack_w) { g.B = (const T*)(ws + q.off_w); g.ldb = q.out8; err = pack<T>(w, p.ldw, p.d_in, p.d_out, ws + q.off_w, q.out8, s); }
+  if (err != hipSuccess) return err;
+  g.M = p.rows; g.N = p.d_out; g.K = p.d_in; g.nc = q.out8; g.mc = 0;
+  g.e = e;
+  return run_product<T, false, true>(q.fwd, g, part, s);
+}
+
+template <typename T>
+hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw,
+                        float* db, char* ws, hipStream_t s) {
+  constexpr int V = kPiece<T>;
+  hipError_t err = hipSuccess;
+  const T* dz = (const T*)dy;
+  int64_t lddz = p.lddy;
+  const bool products = dx || dw;
+  float* sums = db ? (float*)(ws + q.off_sums) : nullptr;
+  if ((q.dz && products) || db) {
+    T* out = q.dz && products ? (T*)(ws + q.off_dz) : nullptr;
+    const bool whole = p.d_out % V == 0 && p.lddy % V == 0 && op_aligned(dy, 16) && (p.act == ABS_ACT_NONE || (p.ldz % V == 0 && op_aligned(z, 16)));
+    const int per = whole ? 32 * V : 32;
+    const dim3 grid((unsigned)((p.d_out + per - 1) / per), (unsigned)q.sum_rows);
+    if (whole) linear_dz_kernel<T, V><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
+    else       linear_dz_kernel<T, 1><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
+    err = hipGetLastError();
+    if (err == hipSuccess && out && q.out8 != p.d_out) {       // the pieces' ends meet zeros in dx
+      linear_zero_kernel<T><<<few_blocks(p.rows * (q.out8 - p.d_out)), 256, 0, s>>>(out + p.d_out, q.out8, p.rows, q.out8 - p.d_out);
+      err = hipGetLastError();
+    }
+    if (err == hipSuccess && db) {
+      linear_db_kernel<<<dim3((unsigned)((p.d_out + 31) / 32)), 256, 0, s>>>(sums, q.sum_rows, p.d_out, db);
+      err = hipGetLastError();
+    }
+    if (out) { dz = out; lddz = q.out8; }
+  }
+  float* part = (float*)(ws + q.off_part);
+  if (err == hipSuccess && dx) {
+    GemmArgs<T> g{};
+    g.A = dz; g.lda = lddz; g.B = (const T*)w; g.ldb = p.ldw;
+    if (q.pack_w) { g.B = (const T*)(ws + q.off_w); g.ldb = q.out8; err = pack<T>(w, p.ldw, p.d_in, p.d_out, ws + q.off_w, q.out8, s); }
+    g.M = p.rows; g.N = p.d_in; g.K = p.d_out;
+    g.e.y = (T*)dx; g.e.ldy = p.lddx; g.e.vec = pieces_ok<T>(p.d_in, {{dx, p.lddx}});
+    if (err == hipSuccess) err = run_product<T, false, false>(q.dx, g, part, s);
+  }
+  if (err == hipSuccess && dw) {
+    GemmArgs<T> g{};
+    g.A = (const T*)x; g.lda = p.ldx; g.B = dz; g.ldb = lddz;
+    if (q.pack_x) { g.A = (const T*)(ws + q.off_x); g.lda = q.in8; err = pack<T>(x, p.ldx, p.rows, p.d_in, ws + q.off_x, q.in8, s); }
+    g.M = p.d_in; g.N = p.d_out; g.K = p.rows; g.mc = q.in8; g.nc = q.out8;
+    g.e.y = (T*)dw; g.e.ldy = p.lddw; g.e.vec = pieces_ok<T>(p.d_out, {{dw, p.lddw}});
+    if (err == hipSuccess) err = run_product<T, true, true>(q.dw, g, part, s);
+  }
+  return err;
+}
+
+}  // namespace
+}  // namespace abs_impl
+
+using namespace abs_impl;
+
+extern "C" {
+
+size_t abs_linear_workspace_size(const abs_linear* p, int32_t backward, int32_t aligned) {
+  if (const char* why = linear_problem(p, backward != 0)) { op_fail(ABS_E_ARG, why); return 0; }
+  return p->rows ? linear_plan(*p, backward != 0, aligned != 0, aligned != 0, aligned != 0).bytes : 0;
+}
+
+int abs_linear_forward(const abs_linear* p, const void* d_x, const void* d_w, const float* d_b, const void* d_r,
+                       void* d_y, void* d_z, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (const char* why = linear_problem(p, false)) return op_fail(ABS_E_ARG, why);
+  if (bad_pitch(p->ldy, p->d_out) || (d_z && bad_pitch(p->ldz, p->d_out)) || (d_r && bad_pitch(p->ldr, p->d_out)))
+    return op_fail(ABS_E_ARG, "linear: a pitch is below the row's length, or 2^32 or more");
+  if (p->rows == 0) return ABS_OK;
+  if (!d_x || !d_w || !d_y) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
+  const uintptr_t all = (uintptr_t)d_x | (uintptr_t)d_w | (uintptr_t)d_r | (uintptr_t)d_y | (uintptr_t)d_z;
+  if (all & (uintptr_t)(op_size(p->dtype) - 1) || (uintptr_t)d_b & 3) return op_fail(ABS_E_ARG, "linear: a pointer is not aligned to its elements");
+  const LinearPlan q = linear_plan(*p, false, op_aligned(d_x, 16), op_aligned(d_w, 16), true);
+  if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "linear: d_workspace must be 256-byte aligned");
+  if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "linear: workspace too small");
+  const hipError_t e = p->dtype == ABS_X_BF16
+      ? forward_run<uint16_t>(*p, q, d_x, d_w, d_b, d_r, d_y, d_z, (char*)d_workspace, (hipStream_t)hip_stream)
+      : forward_run<float>(*p, q, d_x, d_w, d_b, d_r, d_y, d_z, (char*)d_workspace, (hipStream_t)hip_stream);
+  return op_hip("abs_linear_forward", e);
+}
+
+int abs_linear_backward(const abs_linear* p, const void* d_x, const void* d_w, const void* d_z, const void* d_dy,
+                        void* d_dx, void* d_dw, float* d_db, void* d_workspace, size_t workspace_bytes,
+                        void* hip_stream) {
+  if (const char* why = linear_problem(p, true)) return op_fail(ABS_E_ARG, why);
+  if (bad_pitch(p->lddy, p->d_out) || (d_dx && bad_pitch(p->lddx, p->d_in)) || (d_dw && bad_pitch(p->lddw, p->d_out)) ||
+      (p->act != ABS_ACT_NONE && bad_pitch(p->ldz, p->d_out)))
+    return op_fail(ABS_E_ARG, "linear: a pitch is below the row's length, or 2^32 or more");
+  const uintptr_t all = (uintptr_t)d_x | (uintptr_t)d_w | (uintptr_t)d_z | (uintptr_t)d_dy | (uintptr_t)d_dx | (uintptr_t)d_dw;
+  if (all & (uintptr_t)(op_size(p->dtype) - 1) || (uintptr_t)d_db & 3) return op_fail(ABS_E_ARG, "linear: a pointer is not aligned to its elements");
+  const hipStream_t s = (hipStream_t)hip_stream;
+  if (p->rows == 0) {                       // sums over nothing
+    hipError_t e = hipSuccess;
+    if (d_dw) {
+      const unsigned blocks = few_blocks((int64_t)p->d_in * p->d_out);
+      if (p->dtype == ABS_X_BF16) linear_zero_kernel<uint16_t><<<blocks, 256, 0, s>>>((uint16_t*)d_dw, p->lddw, p->d_in, p->d_out);
+      else                        linear_zero_kernel<float><<<blocks, 256, 0, s>>>((float*)d_dw, p->lddw, p->d_in, p->d_out);
+      e = hipGetLastError();
+    }
+    if (e == hipSuccess && d_db) { linear_zero_kernel<float><<<few_blocks(p->d_out), 256, 0, s>>>(d_db, p->d_out, 1, p->d_out); e = hipGetLastError(); }
+    return op_hip("abs_linear_backward", e);
+  }
+  if (!d_dy || (d_dw && !d_x) || (d_dx && !d_w) || (p->act != ABS_ACT_NONE && !d_z)) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
+  const LinearPlan q = linear_plan(*p, true, op_aligned(d_x, 16), op_aligned(d_w, 16), op_aligned(d_dy, 16));
+  if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "linear: d_workspace must be 256-byte aligned");
+  if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "linear: workspace too small");
+  const hipError_t e = p->dtype == ABS_X_BF16
+      ? backward_run<uint16_t>(*p, q, d_x, d_w, d_z, d_dy, d_dx, d_dw, d_db, (char*)d_workspace, s)
+      : backward_run<float>(*p, q, d_x, d_w, d_z, d_dy, d_dx, d_dw, d_db, (char*)d_workspace, s);
+  return op_hip("abs_linear_backward", e);
+}
+
+}  // extern "C"

@@ -1,0 +1,801 @@
+// Group normalisation, channels last, with an activation behind it (abs_group_norm_*).
+//
+// What bounds it is memory: the forward pass has to read and write every element once, the backward pass to read x and dy
+// and write dx.  So a group's values stay in registers between the statistics and their use wherever they fit:
+//  * lanes go along the channels in pieces of V elements (16 bytes where alignment and group width allow), groups padded
+//    to a power of two of lanes (SP), several groups side by side (TX = SP gpc lanes: 128 bytes of a position and more, so
+//    that lines are used whole) and PL positions on top: D = TX PL lanes hold one sample's share of gpc groups, NV
+//    pieces each.  A workgroup holds T / D samples.
+//  * a group's sum is then shuffles over powers of two, and, where D is more than a wavefront, one exchange through LDS.
+//  * the variance is the mean of the squared distances from the mean, two passes over registers: nothing cancels.
+// Samples that do not fit (and few large ones, which would leave most CUs idle) are cut into parts along the positions:
+// one launch leaves each part's statistics, the next one joins them and writes.  Groups too wide for that take a
+// plain kernel.
+#include "operators.h"
+
+#include <algorithm>
+
+namespace abs_impl {
+namespace {
+
+constexpr int kMaxLanes = 1024;            // D: lanes of one sample
+constexpr int kWide = 4;                   // pieces across the channels per lane for groups wider than kMaxLanes pieces
+
+template <typename T>
+struct NormArgs {
+  const T* x; const T* dy; const T* dres; T* y;          // y: dx in the backward pass
+  const float* gamma; const float* beta;
+  float* mean; float* rstd;                              // forward: outputs (may be null); backward: inputs
+  int64_t n, S;
+  int C, G, per, act;
+  float eps;
+  int64_t ldx, ldy, lddy, lddres;
+  int slots, SP, gpc, TX, PL, D;                         // pieces of a group; lanes (see above)
+  int chunks;                                            // of gpc groups
+  int parts, PP;                                         // parts of a sample and their positions
+  float* part;                                           // [n][G][parts][2]: mean and squared distances, or the two sums
+  float* rows;                                           // backward: [row_count][2][C] shares of dgamma, dbeta
+  int row_count;
+};
+
+// The exact order of operations that defines h: three roundings, nothing contracted, so that a value at relu's corner is on the same
+// side in both passes.
+__device__ __forceinline__ float norm_xhat(float x, float mean, float rstd) {
+#pragma clang fp contract(off)
+  const float d = x - mean;
+  return d * rstd;
+}
+__device__ __forceinline__ float norm_h(float xhat, float gamma, float beta) {
+#pragma clang fp contract(off)
+  const float s = xhat * gamma;
+  return s + beta;
+}
+
+// Sum of v over the lanes of one sample's group; every lane gets it.  `red`: 16 x 64 floats of LDS, not in use.
+__device__ __forceinline__ float group_sum(float v, int SP, int TX, int D, float* red) {
+  for (int off = 1; off < SP && off < 64; off <<= 1) v += __shfl_xor(v, off);
+  for (int off = TX; off < D && off < 64; off <<= 1) v += __shfl_xor(v, off);
+  if (D > 64) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int cols = SP < 64 ? min(TX, 64) / SP : 1;                  // groups of a wavefront
+    if (SP < 64 ? (lane & (SP - 1)) == 0 && lane < min(TX, 64) : lane == 0) red[wave * 64 + (SP < 64 ? lane / SP : 0)] = v;
+    __syncthreads();
+    const int per_row = TX > 64 ? TX >> 6 : 1;                        // wavefronts of a position
+    const int spread = SP > 64 ? SP >> 6 : 1;                         // ... of a group in it
+    const int w0 = wave & ~((D >> 6) - 1);
+    const int first = TX > 64 ? (wave & (per_row - 1)) & ~(spread - 1) : 0;
+    const int col = SP < 64 ? (lane / SP) & (cols - 1) : 0;
+    v = 0.f;
+    for (int r = first; r < (D >> 6); r += per_row)
+      for (int j = 0; j < spread; ++j) v += red[(w0 + r + j) * 64 + col];
+  }
+  return v;
+}
+
+// Where a thread stands: its sample inside the workgroup, positions p, p + PL, ..., group and piece.
+struct Place {
+  int sb, p, g, slot;
+};
+template <typename T>
+__device__ __forceinline__ Place place_of(const NormArgs<T>& a) {
+  Place q;
+  const int t = threadIdx.x, tx = t & (a.TX - 1);
+  q.sb = t / a.D;
+  q.p = (t & (a.D - 1)) / a.TX;
+  q.g = tx / a.SP;
+  q.slot = tx & (a.SP - 1);
+  return q;
+}
+
+// Forward.  APPLY: one part holds the sample (parts == 1) and the result is written; else only the part's mean and squared
+// distances are left.  CV: pieces across the channels a lane holds (then NV / CV positions).
+template <typename T, int V, int NV, int CV, bool APPLY>
+__global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
+  typedef OpVec<T, V> Vec;
+  constexpr int NP = NV / CV;
+  __shared__ float red[2][16 * 64];
+  const Place q = place_of(a);
+  const int spb = blockDim.x / a.D;
+  const int64_t per_chunk = (a.n + spb - 1) / spb;
+  const int64_t work = per_chunk * a.chunks * a.parts;
+  for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
+    // neighbouring chunks of the same positions on one XCD (workgroups are dealt out over eight), one after the other:
+    // they share lines where a chunk is narrower than one
+    const int64_t per_sample = (int64_t)a.chunks * a.parts, whole = per_chunk / 8 * 8;
+    int64_t si, rest;
+    if (b < whole * per_sample) { const int64_t j = b >> 3; si = j / per_sample * 8 + (b & 7); rest = j % per_sample; }
+    else { const int64_t j = b - whole * per_sample; si = whole + j / per_sample; rest = j % per_sample; }
+    const int chunk = (int)(rest % a.chunks), part = (int)(rest / a.chunks);
+    const int64_t i = si * spb + q.sb;
+    const int g = chunk * a.gpc + q.g;
+    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
+    const bool live = i < a.n && g < a.G;
+    const int64_t base = i * a.S;
+    Vec v[NV];
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int j = 0; j < CV; ++j) {
+        const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
+        if (live && pos < pos1 && s < a.slots)
+          v[k * CV + j] = *(const Vec*)(a.x + (base + pos) * a.ldx + (int64_t)g * a.per + s * V);
+      }
+    float gam[CV * V], bet[CV * V];
+    if (APPLY && a.gamma) {
+#pragma unroll
+      for (int j = 0; j < CV; ++j) {
+        const int s = q.slot + j * a.SP;
+        if (live && s < a.slots) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            gam[j * V + e] = a.gamma[g * a.per + s * V + e];
+            bet[j * V + e] = a.beta[g * a.per + s * V + e];
+          }
+        }
+      }
+    }
+    const float count = (float)((int64_t)(pos1 - pos0) * a.per);
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int j = 0; j < CV; ++j)
+        if (live && pos0 + q.p + k * a.PL < pos1 && q.slot + j * a.SP < a.slots) {
+          float one = 0.f;
+#pragma unroll
+          for (int e = 0; e < V; ++e) one += op_widen(v[k * CV + j].e[e]);
+          sum += one;
+        }
+    const float mean = group_sum(sum, a.SP, a.TX, a.D, red[0]) / count;
+    float dist = 0.f;
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int j = 0; j < CV; ++j)
+        if (live && pos0 + q.p + k * a.PL < pos1 && q.slot + j * a.SP < a.slots) {
+          float one = 0.f;
+#pragma unroll
+          for (int e = 0; e < V; ++e) { const float d = op_widen(v[k * CV + j].e[e]) - mean; one += d * d; }
+          dist += one;
+        }
+    dist = group_sum(dist, a.SP, a.TX, a.D, red[1]);
+    const bool first = live && q.p == 0 && q.slot == 0;
+    if (!APPLY) {
+      if (first) {
+        float* o = a.part + ((i * a.G + g) * a.parts + part) * 2;
+        o[0] = mean; o[1] = dist;
+      }
+    } else {
+      const float rstd = rsqrtf(dist / count + a.eps);
+      if (first && a.mean) { a.mean[i * a.G + g] = mean; a.rstd[i * a.G + g] = rstd; }
+#pragma unroll
+      for (int k = 0; k < NP; ++k)
+#pragma unroll
+        for (int j = 0; j < CV; ++j) {
+          const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
+          if (live && pos < pos1 && s < a.slots) {
+            Vec o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              float h = norm_xhat(op_widen(v[k * CV + j].e[e]), mean, rstd);
+              if (a.gamma) h = norm_h(h, gam[j * V + e], bet[j * V + e]);
+              op_narrow(op_act(h, a.act), o.e[e]);
+            }
+            *(Vec*)(a.y + (base + pos) * a.ldy + (int64_t)g * a.per + s * V) = o;
+          }
+        }
+    }
+    // (red[0] is written again only behind the second sum's barrier, red[1] only behind the first one's)
+  }
+}
+
+// Joins the parts' statistics and writes; a workgroup takes the positions of one part.
+template <typename T, int V>
+__global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
+  typedef OpVec<T, V> Vec;
+  const Place q = place_of(a);
+  const int64_t work = a.n * a.chunks * a.parts;
+  for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
+    const int chunk = (int)(b % a.chunks), part = (int)(b / a.chunks % a.parts);
+    const int64_t i = b / a.chunks / a.parts;
+    const int g = chunk * a.gpc + q.g;
+    if (g >= a.G || q.slot >= a.slots) continue;
+    const float* st = a.part + (i * a.G + g) * a.parts * 2;
+    float mean = 0.f, dist = 0.f;
+    const float inv = 1.0f / ((float)a.S * (float)a.per);
+    for (int k = 0; k < a.parts; ++k) {
+      const float count = (float)(min((int64_t)(k + 1) * a.PP, a.S) - (int64_t)k * a.PP) * (float)a.per;
+      mean += st[2 * k] * (count * inv);
+    }
+    for (int k = 0; k < a.parts; ++k) {
+      const float count = (float)(min((int64_t)(k + 1) * a.PP, a.S) - (int64_t)k * a.PP) * (float)a.per;
+      const float d = st[2 * k] - mean;
+      dist += st[2 * k + 1] + count * d * d;
+    }
+    const float rstd = rsqrtf(dist * inv + a.eps);
+    if (a.mean && part == 0 && q.p == 0 && q.slot == 0) { a.mean[i * a.G + g] = mean; a.rstd[i * a.G + g] = rstd; }
+    float gam[V], bet[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      gam[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] : 1.f;
+      bet[e] = a.gamma ? a.beta[g * a.per + q.slot * V + e] : 0.f;
+    }
+    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
+    const int64_t col = (int64_t)g * a.per + q.slot * V;
+#pragma unroll 4
+    for (int pos = pos0 + q.p; pos < pos1; pos += a.PL) {
+      const Vec v = *(const Vec*)(a.x + (i * a.S + pos) * a.ldx + col);
+      Vec o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) op_narrow(op_act(norm_h(norm_xhat(op_widen(v.e[e]), mean, rstd), gam[e], bet[e]), a.act), o.e[e]);
+      *(Vec*)(a.y + (i * a.S + pos) * a.ldy + col) = o;
+    }
+  }
+}
+
+// Backward.  A workgroup keeps its chunk of channels for all its samples, so that the shares of dgamma and dbeta add up in
+// registers and leave once per workgroup.  APPLY as in the forward pass: else only the parts' two sums (and the shares).
+template <typename T, int V, int NV, int CV, bool APPLY>
+__global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
+  typedef OpVec<T, V> Vec;
+  constexpr int NP = NV / CV;
+  __shared__ float red[2][16 * 64];
+  extern __shared__ float share[];
+  const Place q = place_of(a);
+  const int spb = blockDim.x / a.D;
+  const int chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks;
+  const int g = chunk * a.gpc + q.g;
+  float gam[CV * V], bet[CV * V], sg[CV * V], sb[CV * V];
+#pragma unroll
+  for (int j = 0; j < CV; ++j)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int s = q.slot + j * a.SP;
+      const bool ok = a.gamma && g < a.G && s < a.slots;
+      gam[j * V + e] = ok ? a.gamma[g * a.per + s * V + e] : 1.f;
+      bet[j * V + e] = ok ? a.beta[g * a.per + s * V + e] : 0.f;
+      sg[j * V + e] = sb[j * V + e] = 0.f;
+    }
+  const int64_t work = (a.n + spb - 1) / spb * a.parts;
+  const float inv = 1.0f / ((float)a.S * (float)a.per);
+  for (int64_t b = row; b < work; b += a.row_count) {
+    const int part = (int)(b % a.parts);
+    const int64_t i = b / a.parts * spb + q.sb;
+    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
+    const bool live = i < a.n && g < a.G;
+    const int64_t base = i * a.S;
+    Vec vx[NV], vd[NV];
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int j = 0; j < CV; ++j) {
+        const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
+        if (live && pos < pos1 && s < a.slots) {
+          vx[k * CV + j] = *(const Vec*)(a.x + (base + pos) * a.ldx + (int64_t)g * a.per + s * V);
+          vd[k * CV + j] = *(const Vec*)(a.dy + (base + pos) * a.lddy + (int64_t)g * a.per + s * V);
+        }
+      }
+    const float mean = live ? a.mean[i * a.G + g] : 0.f, rstd = live ? a.rstd[i * a.G + g] : 0.f;
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int j = 0; j < CV; ++j)
+        if (live && pos0 + q.p + k * a.PL < pos1 && q.slot + j * a.SP < a.slots) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float xh = norm_xhat(op_widen(vx[k * CV + j].e[e]), mean, rstd);
+            const float dh = op_widen(vd[k * CV + j].e[e]) * op_act_slope(norm_h(xh, gam[j * V + e], bet[j * V + e]), a.act);
+            const float w = dh * gam[j * V + e];
+            sb[j * V + e] += dh;
+            sg[j * V + e] += dh * xh;
+            s1 += w;
+            s2 += w * xh;
+          }
+        }
+    s1 = group_sum(s1, a.SP, a.TX, a.D, red[0]);
+    s2 = group_sum(s2, a.SP, a.TX, a.D, red[1]);
+    if (!APPLY) {
+      if (live && q.p == 0 && q.slot == 0) {
+        float* o = a.part + ((i * a.G + g) * a.parts + part) * 2;
+        o[0] = s1; o[1] = s2;
+      }
+    } else {
+      const float m1 = s1 * inv, m2 = s2 * inv;
+#pragma unroll
+      for (int k = 0; k < NP; ++k)
+#pragma unroll
+        for (int j = 0; j < CV; ++j) {
+          const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
+          if (live && pos < pos1 && s < a.slots) {
+            const int64_t col = (int64_t)g * a.per + s * V;
+            Vec o, r;
+            if (a.dres) r = *(const Vec*)(a.dres + (base + pos) * a.lddres + col);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const float xh = norm_xhat(op_widen(vx[k * CV + j].e[e]), mean, rstd);
+              const float dh = op_widen(vd[k * CV + j].e[e]) * op_act_slope(norm_h(xh, gam[j * V + e], bet[j * V + e]), a.act);
+              float v = rstd * (dh * gam[j * V + e] - m1 - xh * m2);
+              if (a.dres) v += op_widen(r.e[e]);
+              op_narrow(v, o.e[e]);
+            }
+            *(Vec*)(a.y + (base + pos) * a.ldy + col) = o;
+          }
+        }
+    }
+  }
+  if (!a.rows) return;
+  // the lanes that share a channel: positions and samples of the workgroup
+  const int t = threadIdx.x, lanes = min(a.TX, 64), stack = blockDim.x / (a.TX > 64 ? a.TX : 64);
+  if (CV == 1) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      for (int off = a.TX; off < 64; off <<= 1) { sg[e] += __shfl_xor(sg[e], off); sb[e] += __shfl_xor(sb[e], off); }
+    }
+    if (stack > 1) {                                // [stack][V][TX], dgamma's shares and then dbeta's
+      const int r = t / (a.TX > 64 ? a.TX : 64), tx = t & (a.TX - 1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h) __syncthreads();
+        if (a.TX >= 64 || (t & 63) < lanes) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) share[(r * V + e) * a.TX + tx] = h ? sb[e] : sg[e];
+        }
+        __syncthreads();
+        if (t < a.TX) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            float sum = 0.f;
+            for (int k = 0; k < stack; ++k) sum += share[(k * V + e) * a.TX + t];
+            (h ? sb : sg)[e] = sum;
+          }
+        }
+      }
+    }
+    if (t >= a.TX) return;
+  }
+  if (g < a.G) {
+    float* o = a.rows + (int64_t)row * 2 * a.C + g * a.per;
+#pragma unroll
+    for (int j = 0; j < CV; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const int s = q.slot + j * a.SP;
+        if (s < a.slots) { o[s * V + e] = sg[j * V + e]; o[a.C + s * V + e] = sb[j * V + e]; }
+      }
+  }
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a) {
+  typedef OpVec<T, V> Vec;
+  const Place q = place_of(a);
+  const int64_t work = a.n * a.chunks * a.parts;
+  const float inv = 1.0f / ((float)a.S * (float)a.per);
+  for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
+    const int chunk = (int)(b % a.chunks), part = (int)(b / a.chunks % a.parts);
+    const int64_t i = b / a.chunks / a.parts;
+    const int g = chunk * a.gpc + q.g;
+    if (g >= a.G || q.slot >= a.slots) continue;
+    const float* st = a.part + (i * a.G + g) * a.parts * 2;
+    float m1 = 0.f, m2 = 0.f;
+    for (int k = 0; k < a.parts; ++k) { m1 += st[2 * k]; m2 += st[2 * k + 1]; }
+    m1 *= inv; m2 *= inv;
+    const float mean = a.mean[i * a.G + g], rstd = a.rstd[i * a.G + g];
+    float gam[V], bet[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      gam[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] : 1.f;
+      bet[e] = a.gamma ? a.beta[g * a.per + q.slot * V + e] : 0.f;
+    }
+    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
+    const int64_t col = (int64_t)g * a.per + q.slot * V;
+#pragma unroll 2
+    for (int pos = pos0 + q.p; pos < pos1; pos += a.PL) {
+      const Vec vx = *(const Vec*)(a.x + (i * a.S + pos) * a.ldx + col);
+      const Vec vd = *(const Vec*)(a.dy + (i * a.S + pos) * a.lddy + col);
+      Vec o, r;
+      if (a.dres) r = *(const Vec*)(a.dres + (i * a.S + pos) * a.lddres + col);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float xh = norm_xhat(op_widen(vx.e[e]), mean, rstd);
+        const float dh = op_widen(vd.e[e]) * op_act_slope(norm_h(xh, gam[e], bet[e]), a.act);
+        float v = rstd * (dh * gam[e] - m1 - xh * m2);
+        if (a.dres) v += op_widen(r.e[e]);
+        op_narrow(v, o.e[e]);
+      }
+      *(Vec*)(a.y + (i * a.S + pos) * a.ldy + col) = o;
+    }
+  }
+}
+
+// dgamma, dbeta: the workgroups' shares added in their order, 32 channels x 32 rows of shares at a time
+__global__ __launch_bounds__(1024) void norm_share_sum_kernel(const float* rows, int row_count, int C, float* dgamma, float* dbeta) {
+  __shared__ float s[32][33];
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+  const float* p = rows + (blockIdx.y ? C : 0) + c;
+  float v = 0.f;
+  if (c < C)
+    for (int k = r; k < row_count; k += 32) v += p[(int64_t)k * 2 * C];
+  s[r][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (r == 0 && c < C) {
+    v = 0.f;
+    for (int k = 0; k < 32; ++k) v += s[k][threadIdx.x];
+    (blockIdx.y ? dbeta : dgamma)[c] = v;
+  }
+}
+
+// ---- groups of any width: a workgroup per sample and group, every pass over memory ---------------------
+__device__ __forceinline__ float block_sum(float v, float* red) {
+  for (int off = 1; off < 64; off <<= 1) v += __shfl_xor(v, off);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.f;
+  for (int w = 0; w < (int)blockDim.x >> 6; ++w) v += red[w];
+  return v;
+}
+
+template <typename T, bool BACKWARD>
+__global__ __launch_bounds__(1024) void norm_plain_kernel(NormArgs<T> a) {
+  __shared__ float red[16];
+  const float inv = 1.0f / ((float)a.S * (float)a.per);
+  for (int64_t b = blockIdx.x; b < a.n * a.G; b += gridDim.x) {
+    const int64_t i = b / a.G;
+    const int g = (int)(b % a.G), c0 = g * a.per;
+    float mean, rstd, m1 = 0.f, m2 = 0.f;
+    if (!BACKWARD) {
+      float sum = 0.f;
+      for (int64_t pos = 0; pos < a.S; ++pos)
+        for (int c = threadIdx.x; c < a.per; c += blockDim.x) sum += op_widen(a.x[(i * a.S + pos) * a.ldx + c0 + c]);
+      mean = block_sum(sum, red) * inv;
+      float dist = 0.f;
+      for (int64_t pos = 0; pos < a.S; ++pos)
+        for (int c = threadIdx.x; c < a.per; c += blockDim.x) {
+          const float d = op_widen(a.x[(i * a.S + pos) * a.ldx + c0 + c]) - mean;
+          dist += d * d;
+        }
+      rstd = rsqrtf(block_sum(dist, red) * inv + a.eps);
+      if (threadIdx.x == 0 && a.mean) { a.mean[b] = mean; a.rstd[b] = rstd; }
+    } else {
+      mean = a.mean[b]; rstd = a.rstd[b];
+      float s1 = 0.f, s2 = 0.f;
+      for (int64_t pos = 0; pos < a.S; ++pos)
+        for (int c = threadIdx.x; c < a.per; c += blockDim.x) {
+          const float gam = a.gamma ? a.gamma[c0 + c] : 1.f, bet = a.gamma ? a.beta[c0 + c] : 0.f;
+          const float xh = norm_xhat(op_widen(a.x[(i * a.S + pos) * a.ldx + c0 + c]), mean, rstd);
+          const float w = op_widen(a.dy[(i * a.S + pos) * a.lddy + c0 + c]) * op_act_slope(norm_h(xh, gam, bet), a.act) * gam;
+          s1 += w; s2 += w * xh;
+        }
+      m1 = block_sum(s1, red) * inv;
+      m2 = block_sum(s2, red) * inv;
+    }
+    for (int64_t pos = 0; pos < a.S; ++pos)
+      for (int c = threadIdx.x; c < a.per; c += blockDim.x) {
+        const int64_t at = i * a.S + pos;
+        const float gam = a.gamma ? a.gamma[c0 + c] : 1.f, bet = a.gamma ? a.beta[c0 + c] : 0.f;
+        const float xh = norm_xhat(op_widen(a.x[at * a.ldx + c0 + c]), mean, rstd), h = norm_h(xh, gam, bet);
+        float v;
+        if (!BACKWARD) v = op_act(h, a.act);
+        else {
+          v = rstd * (op_widen(a.dy[at * a.lddy + c0 + c]) * op_act_slope(h, a.act) * gam - m1 - xh * m2);
+          if (a.dres) v += op_widen(a.dres[at * a.lddres + c0 + c]);
+        }
+        op_narrow(v, a.y[at * a.ldy + c0 + c]);
+      }
+  }
+}
+
+// ... and their shares of dgamma, dbeta: a thread per channel, row_count runs of positions.  Stands before norm_plain_kernel, which
+// may write dx over dres but never over x or dy.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_plain_share_kernel(NormArgs<T> a) {
+  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (c >= a.C) return;
+  const int g = (int)c / a.per;
+  const float gam = a.gamma ? a.gamma[c] : 1.f, bet = a.gamma ? a.beta[c] : 0.f;
+  const int64_t total = a.n * a.S;
+  for (int r = blockIdx.y; r < a.row_count; r += gridDim.y) {
+    float sg = 0.f, sb = 0.f;
+    for (int64_t at = r; at < total; at += a.row_count) {
+      const int64_t i = at / a.S;
+      const float xh = norm_xhat(op_widen(a.x[at * a.ldx + c]), a.mean[i * a.G + g], a.rstd[i * a.G + g]);
+      const float dh = op_widen(a.dy[at * a.lddy + c]) * op_act_slope(norm_h(xh, gam, bet), a.act);
+      sg += dh * xh; sb += dh;
+    }
+    a.rows[(int64_t)r * 2 * a.C + c] = sg;
+    a.rows[(int64_t)r * 2 * a.C + a.C + c] = sb;
+  }
+}
+
+// ---- the plan -------------------------------------------------------------------------------------------
+struct NormPlan {
+  int V, NV, CV, threads, blocks;
+  bool plain, split;
+  int slots, SP, gpc, TX, PL, D, chunks, parts, PP, row_count;
+  size_t off_rows, bytes;                  // workspace: parts' statistics, then the shares of dgamma / dbeta
+};
+
+int pow2_up(int64_t x) { int p = 1; while (p < x) p <<= 1; return p; }
+
+// V: elements of a piece that all pointers, pitches and the group width allow (the same for every operand).
+NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
+  NormPlan q{};
+  const int size = op_size(p.dtype), per = p.channels / p.groups;
+  const int64_t S = p.spatial;
+  q.V = V; q.CV = 1; q.parts = 1; q.PP = (int)S;
+  q.slots = per / V;
+  q.SP = pow2_up(q.slots);
+  const int nv_most = backward ? 8 : 16;
+  if (q.SP > kMaxLanes) {
+    if (q.SP <= kMaxLanes * kWide && S == 1) {        // one position: pieces across the channels instead
+      q.CV = kWide; q.NV = kWide; q.SP = kMaxLanes;
+      q.gpc = 1; q.TX = q.D = kMaxLanes; q.PL = 1; q.chunks = p.groups;
+    } else {
+      q.plain = true;
+    }
+  } else {
+    // groups side by side: 128 bytes of a position, more while a sample has less than a wavefront's pieces
+    const int g_most = std::min(pow2_up(p.groups), kMaxLanes / q.SP);
+    q.gpc = 1;
+    while (q.gpc < g_most && ((int64_t)q.gpc * per * size < 128 || q.gpc * q.SP * S < 256)) q.gpc *= 2;
+    // ... fewer, down to 32 bytes, where only that lets a workgroup hold a sample
+    auto fits = [&](int gpc) { return (int64_t)gpc * q.SP * pow2_up((S + nv_most - 1) / nv_most) <= kMaxLanes; };
+    int gpc = q.gpc;
+    while (gpc > 1 && !fits(gpc) && (int64_t)(gpc / 2) * per * size >= 32) gpc /= 2;
+    if (fits(gpc)) q.gpc = gpc; else q.split = true;
+    q.TX = q.gpc * q.SP;
+    q.chunks = (p.groups + q.gpc - 1) / q.gpc;
+    // few workgroups with much to do each: parts as well
+    if (!q.split && p.n * q.chunks < 128 && S * q.TX >= 4096) q.split = true;
+    if (q.split) {
+      const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, p.n * q.chunks));       // parts that fill the chip
+      const int pl = std::max(1, std::min(kMaxLanes, std::max(256, q.TX)) / q.TX);
+      int64_t pp = (S + want - 1) / want;
+      const int most = pl * nv_most;
+      pp = std::max<int64_t>(pp, (1024 + q.TX - 1) / q.TX);         // (16 KB of 16-byte pieces)
+      if (pp > most) pp = most;
+      q.NV = pp <= pl ? 1 : pp <= 4 * pl ? 4 : nv_most;
+      q.PL = pow2_up((pp + q.NV - 1) / q.NV);
+      q.PP = q.PL * q.NV;
+      q.parts = (int)((S + q.PP - 1) / q.PP);
+      q.D = q.TX * q.PL;
+    } else {
+      // pieces per lane: few lanes per sample keep sums inside a wavefront, more than 256 only where a sample needs them
+      q.NV = nv_most;
+      for (int nv : {1, 4, nv_most})
+        if ((int64_t)q.TX * pow2_up((S + nv - 1) / nv) <= 256) { q.NV = nv; break; }
+      q.PL = pow2_up((S + q.NV - 1) / q.NV);
+      q.D = q.TX * q.PL;
+    }
+  }
+  size_t o = 0;
+  if (q.plain) {
+    q.threads = 1024;
+    q.blocks = (int)std::min<int64_t>(p.n * p.groups, 4096);
+    q.row_count = (int)std::min<int64_t>(64, p.n * S);
+  } else {
+    q.threads = q.split ? q.D : std::max(q.D, 256);
+    const int spb = q.threads / q.D;
+    const int64_t work = (p.n + spb - 1) / spb * q.parts;                       // per chunk
+    if (backward) {
+      // enough workgroups for two to eight on every CU, few enough that the shares they leave stay small
+      const int64_t fill = std::max<int64_t>(1, (int64_t)256 * (2048 / q.threads) / q.chunks);
+      q.row_count = (int)std::max<int64_t>(1, std::min<int64_t>(work, fill));
+      q.blocks = q.row_count * q.chunks;
+    } else {
+      q.blocks = (int)std::min<int64_t>(work * q.chunks, 1 << 20);
+    }
+    if (q.split) o = op_round_up((size_t)p.n * p.groups * q.parts * 8, 256);
+  }
+  q.off_rows = o;
+  if (backward) o += op_round_up((size_t)std::max(q.row_count, 1) * 2 * p.channels * 4, 256);
+  q.bytes = o;
+  return q;
+}
+
+// the widest piece for a struct's sizes and pitches (pointers are looked at by the calls)
+int norm_piece(const abs_group_norm& p, bool backward, bool res, uintptr_t pointers) {
+  const int size = op_size(p.dtype), per = p.channels / p.groups;
+  for (int V = 16 / size; V > 1; V /= 2) {
+    if (per % V || p.ldx % V || (pointers & (uintptr_t)(V * size - 1))) continue;
+    if (!backward && p.ldy % V == 0) return V;
+    if (backward && p.lddy % V == 0 && p.lddx % V == 0 && (!res || p.lddres % V == 0)) return V;
+  }
+  return 1;
+}
+
+const char* norm_problem(const abs_group_norm* p, bool backward) {
+  if (!p) return "group norm: the description is NULL";
+  if (p->dtype != ABS_X_FP32 && p->dtype != ABS_X_BF16) return "group norm: dtype must be ABS_X_FP32 or ABS_X_BF16";
+  if (p->act < ABS_ACT_NONE || p->act > ABS_ACT_GELU) return "group norm: act must be 0..3";
+  if (p->reserved != 0) return "group norm: reserved must be 0";
+  if (p->n < 0 || p->spatial < 1 || p->spatial > 0x7FFFFFFF || p->n > 0x7FFFFFFF || p->n * p->spatial > 0x7FFFFFFF)
+    return "group norm: n >= 0, spatial >= 1 and n x spatial < 2^31";
+  if (p->channels < 1 || p->channels > 1 << 20) return "group norm: channels must be in [1, 2^20]";
+  if (p->groups < 1 || p->groups > p->channels || p->channels % p->groups) return "group norm: groups must divide channels";
+  if (!(p->eps >= 0.f) || p->eps > 1e30f) return "group norm: eps must be finite and not negative";
+  if (p->ldx < p->channels || (backward ? p->lddy < p->channels || p->lddx < p->channels : p->ldy < p->channels))
+    return "group norm: a pitch is below channels";
+  constexpr int64_t most = 1ll << 40;
+  if (p->ldx >= most || (backward ? p->lddy >= most || p->lddx >= most : p->ldy >= most)) return "group norm: a pitch is 2^40 or more";
+  return nullptr;
+}
+
+// the largest workspace over the pieces the pointers may force
+size_t norm_workspace(const abs_group_norm& p, bool backward) {
+  size_t most = 0;
+  for (int V = 16 / op_size(p.dtype); V >= 1; V /= 2)
+    if ((p.channels / p.groups) % V == 0) most = std::max(most, norm_plan(p, backward, V).bytes);
+  return most;
+}
+
+template <typename T>
+void norm_fill(NormArgs<T>& a, const abs_group_norm& p, const NormPlan& q, char* ws) {
+  a.n = p.n; a.S = p.spatial; a.C = p.channels; a.G = p.groups; a.per = p.channels / p.groups; a.act = p.act; a.eps = p.eps;
+  a.ldx = p.ldx;
+  a.slots = q.slots; a.SP = q.SP; a.gpc = q.gpc; a.TX = q.TX; a.PL = q.PL; a.D = q.D; a.chunks = q.chunks;
+  a.parts = q.parts; a.PP = q.PP; a.row_count = q.row_count;
+  a.part = (float*)ws;
+}
+
+template <typename T, int V>
+hipError_t norm_forward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
+  const dim3 grid((unsigned)q.blocks), block((unsigned)q.threads);
+  if (q.CV == kWide) { norm_forward_kernel<T, V, kWide, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
+#define ABS_NORM_F(NV_)                                                             \
+  if (q.NV == NV_) {                                                                \
+    if (q.split) norm_forward_kernel<T, V, NV_, 1, false><<<grid, block, 0, s>>>(a); \
+    else         norm_forward_kernel<T, V, NV_, 1, true><<<grid, block, 0, s>>>(a);  \
+  }
+  ABS_NORM_F(1) ABS_NORM_F(4) ABS_NORM_F(16)
+#undef ABS_NORM_F
+  if (q.split) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    norm_apply_kernel<T, V><<<grid, block, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, int V>
+hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
+  const dim3 grid((unsigned)q.blocks), block((unsigned)q.threads);
+  const int stack = q.threads / std::max(q.TX, 64);
+  const size_t lds = a.rows && q.CV == 1 && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;     // 32 KB at most
+  if (q.CV == kWide) norm_backward_kernel<T, V, kWide, kWide, true><<<grid, block, 0, s>>>(a);
+#define ABS_NORM_B(NV_)                                                                  \
+  else if (q.NV == NV_) {                                                                \
+    if (q.split) norm_backward_kernel<T, V, NV_, 1, false><<<grid, block, lds, s>>>(a);  \
+    else         norm_backward_kernel<T, V, NV_, 1, true><<<grid, block, lds, s>>>(a);   \
+  }
+  ABS_NORM_B(1) ABS_NORM_B(4) ABS_NORM_B(8)
+#undef ABS_NORM_B
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && q.split) {
+    const dim3 all((unsigned)std::min<int64_t>(a.n * a.chunks * a.parts, 1 << 20));
+    norm_backward_apply_kernel<T, V><<<all, block, 0, s>>>(a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+template <typename T>
+hipError_t norm_run(const abs_group_norm& p, bool backward, NormArgs<T> a, const NormPlan& q, char* ws, float* dgamma, float* dbeta,
+                    hipStream_t s) {
+  norm_fill(a, p, q, ws);
+  a.rows = backward && dgamma ? (float*)(ws + q.off_rows) : nullptr;
+  hipError_t e = hipSuccess;
+  if (q.plain) {
+    if (backward) {
+      if (a.rows) {
+        norm_plain_share_kernel<T><<<dim3((unsigned)((p.channels + 255) / 256), (unsigned)q.row_count), 256, 0, s>>>(a);
+        e = hipGetLastError();
+      }
+      if (e == hipSuccess) { norm_plain_kernel<T, true><<<dim3((unsigned)q.blocks), 1024, 0, s>>>(a); e = hipGetLastError(); }
+    } else {
+      norm_plain_kernel<T, false><<<dim3((unsigned)q.blocks), 1024, 0, s>>>(a);
+      e = hipGetLastError();
+    }
+  } else {
+    switch (q.V) {
+      case 8:
+        if constexpr (sizeof(T) == 2) e = backward ? norm_backward_v<T, 8>(a, q, s) : norm_forward_v<T, 8>(a, q, s);
+        break;
+      case 4: e = backward ? norm_backward_v<T, 4>(a, q, s) : norm_forward_v<T, 4>(a, q, s); break;
+      case 2: e = backward ? norm_backward_v<T, 2>(a, q, s) : norm_forward_v<T, 2>(a, q, s); break;
+      default: e = backward ? norm_backward_v<T, 1>(a, q, s) : norm_forward_v<T, 1>(a, q, s); break;
+    }
+  }
+  if (e == hipSuccess && a.rows) {
+    norm_share_sum_kernel<<<dim3((unsigned)((p.channels + 31) / 32), 2), 1024, 0, s>>>(a.rows, q.row_count, p.channels, dgamma, dbeta);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+__global__ void norm_zero_kernel(float* a, float* b, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) { a[i] = 0.f; b[i] = 0.f; }
+}
+
+}  // namespace
+}  // namespace abs_impl
+
+using namespace abs_impl;
+
+extern "C" {
+
+size_t abs_group_norm_workspace_size(const abs_group_norm* p, int32_t backward) {
+  if (const char* why = norm_problem(p, backward != 0)) { op_fail(ABS_E_ARG, why); return 0; }
+  return p->n ? norm_workspace(*p, backward != 0) : 0;
+}
+
+int abs_group_norm_forward(const abs_group_norm* p, const void* d_x, const float* d_gamma, const float* d_beta,
+                           void* d_y, float* d_mean, float* d_rstd, void* d_workspace, size_t workspace_bytes,
+                           void* hip_stream) {
+  if (const char* why = norm_problem(p, false)) return op_fail(ABS_E_ARG, why);
+  if (!d_gamma != !d_beta) return op_fail(ABS_E_ARG, "group norm: gamma and beta come together");
+  if (!d_mean != !d_rstd) return op_fail(ABS_E_ARG, "group norm: mean and rstd come together");
+  if (p->n == 0) return ABS_OK;
+  if (!d_x || !d_y) return op_fail(ABS_E_ARG, "group norm: a device pointer is NULL");
+  const uintptr_t all = (uintptr_t)d_x | (uintptr_t)d_y;
+  if (all & (uintptr_t)(op_size(p->dtype) - 1) || ((uintptr_t)d_gamma | (uintptr_t)d_beta | (uintptr_t)d_mean | (uintptr_t)d_rstd) & 3)
+    return op_fail(ABS_E_ARG, "group norm: a pointer is not aligned to its elements");
+  const NormPlan q = norm_plan(*p, false, norm_piece(*p, false, false, all));
+  if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "group norm: d_workspace must be 256-byte aligned");
+  if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "group norm: workspace too small");
+  hipError_t e;
+  if (p->dtype == ABS_X_BF16) {
+    NormArgs<uint16_t> a{};
+    a.x = (const uint16_t*)d_x; a.y = (uint16_t*)d_y; a.ldy = p->ldy;
+    a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd;
+    e = norm_run(*p, false, a, q, (char*)d_workspace, nullptr, nullptr, (hipStream_t)hip_stream);
+  } else {
+    NormArgs<float> a{};
+    a.x = (const float*)d_x; a.y = (float*)d_y; a.ldy = p->ldy;
+    a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd;
+    e = norm_run(*p, false, a, q, (char*)d_workspace, nullptr, nullptr, (hipStream_t)hip_stream);
+  }
+  return op_hip("abs_group_norm_forward", e);
+}
+
+int abs_group_norm_backward(const abs_group_norm* p, const void* d_x, const float* d_gamma, const float* d_beta,
+                            const float* d_mean, const float* d_rstd, const void* d_dy, const void* d_dres,
+                            void* d_dx, float* d_dgamma, float* d_dbeta, void* d_workspace, size_t workspace_bytes,
+                            void* hip_stream) {
+  if (const char* why = norm_problem(p, true)) return op_fail(ABS_E_ARG, why);
+  if (!d_gamma != !d_beta) return op_fail(ABS_E_ARG, "group norm: gamma and beta come together");
+  if (!d_dgamma != !d_dbeta) return op_fail(ABS_E_ARG, "group norm: dgamma and dbeta come together");
+  if (d_dres && (p->lddres < p->channels || p->lddres >= 1ll << 40)) return op_fail(ABS_E_ARG, "group norm: a pitch is below channels");
+  const uintptr_t f = (uintptr_t)d_gamma | (uintptr_t)d_beta | (uintptr_t)d_mean | (uintptr_t)d_rstd | (uintptr_t)d_dgamma | (uintptr_t)d_dbeta;
+  const uintptr_t all = (uintptr_t)d_x | (uintptr_t)d_dy | (uintptr_t)d_dx | (uintptr_t)d_dres;
+  if (all & (uintptr_t)(op_size(p->dtype) - 1) || f & 3) return op_fail(ABS_E_ARG, "group norm: a pointer is not aligned to its elements");
+  if (p->n == 0) {
+    if (!d_dgamma) return ABS_OK;
+    norm_zero_kernel<<<dim3((unsigned)((p->channels + 255) / 256)), 256, 0, (hipStream_t)hip_stream>>>(d_dgamma, d_dbeta, p->channels);
+    return op_hip("abs_group_norm_backward", hipGetLastError());
+  }
+  if (!d_x || !d_dy || !d_dx || !d_mean || !d_rstd) return op_fail(ABS_E_ARG, "group norm: a device pointer is NULL");
+  const NormPlan q = norm_plan(*p, true, norm_piece(*p, true, d_dres != nullptr, all));
+  if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "group norm: d_workspace must be 256-byte aligned");
+  if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "group norm: workspace too small");
+  hipError_t e;
+  if (p->dtype == ABS_X_BF16) {
+    NormArgs<uint16_t> a{};
+    a.x = (const uint16_t*)d_x; a.dy = (const uint16_t*)d_dy; a.dres = (const uint16_t*)d_dres; a.y = (uint16_t*)d_dx;
+    a.ldy = p->lddx; a.lddy = p->lddy; a.lddres = p->lddres;
+    a.gamma = d_gamma; a.beta = d_beta; a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
+    e = norm_run(*p, true, a, q, (char*)d_workspace, d_dgamma, d_dbeta, (hipStream_t)hip_stream);
+  } else {
+    NormArgs<float> a{};
+    a.x = (const float*)d_x; a.dy = (const float*)d_dy; a.dres = (const float*)d_dres; a.y = (float*)d_dx;
+    a.ldy = p->lddx; a.lddy = p->lddy; a.lddres = p->lddres;
+    a.gamma = d_gamma; a.beta = d_beta; a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
+    e = norm_run(*p, true, a, q, (char*)d_workspace, d_dgamma, d_dbeta, (hipStream_t)hip_stream);
+  }
+  return op_hip("abs_group_norm_backward", e);
+}
+
+}  // extern "C"
