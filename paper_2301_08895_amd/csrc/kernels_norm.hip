@@ -19,7 +19,7 @@ namespace abs_impl {
 namespace {
 
 constexpr int kMaxLanes = 1024;            // D: lanes of one sample
-constexpr int kWide = 4;                   // pieces across the channels per lane for groups wider than kMaxLanes pieces
+constexpr int kWide = 4;                   // pieces across the channels per lane, for groups of more than kMaxLanes single elements
 
 template <typename T>
 struct NormArgs {
@@ -31,11 +31,13 @@ struct NormArgs {
   float eps;
   int64_t ldx, ldy, lddy, lddres;
   int slots, SP, gpc, TX, PL, D;                         // pieces of a group; lanes (see above)
-  int chunks;                                            // of gpc groups
-  int parts, PP;                                         // parts of a sample and their positions
+  uint32_t chunks;                                       // of gpc groups
+  uint32_t parts;                                        // of a sample
+  int PP;                                                // positions of a part
+  uint32_t work;                                         // workgroup's shares: (samples / samples of a workgroup) x parts x chunks
   float* part;                                           // [n][G][parts][2]: mean and squared distances, or the two sums
   float* rows;                                           // backward: [row_count][2][C] shares of dgamma, dbeta
-  int row_count;
+  uint32_t row_count;
 };
 
 // The exact order of operations that defines h: three roundings, nothing contracted, so that a value at relu's corner is on the same
@@ -55,7 +57,7 @@ __device__ __forceinline__ float norm_h(float xhat, float gamma, float beta) {
 __device__ __forceinline__ float group_sum(float v, int SP, int TX, int D, float* red) {
   for (int off = 1; off < SP && off < 64; off <<= 1) v += __shfl_xor(v, off);
   for (int off = TX; off < D && off < 64; off <<= 1) v += __shfl_xor(v, off);
-  if (D > 64) {
+  if (SP > 64 || (D > 64 && D > TX)) {                                // (else a group is inside a wavefront)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int cols = SP < 64 ? min(TX, 64) / SP : 1;                  // groups of a wavefront
     if (SP < 64 ? (lane & (SP - 1)) == 0 && lane < min(TX, 64) : lane == 0) red[wave * 64 + (SP < 64 ? lane / SP : 0)] = v;
@@ -88,63 +90,55 @@ __device__ __forceinline__ Place place_of(const NormArgs<T>& a) {
 }
 
 // Forward.  APPLY: one part holds the sample (parts == 1) and the result is written; else only the part's mean and squared
-// distances are left.  CV: pieces across the channels a lane holds (then NV / CV positions).
-template <typename T, int V, int NV, int CV, bool APPLY>
+// distances are left.  NP positions per lane, CV pieces across the channels of each.  Addresses are a uniform base and a 32-bit
+// offset that walks, so that they cost two registers and not two per piece (with 64 registers of values that decides whether
+// anything spills).
+template <typename T, int V, int NP, int CV, bool APPLY>
 __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
-  typedef OpVec<T, V> Vec;
-  constexpr int NP = NV / CV;
+  typedef Piece<T, V> Vec;
   __shared__ float red[2][16 * 64];
   const Place q = place_of(a);
-  const int spb = blockDim.x / a.D;
-  const int64_t per_chunk = (a.n + spb - 1) / spb;
-  const int64_t work = per_chunk * a.chunks * a.parts;
-  for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
+  const uint32_t spb = blockDim.x / (uint32_t)a.D, per_sample = a.chunks * a.parts, whole = a.work / per_sample / 8 * 8;
+  for (uint32_t b = blockIdx.x; b < a.work; b += gridDim.x) {
     // neighbouring chunks of the same positions on one XCD (workgroups are dealt out over eight), one after the other:
     // they share lines where a chunk is narrower than one
-    const int64_t per_sample = (int64_t)a.chunks * a.parts, whole = per_chunk / 8 * 8;
-    int64_t si, rest;
-    if (b < whole * per_sample) { const int64_t j = b >> 3; si = j / per_sample * 8 + (b & 7); rest = j % per_sample; }
-    else { const int64_t j = b - whole * per_sample; si = whole + j / per_sample; rest = j % per_sample; }
-    const int chunk = (int)(rest % a.chunks), part = (int)(rest / a.chunks);
-    const int64_t i = si * spb + q.sb;
-    const int g = chunk * a.gpc + q.g;
-    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
+    uint32_t si, rest;
+    if (b < whole * per_sample) { const uint32_t j = b >> 3; si = j / per_sample * 8 + (b & 7); rest = j % per_sample; }
+    else { const uint32_t j = b - whole * per_sample; si = whole + j / per_sample; rest = j % per_sample; }
+    const uint32_t chunk = rest % a.chunks, part = rest / a.chunks;
+    const int64_t i0 = (int64_t)si * spb, i = i0 + q.sb;
+    const int g = (int)chunk * a.gpc + q.g;
+    const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
     const bool live = i < a.n && g < a.G;
-    const int64_t base = i * a.S;
-    Vec v[NV];
+    const int have = live ? count_pos : 0;                             // positions of this lane's sample
+    const int64_t col0 = (int64_t)chunk * a.gpc * a.per;
+    const char* const src = (const char*)(a.x + (i0 * a.S + pos0) * a.ldx + col0);
+    const uint32_t lane_col = (uint32_t)(q.g * a.per + q.slot * V);
+    Vec v[NP * CV];
+    {
+      uint32_t off = ((uint32_t)(q.sb * (uint32_t)a.S + q.p) * (uint32_t)a.ldx + lane_col) * (uint32_t)sizeof(T);
+      const uint32_t step = (uint32_t)a.PL * (uint32_t)a.ldx * (uint32_t)sizeof(T);
 #pragma unroll
-    for (int k = 0; k < NP; ++k)
+      for (int k = 0; k < NP; ++k) {
 #pragma unroll
-      for (int j = 0; j < CV; ++j) {
-        const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
-        if (live && pos < pos1 && s < a.slots)
-          v[k * CV + j] = *(const Vec*)(a.x + (base + pos) * a.ldx + (int64_t)g * a.per + s * V);
-      }
-    float gam[CV * V], bet[CV * V];
-    if (APPLY && a.gamma) {
-#pragma unroll
-      for (int j = 0; j < CV; ++j) {
-        const int s = q.slot + j * a.SP;
-        if (live && s < a.slots) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            gam[j * V + e] = a.gamma[g * a.per + s * V + e];
-            bet[j * V + e] = a.beta[g * a.per + s * V + e];
-          }
-        }
+        for (int j = 0; j < CV; ++j)
+          if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) v[k * CV + j].load(src + (off + (uint32_t)(j * a.SP * V * (int)sizeof(T))));
+        off += step;
+        asm volatile("" : "+v"(off));
       }
     }
-    const float count = (float)((int64_t)(pos1 - pos0) * a.per);
+    const float count = (float)count_pos * (float)a.per;
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int j = 0; j < CV; ++j)
-        if (live && pos0 + q.p + k * a.PL < pos1 && q.slot + j * a.SP < a.slots) {
+        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
           float one = 0.f;
 #pragma unroll
-          for (int e = 0; e < V; ++e) one += op_widen(v[k * CV + j].e[e]);
+          for (int e = 0; e < V; ++e) one += v[k * CV + j].at(e);
           sum += one;
+          v[k * CV + j].hide();
         }
     const float mean = group_sum(sum, a.SP, a.TX, a.D, red[0]) / count;
     float dist = 0.f;
@@ -152,11 +146,12 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int j = 0; j < CV; ++j)
-        if (live && pos0 + q.p + k * a.PL < pos1 && q.slot + j * a.SP < a.slots) {
+        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
           float one = 0.f;
 #pragma unroll
-          for (int e = 0; e < V; ++e) { const float d = op_widen(v[k * CV + j].e[e]) - mean; one += d * d; }
+          for (int e = 0; e < V; ++e) { const float d = v[k * CV + j].at(e) - mean; one += d * d; }
           dist += one;
+          v[k * CV + j].hide();
         }
     dist = group_sum(dist, a.SP, a.TX, a.D, red[1]);
     const bool first = live && q.p == 0 && q.slot == 0;
@@ -168,22 +163,35 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
     } else {
       const float rstd = rsqrtf(dist / count + a.eps);
       if (first && a.mean) { a.mean[i * a.G + g] = mean; a.rstd[i * a.G + g] = rstd; }
+      char* const dst = (char*)(a.y + (i0 * a.S + pos0) * a.ldy + col0);
+      const uint32_t step = (uint32_t)a.PL * (uint32_t)a.ldy * (uint32_t)sizeof(T);
 #pragma unroll
-      for (int k = 0; k < NP; ++k)
+      for (int j = 0; j < CV; ++j) {
+        const int s = q.slot + j * a.SP;
+        if (live && s < a.slots) {
+          float gam[V], bet[V];
 #pragma unroll
-        for (int j = 0; j < CV; ++j) {
-          const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
-          if (live && pos < pos1 && s < a.slots) {
-            Vec o;
+          for (int e = 0; e < V; ++e) {
+            gam[e] = a.gamma ? a.gamma[g * a.per + s * V + e] * rstd : rstd;
+            bet[e] = a.gamma ? a.beta[g * a.per + s * V + e] : 0.f;
+          }
+          uint32_t off = ((uint32_t)(q.sb * (uint32_t)a.S + q.p) * (uint32_t)a.ldy + lane_col + (uint32_t)(j * a.SP * V)) * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-              float h = norm_xhat(op_widen(v[k * CV + j].e[e]), mean, rstd);
-              if (a.gamma) h = norm_h(h, gam[j * V + e], bet[j * V + e]);
-              op_narrow(op_act(h, a.act), o.e[e]);
+          for (int k = 0; k < NP; ++k) {
+            if (q.p + k * a.PL < have) {
+              float h[V];
+              Vec o;
+#pragma unroll
+              for (int e = 0; e < V; ++e) h[e] = fmaf(v[k * CV + j].at(e) - mean, gam[e], bet[e]);
+              op_act_all<V>(h, a.act);
+              o.set(h);
+              o.store(dst + off);
             }
-            *(Vec*)(a.y + (base + pos) * a.ldy + (int64_t)g * a.per + s * V) = o;
+            off += step;
+            asm volatile("" : "+v"(off));
           }
         }
+      }
     }
     // (red[0] is written again only behind the second sum's barrier, red[1] only behind the first one's)
   }
@@ -192,59 +200,83 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
 // Joins the parts' statistics and writes; a workgroup takes the positions of one part.
 template <typename T, int V>
 __global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
-  typedef OpVec<T, V> Vec;
+  typedef Piece<T, V> Vec;
   const Place q = place_of(a);
-  const int64_t work = a.n * a.chunks * a.parts;
-  for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-    const int chunk = (int)(b % a.chunks), part = (int)(b / a.chunks % a.parts);
+  for (uint32_t b = blockIdx.x; b < a.work; b += gridDim.x) {
+    const uint32_t chunk = b % a.chunks, part = b / a.chunks % a.parts;
     const int64_t i = b / a.chunks / a.parts;
-    const int g = chunk * a.gpc + q.g;
+    const int g = (int)chunk * a.gpc + q.g;
     if (g >= a.G || q.slot >= a.slots) continue;
-    const float* st = a.part + (i * a.G + g) * a.parts * 2;
+    const float2* st = (const float2*)a.part + (i * a.G + g) * a.parts;
     float mean = 0.f, dist = 0.f;
-    const float inv = 1.0f / ((float)a.S * (float)a.per);
-    for (int k = 0; k < a.parts; ++k) {
-      const float count = (float)(min((int64_t)(k + 1) * a.PP, a.S) - (int64_t)k * a.PP) * (float)a.per;
-      mean += st[2 * k] * (count * inv);
-    }
-    for (int k = 0; k < a.parts; ++k) {
-      const float count = (float)(min((int64_t)(k + 1) * a.PP, a.S) - (int64_t)k * a.PP) * (float)a.per;
-      const float d = st[2 * k] - mean;
-      dist += st[2 * k + 1] + count * d * d;
+    const float inv = 1.0f / ((float)a.S * (float)a.per), full = (float)a.PP * (float)a.per;
+    const uint32_t last = a.parts - 1;
+    const float rest = (float)(a.S - (int64_t)last * a.PP) * (float)a.per;
+#pragma unroll 8
+    for (uint32_t k = 0; k < a.parts; ++k) mean += st[k].x * ((k < last ? full : rest) * inv);
+#pragma unroll 8
+    for (uint32_t k = 0; k < a.parts; ++k) {
+      const float d = st[k].x - mean;
+      dist += fmaf((k < last ? full : rest) * d, d, st[k].y);
     }
     const float rstd = rsqrtf(dist * inv + a.eps);
     if (a.mean && part == 0 && q.p == 0 && q.slot == 0) { a.mean[i * a.G + g] = mean; a.rstd[i * a.G + g] = rstd; }
     float gam[V], bet[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      gam[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] : 1.f;
+      gam[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] * rstd : rstd;
       bet[e] = a.gamma ? a.beta[g * a.per + q.slot * V + e] : 0.f;
     }
-    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
+    const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
     const int64_t col = (int64_t)g * a.per + q.slot * V;
+    const T* src = a.x + (i * a.S + pos0 + q.p) * a.ldx + col;
+    T* dst = a.y + (i * a.S + pos0 + q.p) * a.ldy + col;
 #pragma unroll 4
-    for (int pos = pos0 + q.p; pos < pos1; pos += a.PL) {
-      const Vec v = *(const Vec*)(a.x + (i * a.S + pos) * a.ldx + col);
-      Vec o;
+    for (int pos = q.p; pos < count_pos; pos += a.PL) {
+      Vec v, o;
+      v.load(src);
+      float h[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) op_narrow(op_act(norm_h(norm_xhat(op_widen(v.e[e]), mean, rstd), gam[e], bet[e]), a.act), o.e[e]);
-      *(Vec*)(a.y + (i * a.S + pos) * a.ldy + col) = o;
+      for (int e = 0; e < V; ++e) h[e] = fmaf(v.at(e) - mean, gam[e], bet[e]);
+      op_act_all<V>(h, a.act);
+      o.set(h);
+      o.store(dst);
+      src += a.PL * a.ldx;
+      dst += a.PL * a.ldy;
     }
+  }
+}
+
+// dh of one piece, and xhat
+template <typename T, int V>
+__device__ __forceinline__ void norm_dh(const Piece<T, V>& x, const Piece<T, V>& dy, float mean, float rstd, const float* gam, const float* bet,
+                                        int act, float* xh, float* dh) {
+  float h[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    xh[e] = norm_xhat(x.at(e), mean, rstd);
+    dh[e] = dy.at(e);
+  }
+  if (act != ABS_ACT_NONE) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[e] = norm_h(xh[e], gam[e], bet[e]);
+    op_slope_all<V>(dh, h, act);
   }
 }
 
 // Backward.  A workgroup keeps its chunk of channels for all its samples, so that the shares of dgamma and dbeta add up in
 // registers and leave once per workgroup.  APPLY as in the forward pass: else only the parts' two sums (and the shares).
-template <typename T, int V, int NV, int CV, bool APPLY>
+// Up to four pieces per lane their dh stays in fp32 registers between the sums and dx; eight are computed twice.
+template <typename T, int V, int NP, int CV, bool APPLY>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
-  typedef OpVec<T, V> Vec;
-  constexpr int NP = NV / CV;
+  typedef Piece<T, V> Vec;
+  constexpr bool kKeep = APPLY && NP <= 4;
   __shared__ float red[2][16 * 64];
   extern __shared__ float share[];
   const Place q = place_of(a);
-  const int spb = blockDim.x / a.D;
-  const int chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks;
-  const int g = chunk * a.gpc + q.g;
+  const uint32_t spb = blockDim.x / (uint32_t)a.D;
+  const uint32_t chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks;
+  const int g = (int)chunk * a.gpc + q.g;
   float gam[CV * V], bet[CV * V], sg[CV * V], sb[CV * V];
 #pragma unroll
   for (int j = 0; j < CV; ++j)
@@ -256,42 +288,56 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
       bet[j * V + e] = ok ? a.beta[g * a.per + s * V + e] : 0.f;
       sg[j * V + e] = sb[j * V + e] = 0.f;
     }
-  const int64_t work = (a.n + spb - 1) / spb * a.parts;
+  const uint32_t work = a.work / a.chunks;
   const float inv = 1.0f / ((float)a.S * (float)a.per);
-  for (int64_t b = row; b < work; b += a.row_count) {
-    const int part = (int)(b % a.parts);
-    const int64_t i = b / a.parts * spb + q.sb;
-    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
+  const int64_t col0 = (int64_t)chunk * a.gpc * a.per;
+  const uint32_t lane_col = (uint32_t)(q.g * a.per + q.slot * V), lane_pos = (uint32_t)(q.sb * (uint32_t)a.S + q.p);
+  auto offset = [&](int64_t ld, int j) { return (lane_pos * (uint32_t)ld + lane_col + (uint32_t)(j * a.SP * V)) * (uint32_t)sizeof(T); };
+  for (uint32_t b = row; b < work; b += a.row_count) {
+    const uint32_t part = b % a.parts;
+    const int64_t i0 = (int64_t)(b / a.parts) * spb, i = i0 + q.sb;
+    const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
     const bool live = i < a.n && g < a.G;
-    const int64_t base = i * a.S;
-    Vec vx[NV], vd[NV];
+    const int have = live ? count_pos : 0;
+    const int64_t at = i0 * a.S + pos0;
+    Vec vx[NP * CV], vd[NP * CV];
 #pragma unroll
-    for (int k = 0; k < NP; ++k)
+    for (int j = 0; j < CV; ++j) {
+      uint32_t ox = offset(a.ldx, j), od = offset(a.lddy, j);
+      const char* const px = (const char*)(a.x + at * a.ldx + col0);
+      const char* const pd = (const char*)(a.dy + at * a.lddy + col0);
 #pragma unroll
-      for (int j = 0; j < CV; ++j) {
-        const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
-        if (live && pos < pos1 && s < a.slots) {
-          vx[k * CV + j] = *(const Vec*)(a.x + (base + pos) * a.ldx + (int64_t)g * a.per + s * V);
-          vd[k * CV + j] = *(const Vec*)(a.dy + (base + pos) * a.lddy + (int64_t)g * a.per + s * V);
+      for (int k = 0; k < NP; ++k) {
+        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
+          vx[k * CV + j].load(px + ox);
+          vd[k * CV + j].load(pd + od);
         }
+        ox += (uint32_t)a.PL * (uint32_t)a.ldx * (uint32_t)sizeof(T);
+        od += (uint32_t)a.PL * (uint32_t)a.lddy * (uint32_t)sizeof(T);
+        asm volatile("" : "+v"(ox), "+v"(od));
       }
+    }
     const float mean = live ? a.mean[i * a.G + g] : 0.f, rstd = live ? a.rstd[i * a.G + g] : 0.f;
     float s1 = 0.f, s2 = 0.f;
+    float kept[kKeep ? NP * CV * V : 1];
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int j = 0; j < CV; ++j)
-        if (live && pos0 + q.p + k * a.PL < pos1 && q.slot + j * a.SP < a.slots) {
+        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
+          float xh[V], dh[V];
+          norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, rstd, gam + j * V, bet + j * V, a.act, xh, dh);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float xh = norm_xhat(op_widen(vx[k * CV + j].e[e]), mean, rstd);
-            const float dh = op_widen(vd[k * CV + j].e[e]) * op_act_slope(norm_h(xh, gam[j * V + e], bet[j * V + e]), a.act);
-            const float w = dh * gam[j * V + e];
-            sb[j * V + e] += dh;
-            sg[j * V + e] += dh * xh;
+            const float w = dh[e] * gam[j * V + e];
+            sb[j * V + e] += dh[e];
+            sg[j * V + e] = fmaf(dh[e], xh[e], sg[j * V + e]);
             s1 += w;
-            s2 += w * xh;
+            s2 = fmaf(w, xh[e], s2);
+            if (kKeep) kept[(k * CV + j) * V + e] = w;
           }
+          vx[k * CV + j].hide();
+          if (!kKeep) vd[k * CV + j].hide();
         }
     s1 = group_sum(s1, a.SP, a.TX, a.D, red[0]);
     s2 = group_sum(s2, a.SP, a.TX, a.D, red[1]);
@@ -301,27 +347,43 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
         o[0] = s1; o[1] = s2;
       }
     } else {
-      const float m1 = s1 * inv, m2 = s2 * inv;
+      // dx = rstd w - (rstd m2) xhat - rstd m1
+      const float c1 = -rstd * (s1 * inv), c2 = -rstd * (s2 * inv);
 #pragma unroll
-      for (int k = 0; k < NP; ++k)
+      for (int j = 0; j < CV; ++j) {
+        char* const dst = (char*)(a.y + at * a.ldy + col0);
+        const char* const res = (const char*)(a.dres + at * a.lddres + col0);
+        uint32_t oy = offset(a.ldy, j), orr = offset(a.lddres, j);
 #pragma unroll
-        for (int j = 0; j < CV; ++j) {
-          const int pos = pos0 + q.p + k * a.PL, s = q.slot + j * a.SP;
-          if (live && pos < pos1 && s < a.slots) {
-            const int64_t col = (int64_t)g * a.per + s * V;
+        for (int k = 0; k < NP; ++k) {
+          if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
+            float xh[V], w[V];
+            if constexpr (kKeep) {
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                xh[e] = norm_xhat(vx[k * CV + j].at(e), mean, rstd);
+                w[e] = kept[(k * CV + j) * V + e];
+              }
+            } else {
+              norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, rstd, gam + j * V, bet + j * V, a.act, xh, w);
+#pragma unroll
+              for (int e = 0; e < V; ++e) w[e] *= gam[j * V + e];
+            }
             Vec o, r;
-            if (a.dres) r = *(const Vec*)(a.dres + (base + pos) * a.lddres + col);
+            if (a.dres) r.load(res + orr);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-              const float xh = norm_xhat(op_widen(vx[k * CV + j].e[e]), mean, rstd);
-              const float dh = op_widen(vd[k * CV + j].e[e]) * op_act_slope(norm_h(xh, gam[j * V + e], bet[j * V + e]), a.act);
-              float v = rstd * (dh * gam[j * V + e] - m1 - xh * m2);
-              if (a.dres) v += op_widen(r.e[e]);
-              op_narrow(v, o.e[e]);
+              w[e] = fmaf(rstd, w[e], fmaf(c2, xh[e], c1));
+              if (a.dres) w[e] += r.at(e);
             }
-            *(Vec*)(a.y + (base + pos) * a.ldy + col) = o;
+            o.set(w);
+            o.store(dst + oy);
           }
+          oy += (uint32_t)a.PL * (uint32_t)a.ldy * (uint32_t)sizeof(T);
+          orr += (uint32_t)a.PL * (uint32_t)a.lddres * (uint32_t)sizeof(T);
+          asm volatile("" : "+v"(oy), "+v"(orr));
         }
+      }
     }
   }
   if (!a.rows) return;
@@ -368,55 +430,60 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
 
 template <typename T, int V>
 __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a) {
-  typedef OpVec<T, V> Vec;
+  typedef Piece<T, V> Vec;
   const Place q = place_of(a);
-  const int64_t work = a.n * a.chunks * a.parts;
   const float inv = 1.0f / ((float)a.S * (float)a.per);
-  for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-    const int chunk = (int)(b % a.chunks), part = (int)(b / a.chunks % a.parts);
+  for (uint32_t b = blockIdx.x; b < a.work; b += gridDim.x) {
+    const uint32_t chunk = b % a.chunks, part = b / a.chunks % a.parts;
     const int64_t i = b / a.chunks / a.parts;
-    const int g = chunk * a.gpc + q.g;
+    const int g = (int)chunk * a.gpc + q.g;
     if (g >= a.G || q.slot >= a.slots) continue;
-    const float* st = a.part + (i * a.G + g) * a.parts * 2;
+    const float2* st = (const float2*)a.part + (i * a.G + g) * a.parts;
     float m1 = 0.f, m2 = 0.f;
-    for (int k = 0; k < a.parts; ++k) { m1 += st[2 * k]; m2 += st[2 * k + 1]; }
-    m1 *= inv; m2 *= inv;
+#pragma unroll 8
+    for (uint32_t k = 0; k < a.parts; ++k) { m1 += st[k].x; m2 += st[k].y; }
     const float mean = a.mean[i * a.G + g], rstd = a.rstd[i * a.G + g];
+    const float c1 = -rstd * (m1 * inv), c2 = -rstd * (m2 * inv);
     float gam[V], bet[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       gam[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] : 1.f;
       bet[e] = a.gamma ? a.beta[g * a.per + q.slot * V + e] : 0.f;
     }
-    const int pos0 = part * a.PP, pos1 = (int)min((int64_t)pos0 + a.PP, a.S);
-    const int64_t col = (int64_t)g * a.per + q.slot * V;
+    const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
+    const int64_t at = i * a.S + pos0 + q.p, col = (int64_t)g * a.per + q.slot * V;
+    const T* px = a.x + at * a.ldx + col;
+    const T* pd = a.dy + at * a.lddy + col;
+    const T* pr = a.dres ? a.dres + at * a.lddres + col : nullptr;
+    T* dst = a.y + at * a.ldy + col;
 #pragma unroll 2
-    for (int pos = pos0 + q.p; pos < pos1; pos += a.PL) {
-      const Vec vx = *(const Vec*)(a.x + (i * a.S + pos) * a.ldx + col);
-      const Vec vd = *(const Vec*)(a.dy + (i * a.S + pos) * a.lddy + col);
-      Vec o, r;
-      if (a.dres) r = *(const Vec*)(a.dres + (i * a.S + pos) * a.lddres + col);
+    for (int pos = q.p; pos < count_pos; pos += a.PL) {
+      Vec vx, vd, o, r;
+      vx.load(px); vd.load(pd);
+      if (pr) r.load(pr);
+      float xh[V], dh[V];
+      norm_dh<T, V>(vx, vd, mean, rstd, gam, bet, a.act, xh, dh);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float xh = norm_xhat(op_widen(vx.e[e]), mean, rstd);
-        const float dh = op_widen(vd.e[e]) * op_act_slope(norm_h(xh, gam[e], bet[e]), a.act);
-        float v = rstd * (dh * gam[e] - m1 - xh * m2);
-        if (a.dres) v += op_widen(r.e[e]);
-        op_narrow(v, o.e[e]);
+        dh[e] = fmaf(rstd, dh[e] * gam[e], fmaf(c2, xh[e], c1));
+        if (pr) dh[e] += r.at(e);
       }
-      *(Vec*)(a.y + (i * a.S + pos) * a.ldy + col) = o;
+      o.set(dh);
+      o.store(dst);
+      px += a.PL * a.ldx; pd += a.PL * a.lddy; dst += a.PL * a.ldy;
+      if (pr) pr += a.PL * a.lddres;
     }
   }
 }
 
 // dgamma, dbeta: the workgroups' shares added in their order, 32 channels x 32 rows of shares at a time
-__global__ __launch_bounds__(1024) void norm_share_sum_kernel(const float* rows, int row_count, int C, float* dgamma, float* dbeta) {
+__global__ __launch_bounds__(1024) void norm_share_sum_kernel(const float* rows, uint32_t row_count, int C, float* dgamma, float* dbeta) {
   __shared__ float s[32][33];
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
   const float* p = rows + (blockIdx.y ? C : 0) + c;
   float v = 0.f;
   if (c < C)
-    for (int k = r; k < row_count; k += 32) v += p[(int64_t)k * 2 * C];
+    for (uint32_t k = r; k < row_count; k += 32) v += p[(int64_t)k * 2 * C];
   s[r][threadIdx.x & 31] = v;
   __syncthreads();
   if (r == 0 && c < C) {
@@ -496,7 +563,7 @@ __global__ __launch_bounds__(256) void norm_plain_share_kernel(NormArgs<T> a) {
   const int g = (int)c / a.per;
   const float gam = a.gamma ? a.gamma[c] : 1.f, bet = a.gamma ? a.beta[c] : 0.f;
   const int64_t total = a.n * a.S;
-  for (int r = blockIdx.y; r < a.row_count; r += gridDim.y) {
+  for (uint32_t r = blockIdx.y; r < a.row_count; r += gridDim.y) {
     float sg = 0.f, sb = 0.f;
     for (int64_t at = r; at < total; at += a.row_count) {
       const int64_t i = at / a.S;
@@ -511,9 +578,10 @@ __global__ __launch_bounds__(256) void norm_plain_share_kernel(NormArgs<T> a) {
 
 // ---- the plan -------------------------------------------------------------------------------------------
 struct NormPlan {
-  int V, NV, CV, threads, blocks;
+  int V, NP, CV, threads;
   bool plain, split;
-  int slots, SP, gpc, TX, PL, D, chunks, parts, PP, row_count;
+  int slots, SP, gpc, TX, PL, D, PP;
+  uint32_t chunks, parts, row_count, work, blocks;
   size_t off_rows, bytes;                  // workspace: parts' statistics, then the shares of dgamma / dbeta
 };
 
@@ -527,10 +595,10 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
   q.V = V; q.CV = 1; q.parts = 1; q.PP = (int)S;
   q.slots = per / V;
   q.SP = pow2_up(q.slots);
-  const int nv_most = backward ? 8 : 16;
+  const int np_most = backward ? 8 : 16;
   if (q.SP > kMaxLanes) {
-    if (q.SP <= kMaxLanes * kWide && S == 1) {        // one position: pieces across the channels instead
-      q.CV = kWide; q.NV = kWide; q.SP = kMaxLanes;
+    if (V == 1 && q.SP <= kMaxLanes * kWide && S == 1) {        // single elements of one position: several across the channels
+      q.CV = kWide; q.NP = 1; q.SP = kMaxLanes;
       q.gpc = 1; q.TX = q.D = kMaxLanes; q.PL = 1; q.chunks = p.groups;
     } else {
       q.plain = true;
@@ -541,7 +609,7 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
     q.gpc = 1;
     while (q.gpc < g_most && ((int64_t)q.gpc * per * size < 128 || q.gpc * q.SP * S < 256)) q.gpc *= 2;
     // ... fewer, down to 32 bytes, where only that lets a workgroup hold a sample
-    auto fits = [&](int gpc) { return (int64_t)gpc * q.SP * pow2_up((S + nv_most - 1) / nv_most) <= kMaxLanes; };
+    auto fits = [&](int gpc) { return (int64_t)gpc * q.SP * pow2_up((S + np_most - 1) / np_most) <= kMaxLanes; };
     int gpc = q.gpc;
     while (gpc > 1 && !fits(gpc) && (int64_t)(gpc / 2) * per * size >= 32) gpc /= 2;
     if (fits(gpc)) q.gpc = gpc; else q.split = true;
@@ -553,44 +621,52 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
       const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, p.n * q.chunks));       // parts that fill the chip
       const int pl = std::max(1, std::min(kMaxLanes, std::max(256, q.TX)) / q.TX);
       int64_t pp = (S + want - 1) / want;
-      const int most = pl * nv_most;
+      const int most = pl * np_most;
       pp = std::max<int64_t>(pp, (1024 + q.TX - 1) / q.TX);         // (16 KB of 16-byte pieces)
       if (pp > most) pp = most;
-      q.NV = pp <= pl ? 1 : pp <= 4 * pl ? 4 : nv_most;
-      q.PL = pow2_up((pp + q.NV - 1) / q.NV);
-      q.PP = q.PL * q.NV;
-      q.parts = (int)((S + q.PP - 1) / q.PP);
+      q.NP = pp <= pl ? 1 : pp <= 4 * pl ? 4 : np_most;
+      q.PL = pow2_up((pp + q.NP - 1) / q.NP);
+      q.PP = q.PL * q.NP;
+      q.parts = (uint32_t)((S + q.PP - 1) / q.PP);
       q.D = q.TX * q.PL;
     } else {
-      // pieces per lane: few lanes per sample keep sums inside a wavefront, more than 256 only where a sample needs them
-      q.NV = nv_most;
-      for (int nv : {1, 4, nv_most})
-        if ((int64_t)q.TX * pow2_up((S + nv - 1) / nv) <= 256) { q.NV = nv; break; }
-      q.PL = pow2_up((S + q.NV - 1) / q.NV);
+      q.NP = np_most;
+      for (int np : {1, 4, np_most})
+        if ((int64_t)q.TX * pow2_up((S + np - 1) / np) <= 512) { q.NP = np; break; }
+      q.PL = pow2_up((S + q.NP - 1) / q.NP);
       q.D = q.TX * q.PL;
     }
   }
   size_t o = 0;
+  if (!q.plain) {
+    // a workgroup's samples lie within 32-bit offsets of its first one
+    q.threads = q.split ? q.D : std::max(q.D, 256);
+    // (backward: the more samples share a workgroup, the fewer shares of dgamma and dbeta)
+    if (backward && !q.split)
+      while (q.threads < 1024 && p.n * q.D / (2 * q.threads) * q.chunks >= 512) q.threads *= 2;
+    const int64_t spb = q.threads / q.D, reach = spb * S;
+    const int64_t ld = std::max({p.ldx, backward ? p.lddy : p.ldy, backward ? p.lddx : 0, backward ? p.lddres : 0});
+    const int64_t work = (p.n + spb - 1) / spb * q.parts * q.chunks;
+    if ((double)reach * (double)ld * size >= 4.0e9 || work >= 1ll << 31) { q.plain = true; q.split = false; q.parts = 1; }
+    else q.work = (uint32_t)work;
+  }
   if (q.plain) {
     q.threads = 1024;
-    q.blocks = (int)std::min<int64_t>(p.n * p.groups, 4096);
-    q.row_count = (int)std::min<int64_t>(64, p.n * S);
+    q.blocks = (uint32_t)std::min<int64_t>(p.n * p.groups, 4096);
+    q.row_count = (uint32_t)std::min<int64_t>(64, p.n * S);
   } else {
-    q.threads = q.split ? q.D : std::max(q.D, 256);
-    const int spb = q.threads / q.D;
-    const int64_t work = (p.n + spb - 1) / spb * q.parts;                       // per chunk
     if (backward) {
       // enough workgroups for two to eight on every CU, few enough that the shares they leave stay small
-      const int64_t fill = std::max<int64_t>(1, (int64_t)256 * (2048 / q.threads) / q.chunks);
-      q.row_count = (int)std::max<int64_t>(1, std::min<int64_t>(work, fill));
+      const uint32_t fill = std::max(1u, 256u * (2048u / (uint32_t)q.threads) / q.chunks);
+      q.row_count = std::max(1u, std::min(q.work / q.chunks, fill));
       q.blocks = q.row_count * q.chunks;
     } else {
-      q.blocks = (int)std::min<int64_t>(work * q.chunks, 1 << 20);
+      q.blocks = std::min(q.work, 1u << 20);
     }
     if (q.split) o = op_round_up((size_t)p.n * p.groups * q.parts * 8, 256);
   }
   q.off_rows = o;
-  if (backward) o += op_round_up((size_t)std::max(q.row_count, 1) * 2 * p.channels * 4, 256);
+  if (backward) o += op_round_up((size_t)std::max(q.row_count, 1u) * 2 * p.channels * 4, 256);
   q.bytes = o;
   return q;
 }
@@ -636,18 +712,20 @@ void norm_fill(NormArgs<T>& a, const abs_group_norm& p, const NormPlan& q, char*
   a.n = p.n; a.S = p.spatial; a.C = p.channels; a.G = p.groups; a.per = p.channels / p.groups; a.act = p.act; a.eps = p.eps;
   a.ldx = p.ldx;
   a.slots = q.slots; a.SP = q.SP; a.gpc = q.gpc; a.TX = q.TX; a.PL = q.PL; a.D = q.D; a.chunks = q.chunks;
-  a.parts = q.parts; a.PP = q.PP; a.row_count = q.row_count;
+  a.parts = q.parts; a.PP = q.PP; a.work = q.work; a.row_count = q.row_count;
   a.part = (float*)ws;
 }
 
 template <typename T, int V>
 hipError_t norm_forward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
-  const dim3 grid((unsigned)q.blocks), block((unsigned)q.threads);
-  if (q.CV == kWide) { norm_forward_kernel<T, V, kWide, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
-#define ABS_NORM_F(NV_)                                                             \
-  if (q.NV == NV_) {                                                                \
-    if (q.split) norm_forward_kernel<T, V, NV_, 1, false><<<grid, block, 0, s>>>(a); \
-    else         norm_forward_kernel<T, V, NV_, 1, true><<<grid, block, 0, s>>>(a);  \
+  const dim3 grid(q.blocks), block((unsigned)q.threads);
+  if constexpr (V == 1) {
+    if (q.CV == kWide) { norm_forward_kernel<T, 1, 1, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
+  }
+#define ABS_NORM_F(NP_)                                                             \
+  if (q.NP == NP_) {                                                                \
+    if (q.split) norm_forward_kernel<T, V, NP_, 1, false><<<grid, block, 0, s>>>(a); \
+    else         norm_forward_kernel<T, V, NP_, 1, true><<<grid, block, 0, s>>>(a);  \
   }
   ABS_NORM_F(1) ABS_NORM_F(4) ABS_NORM_F(16)
 #undef ABS_NORM_F
@@ -661,20 +739,22 @@ hipError_t norm_forward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s
 
 template <typename T, int V>
 hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
-  const dim3 grid((unsigned)q.blocks), block((unsigned)q.threads);
+  const dim3 grid(q.blocks), block((unsigned)q.threads);
   const int stack = q.threads / std::max(q.TX, 64);
   const size_t lds = a.rows && q.CV == 1 && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;     // 32 KB at most
-  if (q.CV == kWide) norm_backward_kernel<T, V, kWide, kWide, true><<<grid, block, 0, s>>>(a);
-#define ABS_NORM_B(NV_)                                                                  \
-  else if (q.NV == NV_) {                                                                \
-    if (q.split) norm_backward_kernel<T, V, NV_, 1, false><<<grid, block, lds, s>>>(a);  \
-    else         norm_backward_kernel<T, V, NV_, 1, true><<<grid, block, lds, s>>>(a);   \
+  if constexpr (V == 1) {
+    if (q.CV == kWide) { norm_backward_kernel<T, 1, 1, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
+  }
+#define ABS_NORM_B(NP_)                                                                  \
+  if (q.NP == NP_) {                                                                     \
+    if (q.split) norm_backward_kernel<T, V, NP_, 1, false><<<grid, block, lds, s>>>(a);  \
+    else         norm_backward_kernel<T, V, NP_, 1, true><<<grid, block, lds, s>>>(a);   \
   }
   ABS_NORM_B(1) ABS_NORM_B(4) ABS_NORM_B(8)
 #undef ABS_NORM_B
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && q.split) {
-    const dim3 all((unsigned)std::min<int64_t>(a.n * a.chunks * a.parts, 1 << 20));
+    const dim3 all(std::min(a.work, 1u << 20));
     norm_backward_apply_kernel<T, V><<<all, block, 0, s>>>(a);
     e = hipGetLastError();
   }
@@ -690,12 +770,12 @@ hipError_t norm_run(const abs_group_norm& p, bool backward, NormArgs<T> a, const
   if (q.plain) {
     if (backward) {
       if (a.rows) {
-        norm_plain_share_kernel<T><<<dim3((unsigned)((p.channels + 255) / 256), (unsigned)q.row_count), 256, 0, s>>>(a);
+        norm_plain_share_kernel<T><<<dim3((unsigned)((p.channels + 255) / 256), q.row_count), 256, 0, s>>>(a);
         e = hipGetLastError();
       }
-      if (e == hipSuccess) { norm_plain_kernel<T, true><<<dim3((unsigned)q.blocks), 1024, 0, s>>>(a); e = hipGetLastError(); }
+      if (e == hipSuccess) { norm_plain_kernel<T, true><<<dim3(q.blocks), 1024, 0, s>>>(a); e = hipGetLastError(); }
     } else {
-      norm_plain_kernel<T, false><<<dim3((unsigned)q.blocks), 1024, 0, s>>>(a);
+      norm_plain_kernel<T, false><<<dim3(q.blocks), 1024, 0, s>>>(a);
       e = hipGetLastError();
     }
   } else {

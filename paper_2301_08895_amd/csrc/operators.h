@@ -41,22 +41,106 @@ __device__ __forceinline__ void op_narrow(float f, float& v) { v = f; }
 template <typename T, int V>
 struct alignas(sizeof(T) * V) OpVec { T e[V]; };
 
+// The same held in whole registers: left as an array of 16-bit elements the compiler gives every one a register of its own.
+typedef uint32_t op_u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t op_u32x4 __attribute__((ext_vector_type(4)));
+template <typename T, int V>
+struct Piece {
+  static constexpr int kBytes = V * (int)sizeof(T), kWords = kBytes < 4 ? 1 : kBytes / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const void* p) {
+    if constexpr (kBytes == 16) { const op_u32x4 v = *(const op_u32x4*)p; w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; w[3] = v[3]; }
+    else if constexpr (kBytes == 8) { const op_u32x2 v = *(const op_u32x2*)p; w[0] = v[0]; w[1] = v[1]; }
+    else if constexpr (kBytes == 4) w[0] = *(const uint32_t*)p;
+    else w[0] = *(const uint16_t*)p;
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+  }
+  // forgets what has been computed from the words: they are widened again, not kept widened
+  __device__ __forceinline__ void hide() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
+  }
+  __device__ __forceinline__ void set(const float* f) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) w[e] = __float_as_uint(f[e]);
+    } else if constexpr (V == 1) {
+      w[0] = op_bf16(f[0]);
+    } else {
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        const bf16x2 h = __builtin_convertvector(f32x2{f[2 * i], f[2 * i + 1]}, bf16x2);
+        __builtin_memcpy(&w[i], &h, 4);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(void* p) const {
+    if constexpr (kBytes == 16) *(op_u32x4*)p = op_u32x4{w[0], w[1], w[2], w[3]};
+    else if constexpr (kBytes == 8) *(op_u32x2*)p = op_u32x2{w[0], w[1]};
+    else if constexpr (kBytes == 4) *(uint32_t*)p = w[0];
+    else *(uint16_t*)p = (uint16_t)w[0];
+  }
+};
+
 // ---- activations.  act(z) and act'(z) in fp32; a NaN stays one ----------------------------------------
 __device__ __forceinline__ float op_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }   // 2 ulp
+// The normal distribution function Phi(z) = (1 + erf(z / sqrt 2)) / 2, and e = exp(-z^2 / 2): erfc by the rational form in
+// t = 1 / (1 + p |z| / sqrt 2) of Abramowitz and Stegun, 7.1.26 (|error| of erf <= 1.5e-7), which shares the exponential with the
+// density that the slope needs: 13 operations and two transcendental ones where erff and a further exponential take about 60.
+__device__ __forceinline__ float op_phi(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+  e = __expf(-x * x);
+  const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  const float tail = 0.5f * q * e;                       // Phi(-|z|)
+  return z < 0.f ? tail : 1.0f - tail;
+}
 template <int ACT>
 __device__ __forceinline__ float op_act(float z) {
   if (ACT == ABS_ACT_RELU) return z < 0.f ? 0.f : z;
   if (ACT == ABS_ACT_SILU) return z * op_sigmoid(z);
-  if (ACT == ABS_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  if (ACT == ABS_ACT_GELU) { float e; return z * op_phi(z, e); }
   return z;
 }
 template <int ACT>
 __device__ __forceinline__ float op_act_slope(float z) {
   if (ACT == ABS_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (ACT == ABS_ACT_SILU) { const float p = op_sigmoid(z); return p * (1.0f + z * (1.0f - p)); }
-  if (ACT == ABS_ACT_GELU)
-    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+  if (ACT == ABS_ACT_SILU) { const float p = op_sigmoid(z); return fmaf(z * p, 1.0f - p, p); }
+  if (ACT == ABS_ACT_GELU) { float e; const float c = op_phi(z, e); return fmaf(z * 0.39894228040143268f, e, c); }
   return 1.f;
+}
+// N values at once, the activation a uniform run-time value: one branch
+template <int N>
+__device__ __forceinline__ void op_act_all(float* h, int act) {
+  if (act == ABS_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_RELU>(h[i]);
+  } else if (act == ABS_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_SILU>(h[i]);
+  } else if (act == ABS_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_GELU>(h[i]);
+  }
+}
+// d[i] *= act'(h[i])
+template <int N>
+__device__ __forceinline__ void op_slope_all(float* d, const float* h, int act) {
+  if (act == ABS_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] *= op_act_slope<ABS_ACT_RELU>(h[i]);
+  } else if (act == ABS_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] *= op_act_slope<ABS_ACT_SILU>(h[i]);
+  } else if (act == ABS_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] *= op_act_slope<ABS_ACT_GELU>(h[i]);
+  }
 }
 // the same with the activation as a uniform run-time value
 __device__ __forceinline__ float op_act(float z, int act) {
