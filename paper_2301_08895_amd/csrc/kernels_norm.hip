@@ -53,10 +53,28 @@ __device__ __forceinline__ float norm_h(float xhat, float gamma, float beta) {
   return s + beta;
 }
 
+// v + v of the lane whose number differs in one bit (`off`, a power of two below 64); kFlat: the lanes that differ in lower bits hold equal
+// values already, so a mirror image does.  Cross-lane adds where there are such, LDS's swizzle (no addresses) for the others.
+template <bool kFlat>
+__device__ __forceinline__ float add_xor(float v, int off) {
+#define ABS_DPP(ctrl_) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl_, 0xF, 0xF, true))
+#define ABS_SWZ(x_) __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), ((x_) << 10) | 0x1F))
+  switch (off) {
+    case 1: return v + ABS_DPP(0xB1);                     // quad_perm [1, 0, 3, 2]
+    case 2: return v + ABS_DPP(0x4E);                     // quad_perm [2, 3, 0, 1]
+    case 4: return v + (kFlat ? ABS_DPP(0x141) : ABS_SWZ(4));   // row_half_mirror
+    case 8: return v + (kFlat ? ABS_DPP(0x140) : ABS_SWZ(8));   // row_mirror
+    case 16: return v + ABS_SWZ(16);
+    default: return v + __shfl_xor(v, 32);
+  }
+#undef ABS_DPP
+#undef ABS_SWZ
+}
+
 // Sum of v over the lanes of one sample's group; every lane gets it.  `red`: 16 x 64 floats of LDS, not in use.
 __device__ __forceinline__ float group_sum(float v, int SP, int TX, int D, float* red) {
-  for (int off = 1; off < SP && off < 64; off <<= 1) v += __shfl_xor(v, off);
-  for (int off = TX; off < D && off < 64; off <<= 1) v += __shfl_xor(v, off);
+  for (int off = 1; off < SP && off < 64; off <<= 1) v = add_xor<true>(v, off);
+  for (int off = TX; off < D && off < 64; off <<= 1) v = add_xor<false>(v, off);
   if (SP > 64 || (D > 64 && D > TX)) {                                // (else a group is inside a wavefront)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int cols = SP < 64 ? min(TX, 64) / SP : 1;                  // groups of a wavefront
@@ -89,6 +107,16 @@ __device__ __forceinline__ Place place_of(const NormArgs<T>& a) {
   return q;
 }
 
+// Workgroup b of (samples x rest): neighbouring chunks of the same positions on one XCD (workgroups are dealt out over eight), one after
+// the other: they share lines where a chunk is narrower than one.
+__device__ __forceinline__ void place_work(uint32_t b, uint32_t per_sample, uint32_t samples, uint32_t& sample, uint32_t& rest) {
+  const uint32_t whole = samples / 8 * 8;
+  const bool in = b < whole * per_sample;
+  const uint32_t j = in ? b >> 3 : b - whole * per_sample, s = j / per_sample;
+  sample = in ? s * 8 + (b & 7) : whole + s;
+  rest = j - s * per_sample;
+}
+
 // Forward.  APPLY: one part holds the sample (parts == 1) and the result is written; else only the part's mean and squared
 // distances are left.  NP positions per lane, CV pieces across the channels of each.  Addresses are a uniform base and a 32-bit
 // offset that walks, so that they cost two registers and not two per piece (with 64 registers of values that decides whether
@@ -98,13 +126,10 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
   __shared__ float red[2][16 * 64];
   const Place q = place_of(a);
-  const uint32_t spb = blockDim.x / (uint32_t)a.D, per_sample = a.chunks * a.parts, whole = a.work / per_sample / 8 * 8;
+  const uint32_t spb = blockDim.x / (uint32_t)a.D, per_sample = a.chunks * a.parts;
   for (uint32_t b = blockIdx.x; b < a.work; b += gridDim.x) {
-    // neighbouring chunks of the same positions on one XCD (workgroups are dealt out over eight), one after the other:
-    // they share lines where a chunk is narrower than one
     uint32_t si, rest;
-    if (b < whole * per_sample) { const uint32_t j = b >> 3; si = j / per_sample * 8 + (b & 7); rest = j % per_sample; }
-    else { const uint32_t j = b - whole * per_sample; si = whole + j / per_sample; rest = j % per_sample; }
+    place_work(b, per_sample, a.work / per_sample, si, rest);
     const uint32_t chunk = rest % a.chunks, part = rest / a.chunks;
     const int64_t i0 = (int64_t)si * spb, i = i0 + q.sb;
     const int g = (int)chunk * a.gpc + q.g;
@@ -266,16 +291,17 @@ __device__ __forceinline__ void norm_dh(const Piece<T, V>& x, const Piece<T, V>&
 
 // Backward.  A workgroup keeps its chunk of channels for all its samples, so that the shares of dgamma and dbeta add up in
 // registers and leave once per workgroup.  APPLY as in the forward pass: else only the parts' two sums (and the shares).
-// Up to four pieces per lane their dh stays in fp32 registers between the sums and dx; eight are computed twice.
+// dh gamma stays in fp32 registers between the sums and dx.
 template <typename T, int V, int NP, int CV, bool APPLY>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
-  constexpr bool kKeep = APPLY && NP <= 4;
+  constexpr bool kKeep = APPLY && NP * V <= 32;
   __shared__ float red[2][16 * 64];
   extern __shared__ float share[];
   const Place q = place_of(a);
   const uint32_t spb = blockDim.x / (uint32_t)a.D;
-  const uint32_t chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks;
+  uint32_t chunk, row;
+  place_work(blockIdx.x, a.chunks, a.row_count, row, chunk);
   const int g = (int)chunk * a.gpc + q.g;
   float gam[CV * V], bet[CV * V], sg[CV * V], sb[CV * V];
 #pragma unroll
@@ -293,31 +319,51 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   const int64_t col0 = (int64_t)chunk * a.gpc * a.per;
   const uint32_t lane_col = (uint32_t)(q.g * a.per + q.slot * V), lane_pos = (uint32_t)(q.sb * (uint32_t)a.S + q.p);
   auto offset = [&](int64_t ld, int j) { return (lane_pos * (uint32_t)ld + lane_col + (uint32_t)(j * a.SP * V)) * (uint32_t)sizeof(T); };
-  for (uint32_t b = row; b < work; b += a.row_count) {
-    const uint32_t part = b % a.parts;
-    const int64_t i0 = (int64_t)(b / a.parts) * spb, i = i0 + q.sb;
-    const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
-    const bool live = i < a.n && g < a.G;
-    const int have = live ? count_pos : 0;
-    const int64_t at = i0 * a.S + pos0;
-    Vec vx[NP * CV], vd[NP * CV];
+  // What a workgroup's next share needs is asked for before this one's is worked on, where that is few registers: with single
+  // positions a share is over in the time of a load.
+  constexpr bool kAhead = NP * CV * Vec::kWords <= 4;
+  struct Fetched { Vec x[NP * CV], dy[NP * CV], res[kAhead ? NP * CV : 1]; float mean, rstd; int have; int64_t i, at; uint32_t part; };
+  auto fetch = [&](uint32_t b, Fetched& f) {
+    f.part = b % a.parts;
+    const int64_t i0 = (int64_t)(b / a.parts) * spb;
+    const int pos0 = (int)f.part * a.PP;
+    f.i = i0 + q.sb;
+    f.at = i0 * a.S + pos0;
+    const bool live = f.i < a.n && g < a.G;
+    f.have = live ? (int)min((int64_t)a.PP, a.S - pos0) : 0;
 #pragma unroll
     for (int j = 0; j < CV; ++j) {
-      uint32_t ox = offset(a.ldx, j), od = offset(a.lddy, j);
-      const char* const px = (const char*)(a.x + at * a.ldx + col0);
-      const char* const pd = (const char*)(a.dy + at * a.lddy + col0);
+      uint32_t ox = offset(a.ldx, j), od = offset(a.lddy, j), orr = offset(a.lddres, j);
+      const char* const px = (const char*)(a.x + f.at * a.ldx + col0);
+      const char* const pd = (const char*)(a.dy + f.at * a.lddy + col0);
+      const char* const pr = (const char*)(a.dres + f.at * a.lddres + col0);
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
-        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
-          vx[k * CV + j].load(px + ox);
-          vd[k * CV + j].load(pd + od);
+        if (q.p + k * a.PL < f.have && q.slot + j * a.SP < a.slots) {
+          f.x[k * CV + j].load(px + ox);
+          f.dy[k * CV + j].load(pd + od);
+          if (APPLY && kAhead && a.dres) f.res[kAhead ? k * CV + j : 0].load(pr + orr);
         }
         ox += (uint32_t)a.PL * (uint32_t)a.ldx * (uint32_t)sizeof(T);
         od += (uint32_t)a.PL * (uint32_t)a.lddy * (uint32_t)sizeof(T);
+        if (kAhead) orr += (uint32_t)a.PL * (uint32_t)a.lddres * (uint32_t)sizeof(T);
         asm volatile("" : "+v"(ox), "+v"(od));
       }
     }
-    const float mean = live ? a.mean[i * a.G + g] : 0.f, rstd = live ? a.rstd[i * a.G + g] : 0.f;
+    f.mean = live ? a.mean[f.i * a.G + g] : 0.f;
+    f.rstd = live ? a.rstd[f.i * a.G + g] : 0.f;
+  };
+  Fetched next;
+  if (kAhead && row < work) fetch(row, next);
+  for (uint32_t b = row; b < work; b += a.row_count) {
+    Fetched now;
+    if (kAhead) { now = next; if (b + a.row_count < work) fetch(b + a.row_count, next); }
+    else fetch(b, now);
+    Vec* const vx = now.x;
+    Vec* const vd = now.dy;
+    const float mean = now.mean, rstd = now.rstd;
+    const int have = now.have;
+    const int64_t at = now.at;
     float s1 = 0.f, s2 = 0.f;
     float kept[kKeep ? NP * CV * V : 1];
 #pragma unroll
@@ -342,8 +388,8 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     s1 = group_sum(s1, a.SP, a.TX, a.D, red[0]);
     s2 = group_sum(s2, a.SP, a.TX, a.D, red[1]);
     if (!APPLY) {
-      if (live && q.p == 0 && q.slot == 0) {
-        float* o = a.part + ((i * a.G + g) * a.parts + part) * 2;
+      if (have > 0 && q.p == 0 && q.slot == 0) {
+        float* o = a.part + ((now.i * a.G + g) * a.parts + now.part) * 2;
         o[0] = s1; o[1] = s2;
       }
     } else {
@@ -370,7 +416,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
               for (int e = 0; e < V; ++e) w[e] *= gam[j * V + e];
             }
             Vec o, r;
-            if (a.dres) r.load(res + orr);
+            if (a.dres) { if constexpr (kAhead) r = now.res[k * CV + j]; else r.load(res + orr); }
 #pragma unroll
             for (int e = 0; e < V; ++e) {
               w[e] = fmaf(rstd, w[e], fmaf(c2, xh[e], c1));
@@ -585,6 +631,10 @@ struct NormPlan {
   size_t off_rows, bytes;                  // workspace: parts' statistics, then the shares of dgamma / dbeta
 };
 
+// The widest piece: 16 bytes; backward four elements, since a lane keeps four sums and parameters per channel of its piece (eight bf16
+// elements take 112 registers and more where four take 74).
+int norm_widest(int dtype, bool backward) { return dtype == ABS_X_BF16 && !backward ? 8 : 4; }
+
 int pow2_up(int64_t x) { int p = 1; while (p < x) p <<= 1; return p; }
 
 // V: elements of a piece that all pointers, pitches and the group width allow (the same for every operand).
@@ -609,10 +659,16 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
     q.gpc = 1;
     while (q.gpc < g_most && ((int64_t)q.gpc * per * size < 128 || q.gpc * q.SP * S < 256)) q.gpc *= 2;
     // ... fewer, down to 32 bytes, where only that lets a workgroup hold a sample
-    auto fits = [&](int gpc) { return (int64_t)gpc * q.SP * pow2_up((S + np_most - 1) / np_most) <= kMaxLanes; };
-    int gpc = q.gpc;
-    while (gpc > 1 && !fits(gpc) && (int64_t)(gpc / 2) * per * size >= 32) gpc /= 2;
-    if (fits(gpc)) q.gpc = gpc; else q.split = true;
+    // (backward: half of its lanes where that does it: two workgroups share a CU, and one loads while the other works)
+    auto lanes = [&](int gpc) { return (int64_t)gpc * q.SP * pow2_up((S + np_most - 1) / np_most); };
+    auto narrow = [&](int most) {
+      int gpc = q.gpc;
+      while (gpc > 1 && lanes(gpc) > most && (int64_t)(gpc / 2) * per * size >= 32) gpc /= 2;
+      if (lanes(gpc) > most) return false;
+      q.gpc = gpc;
+      return true;
+    };
+    q.split = !(backward && narrow(kMaxLanes / 2)) && !narrow(kMaxLanes);
     q.TX = q.gpc * q.SP;
     q.chunks = (p.groups + q.gpc - 1) / q.gpc;
     // few workgroups with much to do each: parts as well
@@ -643,7 +699,7 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
     q.threads = q.split ? q.D : std::max(q.D, 256);
     // (backward: the more samples share a workgroup, the fewer shares of dgamma and dbeta)
     if (backward && !q.split)
-      while (q.threads < 1024 && p.n * q.D / (2 * q.threads) * q.chunks >= 512) q.threads *= 2;
+      while (q.threads < 512 && p.n * q.D / (2 * q.threads) * q.chunks >= 512) q.threads *= 2;
     const int64_t spb = q.threads / q.D, reach = spb * S;
     const int64_t ld = std::max({p.ldx, backward ? p.lddy : p.ldy, backward ? p.lddx : 0, backward ? p.lddres : 0});
     const int64_t work = (p.n + spb - 1) / spb * q.parts * q.chunks;
@@ -656,8 +712,8 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
     q.row_count = (uint32_t)std::min<int64_t>(64, p.n * S);
   } else {
     if (backward) {
-      // enough workgroups for two to eight on every CU, few enough that the shares they leave stay small
-      const uint32_t fill = std::max(1u, 256u * (2048u / (uint32_t)q.threads) / q.chunks);
+      // as many workgroups as the CUs hold at once, 1536 lanes each by their registers
+      const uint32_t fill = std::max(1u, 256u * std::max(1u, 1536u / (uint32_t)q.threads) / q.chunks);
       q.row_count = std::max(1u, std::min(q.work / q.chunks, fill));
       q.blocks = q.row_count * q.chunks;
     } else {
@@ -674,7 +730,7 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
 // the widest piece for a struct's sizes and pitches (pointers are looked at by the calls)
 int norm_piece(const abs_group_norm& p, bool backward, bool res, uintptr_t pointers) {
   const int size = op_size(p.dtype), per = p.channels / p.groups;
-  for (int V = 16 / size; V > 1; V /= 2) {
+  for (int V = norm_widest(p.dtype, backward); V > 1; V /= 2) {
     if (per % V || p.ldx % V || (pointers & (uintptr_t)(V * size - 1))) continue;
     if (!backward && p.ldy % V == 0) return V;
     if (backward && p.lddy % V == 0 && p.lddx % V == 0 && (!res || p.lddres % V == 0)) return V;
@@ -702,7 +758,7 @@ const char* norm_problem(const abs_group_norm* p, bool backward) {
 // the largest workspace over the pieces the pointers may force
 size_t norm_workspace(const abs_group_norm& p, bool backward) {
   size_t most = 0;
-  for (int V = 16 / op_size(p.dtype); V >= 1; V /= 2)
+  for (int V = norm_widest(p.dtype, backward); V >= 1; V /= 2)
     if ((p.channels / p.groups) % V == 0) most = std::max(most, norm_plan(p, backward, V).bytes);
   return most;
 }
@@ -781,7 +837,7 @@ hipError_t norm_run(const abs_group_norm& p, bool backward, NormArgs<T> a, const
   } else {
     switch (q.V) {
       case 8:
-        if constexpr (sizeof(T) == 2) e = backward ? norm_backward_v<T, 8>(a, q, s) : norm_forward_v<T, 8>(a, q, s);
+        if constexpr (sizeof(T) == 2) e = norm_forward_v<T, 8>(a, q, s);
         break;
       case 4: e = backward ? norm_backward_v<T, 4>(a, q, s) : norm_forward_v<T, 4>(a, q, s); break;
       case 2: e = backward ? norm_backward_v<T, 2>(a, q, s) : norm_forward_v<T, 2>(a, q, s); break;
