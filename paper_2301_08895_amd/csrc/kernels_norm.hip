@@ -53,28 +53,36 @@ __device__ __forceinline__ float norm_h(float xhat, float gamma, float beta) {
   return s + beta;
 }
 
-// v + v of the lane whose number differs in one bit (`off`, a power of two below 64); kFlat: the lanes that differ in lower bits hold equal
-// values already, so a mirror image does.  Cross-lane adds where there are such, LDS's swizzle (no addresses) for the others.
-template <bool kFlat>
-__device__ __forceinline__ float add_xor(float v, int off) {
-#define ABS_DPP(ctrl_) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl_, 0xF, 0xF, true))
-#define ABS_SWZ(x_) __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), ((x_) << 10) | 0x1F))
-  switch (off) {
-    case 1: return v + ABS_DPP(0xB1);                     // quad_perm [1, 0, 3, 2]
-    case 2: return v + ABS_DPP(0x4E);                     // quad_perm [2, 3, 0, 1]
-    case 4: return v + (kFlat ? ABS_DPP(0x141) : ABS_SWZ(4));   // row_half_mirror
-    case 8: return v + (kFlat ? ABS_DPP(0x140) : ABS_SWZ(8));   // row_mirror
-    case 16: return v + ABS_SWZ(16);
-    default: return v + __shfl_xor(v, 32);
-  }
+// v + v of the lane whose number differs in bit OFF; kFlat: the lanes that differ in lower bits hold equal values already, so a
+// mirror image does.  Cross-lane adds where there are such, LDS's swizzle (no addresses) for the others.
+template <int OFF, bool kFlat>
+__device__ __forceinline__ float add_xor(float v) {
+#define ABS_DPP(ctrl_) v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl_, 0xF, 0xF, true))
+  if constexpr (OFF == 1) return ABS_DPP(0xB1);                        // quad_perm [1, 0, 3, 2]
+  else if constexpr (OFF == 2) return ABS_DPP(0x4E);                   // quad_perm [2, 3, 0, 1]
+  else if constexpr (OFF == 4 && kFlat) return ABS_DPP(0x141);         // row_half_mirror
+  else if constexpr (OFF == 8 && kFlat) return ABS_DPP(0x140);         // row_mirror
+  else if constexpr (OFF < 32) return v + __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), (OFF << 10) | 0x1F));
+  else return v + __shfl_xor(v, 32);
 #undef ABS_DPP
-#undef ABS_SWZ
+}
+// ... over all bits that are set in `bits` (uniform)
+template <bool kFlat>
+__device__ __forceinline__ float add_lanes(float v, int bits) {
+  asm volatile("" : "+s"(bits));          // (tested here: kept outside the loops, the tests' results would fill the scalar registers)
+  if (bits & 1) v = add_xor<1, kFlat>(v);
+  if (bits & 2) v = add_xor<2, kFlat>(v);
+  if (bits & 4) v = add_xor<4, kFlat>(v);
+  if (bits & 8) v = add_xor<8, kFlat>(v);
+  if (bits & 16) v = add_xor<16, kFlat>(v);
+  if (bits & 32) v = add_xor<32, kFlat>(v);
+  return v;
 }
 
 // Sum of v over the lanes of one sample's group; every lane gets it.  `red`: 16 x 64 floats of LDS, not in use.
 __device__ __forceinline__ float group_sum(float v, int SP, int TX, int D, float* red) {
-  for (int off = 1; off < SP && off < 64; off <<= 1) v = add_xor<true>(v, off);
-  for (int off = TX; off < D && off < 64; off <<= 1) v = add_xor<false>(v, off);
+  v = add_lanes<true>(v, SP - 1);                                      // pieces of the group
+  v = add_lanes<false>(v, (D - 1) & ~(TX - 1));                        // positions
   if (SP > 64 || (D > 64 && D > TX)) {                                // (else a group is inside a wavefront)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int cols = SP < 64 ? min(TX, 64) / SP : 1;                  // groups of a wavefront
@@ -318,52 +326,65 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   const float inv = 1.0f / ((float)a.S * (float)a.per);
   const int64_t col0 = (int64_t)chunk * a.gpc * a.per;
   const uint32_t lane_col = (uint32_t)(q.g * a.per + q.slot * V), lane_pos = (uint32_t)(q.sb * (uint32_t)a.S + q.p);
-  auto offset = [&](int64_t ld, int j) { return (lane_pos * (uint32_t)ld + lane_col + (uint32_t)(j * a.SP * V)) * (uint32_t)sizeof(T); };
+  // a lane's first piece in each array, as 32-bit offsets from the workgroup's place there
+  auto offset = [&](int64_t ld) { return (lane_pos * (uint32_t)ld + lane_col) * (uint32_t)sizeof(T); };
+  const uint32_t ox0 = offset(a.ldx), od0 = offset(a.lddy), or0 = offset(a.lddres), oy0 = offset(a.ldy);
+  const uint32_t wide = (uint32_t)(a.SP * V) * (uint32_t)sizeof(T);                            // to the next of CV pieces
+  auto walk = [&](uint32_t& off, int64_t ld) {
+    off += (uint32_t)a.PL * (uint32_t)ld * (uint32_t)sizeof(T);
+    asm volatile("" : "+v"(off));
+  };
   // What a workgroup's next share needs is asked for before this one's is worked on, where that is few registers: with single
   // positions a share is over in the time of a load.
   constexpr bool kAhead = NP * CV * Vec::kWords <= 4;
-  struct Fetched { Vec x[NP * CV], dy[NP * CV], res[kAhead ? NP * CV : 1]; float mean, rstd; int have; int64_t i, at; uint32_t part; };
-  auto fetch = [&](uint32_t b, Fetched& f) {
-    f.part = b % a.parts;
-    const int64_t i0 = (int64_t)(b / a.parts) * spb;
-    const int pos0 = (int)f.part * a.PP;
-    f.i = i0 + q.sb;
-    f.at = i0 * a.S + pos0;
-    const bool live = f.i < a.n && g < a.G;
-    f.have = live ? (int)min((int64_t)a.PP, a.S - pos0) : 0;
+  struct Fetched { Vec x[NP * CV], dy[NP * CV], res[kAhead ? NP * CV : 1]; float mean, rstd; int have; int64_t stat; uint32_t part; };
+  // Uniform places of the share to be fetched: samples a.row_count shares on, or parts of them.
+  const int64_t base = col0 * (int64_t)sizeof(T);
+  struct Spot { const char *x, *dy, *res; char* y; int64_t i0; };
+  auto spot_of = [&](uint32_t b) {
+    const uint32_t s = a.parts == 1 ? b : b / a.parts;
+    const int64_t i0 = (int64_t)s * spb, at = i0 * a.S + (int64_t)(b - s * a.parts) * a.PP;
+    return Spot{(const char*)a.x + at * a.ldx * (int64_t)sizeof(T) + base, (const char*)a.dy + at * a.lddy * (int64_t)sizeof(T) + base,
+                (const char*)a.dres + at * a.lddres * (int64_t)sizeof(T) + base, (char*)a.y + at * a.ldy * (int64_t)sizeof(T) + base, i0};
+  };
+  const int64_t hop = (int64_t)a.row_count * spb;                       // parts == 1: samples between a workgroup's shares
+  const int64_t hop_bytes = hop * a.S * (int64_t)sizeof(T);
+  auto fetch = [&](uint32_t b, const Spot& p, Fetched& f) {
+    f.part = a.parts == 1 ? 0u : b % a.parts;
+    const int64_t i = p.i0 + q.sb;
+    const bool live = i < a.n && g < a.G;
+    f.have = live ? (int)min((int64_t)a.PP, a.S - (int64_t)f.part * a.PP) : 0;
+    uint32_t ox = ox0, od = od0, orr = or0;
 #pragma unroll
-    for (int j = 0; j < CV; ++j) {
-      uint32_t ox = offset(a.ldx, j), od = offset(a.lddy, j), orr = offset(a.lddres, j);
-      const char* const px = (const char*)(a.x + f.at * a.ldx + col0);
-      const char* const pd = (const char*)(a.dy + f.at * a.lddy + col0);
-      const char* const pr = (const char*)(a.dres + f.at * a.lddres + col0);
+    for (int k = 0; k < NP; ++k) {
 #pragma unroll
-      for (int k = 0; k < NP; ++k) {
+      for (int j = 0; j < CV; ++j)
         if (q.p + k * a.PL < f.have && q.slot + j * a.SP < a.slots) {
-          f.x[k * CV + j].load(px + ox);
-          f.dy[k * CV + j].load(pd + od);
-          if (APPLY && kAhead && a.dres) f.res[kAhead ? k * CV + j : 0].load(pr + orr);
+          f.x[k * CV + j].load(p.x + (ox + j * wide));
+          f.dy[k * CV + j].load(p.dy + (od + j * wide));
+          if (APPLY && kAhead && a.dres) f.res[kAhead ? k * CV + j : 0].load(p.res + (orr + j * wide));
         }
-        ox += (uint32_t)a.PL * (uint32_t)a.ldx * (uint32_t)sizeof(T);
-        od += (uint32_t)a.PL * (uint32_t)a.lddy * (uint32_t)sizeof(T);
-        if (kAhead) orr += (uint32_t)a.PL * (uint32_t)a.lddres * (uint32_t)sizeof(T);
-        asm volatile("" : "+v"(ox), "+v"(od));
-      }
+      if (NP > 1) { walk(ox, a.ldx); walk(od, a.lddy); if (kAhead) walk(orr, a.lddres); }
     }
-    f.mean = live ? a.mean[f.i * a.G + g] : 0.f;
-    f.rstd = live ? a.rstd[f.i * a.G + g] : 0.f;
+    f.stat = i * a.G + g;
+    f.mean = live ? a.mean[f.stat] : 0.f;
+    f.rstd = live ? a.rstd[f.stat] : 0.f;
   };
   Fetched next;
-  if (kAhead && row < work) fetch(row, next);
+  Spot here = spot_of(row), there = here;
+  if (kAhead && row < work) fetch(row, here, next);
   for (uint32_t b = row; b < work; b += a.row_count) {
     Fetched now;
-    if (kAhead) { now = next; if (b + a.row_count < work) fetch(b + a.row_count, next); }
-    else fetch(b, now);
+    if (a.parts > 1) { if (b != row) here = spot_of(b); }
+    else if (b != row) here = there;
+    if (kAhead && a.parts > 1) there = spot_of(b + a.row_count);
+    else there = Spot{here.x + hop_bytes * a.ldx, here.dy + hop_bytes * a.lddy, here.res + hop_bytes * a.lddres, here.y + hop_bytes * a.ldy, here.i0 + hop};
+    if (kAhead) { now = next; if (b + a.row_count < work) fetch(b + a.row_count, there, next); }
+    else fetch(b, here, now);
     Vec* const vx = now.x;
     Vec* const vd = now.dy;
     const float mean = now.mean, rstd = now.rstd;
     const int have = now.have;
-    const int64_t at = now.at;
     float s1 = 0.f, s2 = 0.f;
     float kept[kKeep ? NP * CV * V : 1];
 #pragma unroll
@@ -389,19 +410,17 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     s2 = group_sum(s2, a.SP, a.TX, a.D, red[1]);
     if (!APPLY) {
       if (have > 0 && q.p == 0 && q.slot == 0) {
-        float* o = a.part + ((now.i * a.G + g) * a.parts + now.part) * 2;
+        float* o = a.part + (now.stat * a.parts + now.part) * 2;
         o[0] = s1; o[1] = s2;
       }
     } else {
       // dx = rstd w - (rstd m2) xhat - rstd m1
       const float c1 = -rstd * (s1 * inv), c2 = -rstd * (s2 * inv);
+      uint32_t oy = oy0, orr = or0;
 #pragma unroll
-      for (int j = 0; j < CV; ++j) {
-        char* const dst = (char*)(a.y + at * a.ldy + col0);
-        const char* const res = (const char*)(a.dres + at * a.lddres + col0);
-        uint32_t oy = offset(a.ldy, j), orr = offset(a.lddres, j);
+      for (int k = 0; k < NP; ++k) {
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
+        for (int j = 0; j < CV; ++j)
           if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
             float xh[V], w[V];
             if constexpr (kKeep) {
@@ -416,19 +435,16 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
               for (int e = 0; e < V; ++e) w[e] *= gam[j * V + e];
             }
             Vec o, r;
-            if (a.dres) { if constexpr (kAhead) r = now.res[k * CV + j]; else r.load(res + orr); }
+            if (a.dres) { if constexpr (kAhead) r = now.res[k * CV + j]; else r.load(here.res + (orr + j * wide)); }
 #pragma unroll
             for (int e = 0; e < V; ++e) {
               w[e] = fmaf(rstd, w[e], fmaf(c2, xh[e], c1));
               if (a.dres) w[e] += r.at(e);
             }
             o.set(w);
-            o.store(dst + oy);
+            o.store(here.y + (oy + j * wide));
           }
-          oy += (uint32_t)a.PL * (uint32_t)a.ldy * (uint32_t)sizeof(T);
-          orr += (uint32_t)a.PL * (uint32_t)a.lddres * (uint32_t)sizeof(T);
-          asm volatile("" : "+v"(oy), "+v"(orr));
-        }
+        if (NP > 1) { walk(oy, a.ldy); walk(orr, a.lddres); }
       }
     }
   }
@@ -438,7 +454,8 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   if (CV == 1) {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      for (int off = a.TX; off < 64; off <<= 1) { sg[e] += __shfl_xor(sg[e], off); sb[e] += __shfl_xor(sb[e], off); }
+      sg[e] = add_lanes<false>(sg[e], 63 & ~(a.TX - 1));
+      sb[e] = add_lanes<false>(sb[e], 63 & ~(a.TX - 1));
     }
     if (stack > 1) {                                // [stack][V][TX], dgamma's shares and then dbeta's
       const int r = t / (a.TX > 64 ? a.TX : 64), tx = t & (a.TX - 1);
@@ -712,9 +729,10 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
     q.row_count = (uint32_t)std::min<int64_t>(64, p.n * S);
   } else {
     if (backward) {
-      // as many workgroups as the CUs hold at once, 1536 lanes each by their registers
-      const uint32_t fill = std::max(1u, 256u * std::max(1u, 1536u / (uint32_t)q.threads) / q.chunks);
-      q.row_count = std::max(1u, std::min(q.work / q.chunks, fill));
+      // as many workgroups as the CUs hold at once (1024 lanes each by their registers); a workgroup per share where a share has
+      // so many positions that its two numbers per channel do not count
+      const uint32_t fill = std::max(1u, 256u * (1024u / (uint32_t)q.threads) / q.chunks), all = q.work / q.chunks;
+      q.row_count = std::min((int64_t)q.threads / q.D * q.PL * q.NP >= 64 && all <= 4096 ? all : std::min(all, fill), all);
       q.blocks = q.row_count * q.chunks;
     } else {
       q.blocks = std::min(q.work, 1u << 20);

@@ -117,6 +117,7 @@ __device__ __forceinline__ float op_act_slope(float z) {
 // N values at once, the activation a uniform run-time value: one branch
 template <int N>
 __device__ __forceinline__ void op_act_all(float* h, int act) {
+  asm volatile("" : "+s"(act));           // (compared here: not once, with the result kept in scalar registers)
   if (act == ABS_ACT_RELU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_RELU>(h[i]);
@@ -131,6 +132,7 @@ __device__ __forceinline__ void op_act_all(float* h, int act) {
 // d[i] *= act'(h[i])
 template <int N>
 __device__ __forceinline__ void op_slope_all(float* d, const float* h, int act) {
+  asm volatile("" : "+s"(act));
   if (act == ABS_ACT_RELU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) d[i] *= op_act_slope<ABS_ACT_RELU>(h[i]);
