@@ -262,6 +262,182 @@ __global__ __launch_bounds__(256, RING <= 2 ? 2 : 1) void linear_tile_kernel(Gem
   }
 }
 
+// ---------------------------------------------------------------------- the large-tile kernel (bf16)
+// 256 x 256 of the result, 8 wavefronts (2 x 4) of 128 x 64 as 8 x 4 blocks of MFMA 16x16x32, a k-step of 64.  What bounds a bf16
+// product on tiles is the bytes staged per flop: a 256 x 256 tile stages half of what a 128 x 128 one does.  A k-step is
+// four turns of 16 MFMAs per wavefront (half of A times half of B); the two wavefronts of a SIMD are half a turn apart, so that
+// while one multiplies the other reads fragments and requests.  A half is requested again, for the step after the next, as soon as
+// both hold it in registers: a request is seven turns in flight, counted and never drained inside the loop.
+// A half of A is 64 of each wavefront row's 128 rows, a half of B 32 of each wavefront column's 64 columns: 16 KB, two requests per
+// wavefront.  [row][k] operands: 128 rows of 128 bytes, pieces XORed by (row >> 1) & 7; [k][row] operands: 64 rows of 128
+// elements, 64-byte blocks XORed by k & 3 and their 32-byte halves by (k >> 3) & 1 (the four quarters of a wavefront read rows 8 apart).
+constexpr int kBig = 256;
+constexpr int kHalf = 128 * 64;                           // elements of a half of an operand's step
+
+template <bool TR, bool IS_A>
+struct BigOperand {
+  const uint16_t* src[2][2];                              // a lane's piece [half][request] of k-step 0
+  int k[2];                                               // its contraction index there, by request
+  int64_t step;
+  __device__ __forceinline__ void init(const uint16_t* base, int64_t ld, int64_t r0, int64_t rows, int64_t contiguous, int64_t k0, int wave, int lane) {
+    step = TR ? 64 * ld : 64;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (TR) {
+        const int row = wave * 8 + q * 4 + (lane >> 4), pc = lane & 15;
+        const int col = (((pc >> 2) ^ (row & 3)) << 5) | (((pc & 3) ^ (((row >> 3) & 1) << 1)) << 3);
+        k[q] = row;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int64_t c = r0 + (IS_A ? (col >> 6) * 128 + h * 64 + (col & 63) : (col >> 5) * 64 + h * 32 + (col & 31));
+          src[h][q] = base + (k0 + row) * ld + min(c, contiguous - 8);
+        }
+      } else {
+        const int row = wave * 16 + q * 8 + (lane >> 3);
+        k[q] = ((lane & 7) ^ ((row >> 1) & 7)) * 8;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int64_t r = r0 + (IS_A ? (row >> 6) * 128 + h * 64 + (row & 63) : (row >> 5) * 64 + h * 32 + (row & 31));
+          src[h][q] = base + min(r, rows - 1) * ld + k0 + k[q];
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void request(int64_t j, int64_t left, int h, uint32_t lds) const {
+    if (left >= 64) {
+      lds_request16(src[h][0] + j * step, lds);
+      lds_request16(src[h][1] + j * step, lds + 1024);
+    } else {
+      lds_request16(k[0] < left ? (const void*)(src[h][0] + j * step) : (const void*)&g_zero_piece, lds);
+      lds_request16(k[1] < left ? (const void*)(src[h][1] + j * step) : (const void*)&g_zero_piece, lds + 1024);
+    }
+  }
+};
+
+// Where a lane's fragments of a half start, in elements: block i, 32-wide part s of the step.
+template <bool TR, bool IS_A>
+__device__ __forceinline__ bf16x8_t big_fragment(const uint16_t* half, int w, int i, int s, int lane) {
+  const int lr = lane & 15, lk = lane >> 4;
+  if (TR) {
+    const int tr = lr >> 2, blk = IS_A ? w * 2 + (i >> 1) : w;
+    const uint16_t* q = half + (s * 32 + 8 * lk + tr) * 128 + ((blk ^ tr) << 5) + (((i & 1) ^ (lk & 1)) << 4) + 4 * (lr & 3);
+    union { s16x4_t h[2]; bf16x8_t v; } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(q));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(q + 4 * 128));
+    return u.v;
+  }
+  const int row = w * (IS_A ? 64 : 32) + i * 16 + lr;
+  return *(const bf16x8_t*)(half + row * 64 + ((((s << 2) | lk) ^ ((lr >> 1) & 7)) << 3));
+}
+
+template <bool ATR, bool BTR>
+__global__ __launch_bounds__(512, 1) void linear_big_kernel(GemmArgs<uint16_t> g) {
+  __shared__ __attribute__((aligned(1024))) uint16_t smem[8 * kHalf];          // [stage][A0 A1], then [stage][B0 B1]
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const int total = g.mt * g.nt * g.nsplit, per = (total + 7) / 8;
+  const int id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+  if (((int)blockIdx.x >> 3) >= per || id >= total) return;
+  const int split = id / (g.mt * g.nt), tile = id - split * (g.mt * g.nt);
+  const int64_t m0 = (int64_t)(tile / g.nt) * kBig, n0 = (int64_t)(tile % g.nt) * kBig;
+  const int64_t k0 = (int64_t)split * g.steps_per_split * 64;
+  const int64_t kend = min(g.K, k0 + (int64_t)g.steps_per_split * 64);
+  const int nks = (int)((kend - k0 + 63) / 64);
+
+  BigOperand<ATR, true> oa;
+  BigOperand<BTR, false> ob;
+  oa.init(g.A, g.lda, m0, g.M, g.mc, k0, wave, lane);
+  ob.init(g.B, g.ldb, n0, g.N, g.nc, k0, wave, lane);
+  const uint32_t dma_a = lds_at(smem) + (uint32_t)wave * 2048u, dma_b = dma_a + 4 * kHalf * 2;
+  auto request_a = [&](int j, int st, int h) { oa.request(j, g.K - k0 - (int64_t)j * 64, h, dma_a + (uint32_t)((st * 2 + h) * kHalf * 2)); };
+  auto request_b = [&](int j, int st, int h) { ob.request(j, g.K - k0 - (int64_t)j * 64, h, dma_b + (uint32_t)((st * 2 + h) * kHalf * 2)); };
+
+  f32x4_t acc[8][4];
+#pragma unroll
+  for (int a = 0; a < 8; ++a)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) acc[a][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  bf16x8_t fa[8], fbx[2][2], fby[2][2];
+#define ABS_LOAD_A(st_, h_)                                                                                          \
+  _Pragma("unroll") for (int q_ = 0; q_ < 8; ++q_)                                                                   \
+    fa[q_] = big_fragment<ATR, true>(smem + ((st_) * 2 + (h_)) * kHalf, wm, q_ >> 1, q_ & 1, lane);
+#define ABS_LOAD_B(dst_, st_, h_)                                                                                    \
+  _Pragma("unroll") for (int s_ = 0; s_ < 2; ++s_) _Pragma("unroll") for (int j_ = 0; j_ < 2; ++j_)                  \
+    dst_[j_][s_] = big_fragment<BTR, false>(smem + (4 + (st_) * 2 + (h_)) * kHalf, wn, j_, s_, lane);
+#define ABS_MMA(ha_, hb_, b_)                                                                                        \
+  __builtin_amdgcn_sched_barrier(0);                                                                                 \
+  _Pragma("unroll") for (int s_ = 0; s_ < 2; ++s_) _Pragma("unroll") for (int i_ = 0; i_ < 4; ++i_)                  \
+    _Pragma("unroll") for (int j_ = 0; j_ < 2; ++j_)                                                                 \
+      acc[(ha_) * 4 + i_][(hb_) * 2 + j_] =                                                                          \
+          __builtin_amdgcn_mfma_f32_16x16x32_bf16(b_[j_][s_], fa[2 * i_ + s_], acc[(ha_) * 4 + i_][(hb_) * 2 + j_], 0, 0, 0); \
+  __builtin_amdgcn_sched_barrier(0);                                                                                 \
+  asm volatile("s_barrier" ::: "memory");
+#define ABS_TURN(i_)                                                                                                 \
+  if (left >= 2)      ring_wait<12>();                                                                               \
+  else if (left == 1) ring_wait<10 - 2 * (i_)>();                                                                    \
+  else                ring_wait<(i_) == 0 ? 2 : 0>();
+#define ABS_STEP(X_, Y_, st_)                                                                                        \
+  {                                                                                                                  \
+    const int left = nks - 1 - j;                                                                                    \
+    ABS_LOAD_A(st_, 0);                                                                                              \
+    if (left >= 2) request_b(j + 2, st_, 0);                                                                         \
+    ABS_TURN(0); ABS_MMA(0, 0, X_);                                                                                  \
+    ABS_LOAD_B(Y_, st_, 1);                                                                                          \
+    if (left >= 2) request_a(j + 2, st_, 0);                                                                         \
+    ABS_TURN(1); ABS_MMA(0, 1, Y_);                                                                                  \
+    ABS_LOAD_A(st_, 1);                                                                                              \
+    if (left >= 2) request_b(j + 2, st_, 1);                                                                         \
+    ABS_TURN(2); ABS_MMA(1, 1, Y_);                                                                                  \
+    if (left >= 1) ABS_LOAD_B(Y_, (st_) ^ 1, 0);                                                                     \
+    if (left >= 2) request_a(j + 2, st_, 1);                                                                         \
+    ABS_TURN(3); ABS_MMA(1, 0, X_);                                                                                  \
+  }
+  request_b(0, 0, 0); request_a(0, 0, 0); request_b(0, 0, 1); request_a(0, 0, 1);
+  if (nks > 1) {
+    request_b(1, 1, 0); request_a(1, 1, 0); request_b(1, 1, 1); request_a(1, 1, 1);
+    ring_wait<12>();
+  } else {
+    ring_wait<4>();
+  }
+  ABS_LOAD_B(fbx, 0, 0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (requested again in the first turn)
+  if (wm) asm volatile("s_barrier" ::: "memory");
+  for (int j = 0;;) {
+    ABS_STEP(fbx, fby, 0);
+    if (++j >= nks) break;
+    ABS_STEP(fby, fbx, 1);
+    if (++j >= nks) break;
+  }
+  if (!wm) asm volatile("s_barrier" ::: "memory");
+#undef ABS_STEP
+#undef ABS_TURN
+#undef ABS_MMA
+#undef ABS_LOAD_B
+#undef ABS_LOAD_A
+  // Register r of a lane: column 4 (lane / 16) + r, row lane % 16 of its block.  32 rows of a wavefront at a time through LDS.
+  __syncthreads();
+  float* const stage_out = (float*)smem + wave * (32 * kOutPitch);
+  Epilogue<uint16_t> e = g.e;
+  if (e.part) e.part += split * e.part_stride;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) *(f32x4_t*)&stage_out[(a * 16 + (lane & 15)) * kOutPitch + b * 16 + 4 * (lane >> 4)] = acc[2 * i + a][b];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int r = lane >> 3; r < 32; r += 8) {
+      const int64_t m = m0 + wm * 128 + i * 32 + r, n = n0 + wn * 64 + (lane & 7) * 8;
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) *(f32x4_t*)&v[4 * q] = *(const f32x4_t*)&stage_out[r * kOutPitch + (lane & 7) * 8 + 4 * q];
+      if (m < g.M) finish(e, m, n, g.N, v);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // ---------------------------------------------------------------------- shares of the contraction, added in their order
 template <typename T>
 __global__ __launch_bounds__(256) void linear_join_kernel(Epilogue<T> e, int64_t M, int64_t N, int shares) {
@@ -409,12 +585,28 @@ unsigned few_blocks(int64_t threads) { return (unsigned)std::max<int64_t>(1, std
 // ---------------------------------------------------------------------- the plan
 constexpr int kFewRows = 8;                  // up to here linear_rows_kernel
 
-struct Product {                              // one product on the tile kernel
+struct Product {                              // one product on a tile kernel
+  bool big;
   int mt, nt, nsplit, steps_per_split;
   size_t part_bytes;
 };
-Product plan_product(int64_t M, int64_t N, int64_t K, int step) {
+Product plan_product(int64_t M, int64_t N, int64_t K, int dtype) {
   Product q{};
+  const int step = dtype == ABS_X_BF16 ? 64 : 32;
+  if (dtype == ABS_X_BF16) {
+    q.mt = (int)((M + kBig - 1) / kBig);
+    q.nt = (int)((N + kBig - 1) / kBig);
+    const int64_t tiles = (int64_t)q.mt * q.nt, steps = (K + 63) / 64;
+    const int64_t split = tiles >= 192 ? 1 : std::max<int64_t>(1, std::min<int64_t>({8, 256 / tiles, steps / 8}));
+    // whole tiles for most CUs, and little of them beyond the result
+    if (tiles * split >= 192 && (double)M * (double)N >= 0.7 * (double)tiles * kBig * kBig) {
+      q.big = true;
+      q.steps_per_split = (int)((steps + split - 1) / split);
+      q.nsplit = (int)((steps + q.steps_per_split - 1) / q.steps_per_split);
+      if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
+      return q;
+    }
+  }
   q.mt = (int)((M + kTile - 1) / kTile);
   q.nt = (int)((N + kTile - 1) / kTile);
   const int64_t tiles = (int64_t)q.mt * q.nt, steps = (K + step - 1) / step;
@@ -438,7 +630,7 @@ struct LinearPlan {
 // aligned: the pointers are; need_copy of x / w and, for the backward pass, of dy into dz
 LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok, bool dy_ok) {
   LinearPlan q{};
-  const int size = op_size(p.dtype), piece = 16 / size, step = 128 / size;
+  const int size = op_size(p.dtype), piece = 16 / size;
   q.in8 = (int64_t)op_round_up(p.d_in, piece);
   q.out8 = (int64_t)op_round_up(p.d_out, piece);
   const bool x_whole = x_ok && p.d_in % piece == 0 && p.ldx % piece == 0;
@@ -460,7 +652,7 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
       q.pack_w = !w_whole;
       if (q.pack_x) q.off_x = take((size_t)p.rows * q.in8 * size);
       if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
-      q.fwd = plan_product(p.rows, p.d_out, p.d_in, step);
+      q.fwd = plan_product(p.rows, p.d_out, p.d_in, p.dtype);
       q.off_part = take(q.fwd.part_bytes);
     }
   } else {
@@ -473,8 +665,8 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     const int cols = (p.d_out + 31) / 32;
     q.sum_rows = (int)std::max<int64_t>(1, std::min<int64_t>((p.rows + 31) / 32, std::max(1, 4096 / cols)));
     q.off_sums = take((size_t)q.sum_rows * p.d_out * 4);
-    q.dx = plan_product(p.rows, p.d_in, p.d_out, step);
-    q.dw = plan_product(p.d_in, p.d_out, p.rows, step);
+    q.dx = plan_product(p.rows, p.d_in, p.d_out, p.dtype);
+    q.dw = plan_product(p.d_in, p.d_out, p.rows, p.dtype);
     q.off_part = take(std::max(q.dx.part_bytes, q.dw.part_bytes));
   }
   q.bytes = o;
@@ -513,8 +705,10 @@ hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, hipStream_t
   if (q.nsplit > 1) g.e = join;
   else g.e.part = nullptr;
   const dim3 grid((unsigned)((total + 7) / 8 * 8));
-  if (total > 256) linear_tile_kernel<T, ATR, BTR, 2><<<grid, 256, 0, s>>>(g);
-  else             linear_tile_kernel<T, ATR, BTR, 4><<<grid, 256, 0, s>>>(g);
+  if (q.big) {
+    if constexpr (sizeof(T) == 2) linear_big_kernel<ATR, BTR><<<grid, 512, 0, s>>>(g);
+  } else if (total > 256) linear_tile_kernel<T, ATR, BTR, 2><<<grid, 256, 0, s>>>(g);
+  else linear_tile_kernel<T, ATR, BTR, 4><<<grid, 256, 0, s>>>(g);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && q.nsplit > 1) {
     linear_join_kernel<T><<<few_blocks(g.M * ((g.N + kPiece<T> - 1) / kPiece<T>)), 256, 0, s>>>(join, g.M, g.N, q.nsplit);

@@ -81,6 +81,22 @@ def test_linear_pitches_and_starts(rows, pad, lead, dtype):
         ou.close(g, v, s)
 
 
+# results of many 256 x 256 tiles: ragged in every direction, contractions of one step and two, in shares for the gradients
+@pytest.mark.parametrize("rows,d_in,d_out,act", [(3400, 1000, 3904, SILU), (3333, 777, 3901, GELU), (50_000, 24, 256, RELU),
+                                                 (50_000, 70, 250, NONE), (50_000, 136, 512, SILU), (12_300, 2048, 1030, NONE)])
+def test_linear_of_many_tiles(rows, d_in, d_out, act):
+    x, w = rows_of(rows, d_in, BF), rows_of(d_in, d_out, BF, scale=d_in ** -0.5)
+    b, r = torch.randn(d_out, device="cuda"), rows_of(rows, d_out, BF)
+    y, z = lib.linear_forward(x, w, b, act=act, residual=r, keep_z=True)
+    want, wz, sy, sz = ou.linear(x, w, b, act, r)
+    ou.close(z, wz, sz, "z")
+    ou.close(y, want, sy, "y")
+    dy = rows_of(rows, d_out, BF)
+    got = lib.linear_backward(x, w, dy, act=act, z=z)
+    for g, v, s, name in zip(got, *ou.linear_gradient(x, w, z, dy, act), ("dx", "dw", "db")):
+        ou.close(g, v, s, name)
+
+
 def test_linear_of_no_rows():
     x, w = torch.empty(0, 24, device="cuda", dtype=BF), rows_of(24, 16, BF)
     assert lib.linear_forward(x, w).shape == (0, 16)
