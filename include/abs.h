@@ -338,8 +338,8 @@ int abs_calibrate_mfma(int32_t data_mode, int32_t iters, int32_t workgroups, flo
  * each with its gradient.  They need no handle: sizes travel in a small struct, matrices are row-major DEVICE
  * arrays owned by the caller with a row pitch in elements (ld*, at least the row's length), in the dtype the
  * struct names (ABS_X_FP32 or ABS_X_BF16; biases, gamma, beta, saved statistics and their gradients are always
- * fp32).  Any size, pitch and alignment that the elements allow is taken; rows whose length, pitch and start are
- * multiples of 16 bytes are read in place, others cost a copy (linear) or narrower loads.  What lies between a
+ * fp32).  Any size, pitch and alignment that the elements allow is taken (a large product of matrices whose rows'
+ * length, pitch or start are not multiples of 16 bytes copies them into the workspace first).  What lies between a
  * row's end and the next row is neither read nor written.  Sums, statistics and products are held in fp32 and
  * rounded once to the output's dtype; they have a fixed order (no float atomics): two calls give the same bits.
  *

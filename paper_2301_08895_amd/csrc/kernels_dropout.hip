@@ -29,13 +29,13 @@ __device__ __forceinline__ float dropped(float x, uint32_t part, uint32_t drop, 
   return part >= drop ? x * scale : 0.f;       // a select: what is dropped may be infinite
 }
 
-// Pieces of 16 bytes: rows of whole pieces, and a flat array whose last few elements the last thread takes one by one.
+// Pieces of 16 bytes, at any alignment of the elements: rows of whole pieces, and a flat array whose last few elements the last thread takes one by one.
 // A thread takes kPieces pieces a block's width apart, all loads before the first draw is needed.
 constexpr int kDropPieces = 2;
 template <typename T, bool RES, bool FLAT>
 __global__ __launch_bounds__(256) void dropout_vector_kernel(DropArgs<T> a) {
   constexpr int V = 16 / sizeof(T);
-  typedef OpVec<T, V> Vec;
+  typedef Piece<T, V> Vec;
   const int64_t per_row = a.cols / V, pieces = per_row * a.rows;
   const int64_t p0 = (int64_t)op_block() * (256 * kDropPieces) + threadIdx.x;
   Vec vx[kDropPieces], vr[kDropPieces];
@@ -51,8 +51,8 @@ __global__ __launch_bounds__(256) void dropout_vector_kernel(DropArgs<T> a) {
       }
       ox[i] = row * a.ldx + c * V;
       oy[i] = row * a.ldy + c * V;
-      vx[i] = *(const Vec*)(a.x + ox[i]);
-      if (RES) vr[i] = *(const Vec*)(a.r + row * a.ldr + c * V);
+      vx[i].load(a.x + ox[i]);
+      if (RES) vr[i].load(a.r + row * a.ldr + c * V);
     }
   }
 #pragma unroll
@@ -60,18 +60,19 @@ __global__ __launch_bounds__(256) void dropout_vector_kernel(DropArgs<T> a) {
     const int64_t p = p0 + i * 256;
     if (p < pieces) {
       Vec o;
+      float f[V];
 #pragma unroll
       for (int h = 0; h < V / 4; ++h) {
         const uint64_t w = dropout_draw(a.key, (uint64_t)p * (V / 4) + h);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int e = 4 * h + j;
-          float v = dropped(op_widen(vx[i].e[e]), (uint32_t)(w >> (16 * j)) & 0xFFFFu, a.drop, a.scale);
-          if (RES) v += op_widen(vr[i].e[e]);
-          op_narrow(v, o.e[e]);
+          f[e] = dropped(vx[i].at(e), (uint32_t)(w >> (16 * j)) & 0xFFFFu, a.drop, a.scale);
+          if (RES) f[e] += vr[i].at(e);
         }
       }
-      *(Vec*)(a.y + oy[i]) = o;
+      o.set(f);
+      o.store(a.y + oy[i]);
     }
   }
   if (FLAT && p0 == 0) {
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(256) void dropout_vector_kernel(DropArgs<T> a) {
   }
 }
 
-// Any pitch, width and alignment: a thread takes the four elements of a draw, one by one, also across a row's end.
+// Rows that are not whole pieces, a pitch apart: a thread takes the four elements of a draw, one by one, also across a row's end.
 template <typename T, bool RES>
 __global__ __launch_bounds__(256) void dropout_element_kernel(DropArgs<T> a) {
   const uint64_t total = (uint64_t)a.rows * (uint64_t)a.cols;
@@ -117,9 +118,7 @@ hipError_t launch_dropout(const abs_dropout& p, const void* x, const void* r, vo
   a.scale = (float)(65536.0 / (65536 - p.drop));
   const bool flat = p.rows == 1 || (p.ldx == p.cols && p.ldy == p.cols && a.ldr == p.cols);
   if (flat) { a.cols *= a.rows; a.rows = 1; }
-  const bool aligned = op_aligned(x, 16) && op_aligned(y, 16) && (!r || op_aligned(r, 16));
-  const bool whole = a.cols % V == 0 && a.ldx % V == 0 && a.ldy % V == 0 && a.ldr % V == 0;
-  if (aligned && (flat || whole)) {
+  if (flat || a.cols % V == 0) {                       // (at any pitch and alignment)
     const int64_t pieces = a.cols / V * a.rows;
     const dim3 grid = op_grid((uint64_t)std::max<int64_t>(1, (pieces + 256 * kDropPieces - 1) / (256 * kDropPieces)));
     if (flat) {

@@ -35,7 +35,7 @@ template <typename T>
 struct Epilogue {
   const float* bias; const T* r; T* y; T* z; float* part;
   int64_t ldr, ldy, ldz, ldpart, part_stride;
-  int act, vec;                      // vec: a 16-byte piece of columns is one access for every array
+  int act;
 };
 
 template <typename T>
@@ -58,31 +58,22 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t 
       for (int q = 0; q < V / 4; ++q)
         if (n + 4 * q < N) *(f32x4_t*)(e.part + m * e.ldpart + n + 4 * q) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
     }
-  } else if (e.vec) {
-    if (n >= N) return;                           // (N is whole pieces)
-    typedef OpVec<T, V> Vec;
-    Vec r, o;
-    if (e.r) r = *(const Vec*)(e.r + m * e.ldr + n);
+  } else if (n + V <= N) {
+    Piece<T, V> r, o;
+    if (e.r) r.load(e.r + m * e.ldr + n);
     if (e.bias) {
+      const Loose<float, V> b = *(const Loose<float, V>*)(e.bias + n);
 #pragma unroll
-      for (int q = 0; q < V / 4; ++q) {
-        const f32x4_t b = *(const f32x4_t*)(e.bias + n + 4 * q);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[4 * q + i] += b[i];
-      }
+      for (int i = 0; i < V; ++i) v[i] += b.e[i];
     }
-    if (e.z) {
+    if (e.z) { o.set(v); o.store(e.z + m * e.ldz + n); }
+    op_act_all<V>(v, e.act);
+    if (e.r) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) op_narrow(v[i], o.e[i]);
-      *(Vec*)(e.z + m * e.ldz + n) = o;
+      for (int i = 0; i < V; ++i) v[i] += r.at(i);
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float h = op_act(v[i], e.act);
-      if (e.r) h += op_widen(r.e[i]);
-      op_narrow(h, o.e[i]);
-    }
-    *(Vec*)(e.y + m * e.ldy + n) = o;
+    o.set(v);
+    o.store(e.y + m * e.ldy + n);
   } else {
 #pragma unroll 1
     for (int i = 0; i < V; ++i)
@@ -440,67 +431,376 @@ __global__ __launch_bounds__(512, 1) void linear_big_kernel(GemmArgs<uint16_t> g
 
 // ---------------------------------------------------------------------- shares of the contraction, added in their order
 template <typename T>
-__global__ __launch_bounds__(256) void linear_join_kernel(Epilogue<T> e, int64_t M, int64_t N, int shares) {
+struct Join { Epilogue<T> e; int64_t M, N; int shares; const float* db_part; float* db; };       // db: the shares of db as well
+template <typename T>
+__global__ __launch_bounds__(256) void linear_join_kernel(Join<T> first, Join<T> second) {
   constexpr int V = kPiece<T>;
+  const Join<T>& j = blockIdx.y ? second : first;
+  const int shares = j.shares;
+  if (j.db_part)
+    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < j.N; n += (int64_t)gridDim.x * 256) {
+      float s = 0.f;
+#pragma unroll 8
+      for (int k = 0; k < shares; ++k) s += j.db_part[k * j.N + n];
+      j.db[n] = s;
+    }
+  Epilogue<T> e = j.e;
   const float* const part = e.part;
   e.part = nullptr;
-  const int64_t pieces = (N + V - 1) / V, total = M * pieces;
+  const int64_t pieces = (j.N + V - 1) / V, total = j.M * pieces;
 #pragma unroll 1
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
     const int64_t m = q / pieces, n = (q - m * pieces) * V;
     float v[V];
 #pragma unroll
     for (int h = 0; h < V / 4; ++h) {
-      if (n + 4 * h >= N) { v[4 * h] = v[4 * h + 1] = v[4 * h + 2] = v[4 * h + 3] = 0.f; continue; }
+      if (n + 4 * h >= j.N) { v[4 * h] = v[4 * h + 1] = v[4 * h + 2] = v[4 * h + 3] = 0.f; continue; }
       const float* p = part + m * e.ldpart + n + 4 * h;
       f32x4_t s = *(const f32x4_t*)p;
+#pragma unroll 8
       for (int k = 1; k < shares; ++k) s += *(const f32x4_t*)(p + k * e.part_stride);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[4 * h + i] = s[i];
     }
-    finish(e, m, n, N, v);
+    finish(e, m, n, j.N, v);
   }
 }
 
-// ---------------------------------------------------------------------- few rows: the weights' bytes are what counts
-// A workgroup takes 8 pieces of columns (128 bytes of a weight row) and a run of the contraction, 32 weight rows at a time;
-// every weight is read once, for all R rows of x.  The runs' sums go to shares that linear_join_kernel adds.
-template <typename T, int V, int R>
-__global__ __launch_bounds__(256) void linear_rows_kernel(const T* x, int64_t ldx, const T* w, int64_t ldw, int rows, int K, int N, int run,
-                                                          float* part, int64_t ldpart, int64_t part_stride) {
-  typedef OpVec<T, V> Vec;
-  __shared__ float red[32][8 * V + 1];
-  const int t = threadIdx.x, c = t & 7, kl = t >> 3;
-  const int n = (int)blockIdx.x * 8 * V + c * V, k0 = (int)blockIdx.y * run, k1 = min(K, k0 + run);
-  float acc[R][V];
+// ---------------------------------------------------------------------- small products: operands straight from memory into registers
+// A product that a handful of tiles covers waits for launches and memory's latency, not for arithmetic.  So a whole forward or
+// backward pass is one launch without workspace: a workgroup has 32 x 64 of the result (dW: 64 x 64), its eight wavefronts
+// share the contraction (blocks of 16 bf16 or 8 fp32 go round them), every operand goes from memory into the matrix
+// instruction's registers with no LDS in between, and the eight partial results meet in LDS once.  Reads are per element, pair or
+// piece at any alignment; dz is computed where it is read, and db summed by the workgroups of dW's first row of tiles.
+// [k][column] operands: a lane reads two neighbouring columns of 8 (fp32: 4) rows, so its even columns make one fragment
+// and its odd ones another; [row][k] operands follow the same numbering, row 2 (lane % 32) + j in fragment j.
+constexpr int kSmallWaves = 8;
+template <typename T> constexpr int kBlockK = sizeof(T) == 2 ? 16 : 8;       // contraction of one wavefront's step
+
+template <typename T> struct FragOf;
+template <> struct FragOf<uint16_t> { typedef bf16x8_t type; };
+template <> struct FragOf<float> { typedef f32x4_t type; };
+template <typename T> using Frag = typename FragOf<T>::type;
+
+// [row][k]: elements k .. k + 7 (fp32: 3) of a row, zeros from K on
+template <typename T>
+struct RowPart {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const T* p, int k, int K) {
+    constexpr int N = kPiece<T>;
+    if (k + N <= K) {
+      const Loose<T, N> l = *(const Loose<T, N>*)(p + k);
+      __builtin_memcpy(w, &l, 16);
+    } else {
+      T v[N];
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int e = 0; e < V; ++e) acc[r][e] = 0.f;
-  if (n < N) {
-#pragma unroll 4
-    for (int k = k0 + kl; k < k1; k += 32) {
-      const Vec v = *(const Vec*)(w + (int64_t)k * ldw + n);
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const float xv = r < rows ? op_widen(x[r * ldx + k]) : 0.f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) acc[r][e] = fmaf(xv, op_widen(v.e[e]), acc[r][e]);
+      for (int e = 0; e < N; ++e) {
+        const T x = p[min(k + e, K - 1)];
+        v[e] = k + e < K ? x : T(0);
       }
+      __builtin_memcpy(w, v, 16);
     }
   }
+  __device__ __forceinline__ Frag<T> frag() const { Frag<T> f; __builtin_memcpy(&f, w, 16); return f; }
+  // this = dz, from dy (this) and z
+  __device__ __forceinline__ void slope(const RowPart& z, int act) {
+    Piece<T, kPiece<T>> d, h;
+    float f[kPiece<T>], g[kPiece<T>];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    __syncthreads();
+    for (int i = 0; i < 4; ++i) { d.w[i] = w[i]; h.w[i] = z.w[i]; }
 #pragma unroll
-    for (int e = 0; e < V; ++e) red[kl][c * V + e] = acc[r][e];
-    __syncthreads();
-    const int col = (int)blockIdx.x * 8 * V + t;
-    if (t < 8 * V && col < N && r < rows) {
-      float s = 0.f;
-      for (int k = 0; k < 32; ++k) s += red[k][t];
-      part[blockIdx.y * part_stride + r * ldpart + col] = s;
+    for (int e = 0; e < kPiece<T>; ++e) { f[e] = d.at(e); g[e] = h.at(e); }
+    op_slope_all<kPiece<T>>(f, g, act);
+    d.set(f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = d.w[i];
+  }
+};
+
+// [k][column]: two neighbouring columns of rows k .. k + 7 (fp32: 3), zeros from K on.  A lane's columns are c and c + 1; beyond the last
+// column it reads the last two (what it computes from them is not stored), at the last of an odd number the pair before (swap).
+struct ColumnPlace { int at; bool swap; };
+__device__ __forceinline__ ColumnPlace column_place(int c, int N) { return {min(c, N - 2), c == N - 1}; }
+template <typename T> struct ColumnPart;
+template <>
+struct ColumnPart<uint16_t> {
+  uint32_t w[8];                                            // a row's two columns
+  __device__ __forceinline__ void load(const uint16_t* p, int64_t ld, int k, int K, ColumnPlace c, int N) {
+    const uint16_t* q = p + (int64_t)min(k, K - 1) * ld + c.at;
+    if (k + 8 <= K) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const Loose<uint16_t, 2> l = *(const Loose<uint16_t, 2>*)q;
+        __builtin_memcpy(&w[r], &l, 4);
+        q += ld;
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        w[r] = 0u;
+        if (k + r < K) {
+          const Loose<uint16_t, 2> l = *(const Loose<uint16_t, 2>*)q;
+          __builtin_memcpy(&w[r], &l, 4);
+          q += ld;
+        }
+      }
     }
+    if (N & 1) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) w[r] = c.swap ? w[r] >> 16 : w[r];
+    }
+  }
+  __device__ __forceinline__ bf16x8_t frag(int odd) const {
+    uint32_t f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], odd ? 0x07060302u : 0x05040100u);
+    bf16x8_t v;
+    __builtin_memcpy(&v, f, 16);
+    return v;
+  }
+  __device__ __forceinline__ void slope(const ColumnPart& z, int act, float& s0, float& s1) {
+#pragma unroll
+    for (int r = 0; r < 8; r += 4) {
+      float f[8], h[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[r + i] << 16); f[2 * i + 1] = __uint_as_float(w[r + i] & 0xFFFF0000u);
+        h[2 * i] = __uint_as_float(z.w[r + i] << 16); h[2 * i + 1] = __uint_as_float(z.w[r + i] & 0xFFFF0000u);
+      }
+      op_slope_all<8>(f, h, act);
+      Piece<uint16_t, 8> o;
+      o.set(f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { s0 += f[2 * i]; s1 += f[2 * i + 1]; w[r + i] = o.w[i]; }
+    }
+  }
+  __device__ __forceinline__ void sum(float& s0, float& s1) const {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) { s0 += __uint_as_float(w[r] << 16); s1 += __uint_as_float(w[r] & 0xFFFF0000u); }
+  }
+};
+template <>
+struct ColumnPart<float> {
+  float w[2][4];                                            // [column][row]
+  __device__ __forceinline__ void load(const float* p, int64_t ld, int k, int K, ColumnPlace c, int N) {
+    const float* q = p + (int64_t)min(k, K - 1) * ld + c.at;
+    if (k + 4 <= K) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const Loose<float, 2> l = *(const Loose<float, 2>*)q;
+        w[0][r] = l.e[0]; w[1][r] = l.e[1];
+        q += ld;
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        w[0][r] = w[1][r] = 0.f;
+        if (k + r < K) {
+          const Loose<float, 2> l = *(const Loose<float, 2>*)q;
+          w[0][r] = l.e[0]; w[1][r] = l.e[1];
+          q += ld;
+        }
+      }
+    }
+    if (N & 1) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) w[0][r] = c.swap ? w[1][r] : w[0][r];
+    }
+  }
+  __device__ __forceinline__ f32x4_t frag(int odd) const { return f32x4_t{w[odd][0], w[odd][1], w[odd][2], w[odd][3]}; }
+  __device__ __forceinline__ void slope(const ColumnPart& z, int act, float& s0, float& s1) {
+    op_slope_all<8>(&w[0][0], &z.w[0][0], act);
+    sum(s0, s1);
+  }
+  __device__ __forceinline__ void sum(float& s0, float& s1) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) { s0 += w[0][r]; s1 += w[1][r]; }
+  }
+};
+
+template <typename T>
+struct DzSource { const T* dy; const T* z; int64_t lddy, ldz; int act; };
+
+// Tiles of one of the products; its contraction in `splits` shares of `steps` blocks each, which leave in fp32 to be joined.
+template <typename T>
+struct SmallPart { Epilogue<T> e; int nt, tiles, splits, steps; };
+template <typename T>
+struct SmallArgs {
+  const T* x; const T* w;
+  int64_t ldx, ldw;
+  int rows, d_in, d_out;
+  DzSource<T> dz;
+  SmallPart<T> a, b;                   // a: the forward product, or dx; b: dW (its workgroups come behind dx's)
+  float* db;                           // or its shares [splits][d_out]
+  bool dw;
+};
+
+// 32 rows of the partial results of all wavefronts, added in their order, and what follows
+template <typename T>
+__device__ __forceinline__ void small_finish(const Epilogue<T>& e, const f32x16_t& a0, const f32x16_t& a1, float* red, int waves, int64_t m0,
+                                             int m_step, int64_t M, int64_t n0, int64_t N) {
+  constexpr int kPitch = 64 + 4, V = kPiece<T>, LPR = 64 / V;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  if (wave < waves) {
+    float* q = red + (wave * 32 + (lane & 31)) * kPitch + 8 * (lane >> 5);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {       // registers 4 b .. of a0 / a1: even / odd columns 2 (8 b + 4 (lane / 32) + r)
+      *(f32x4_t*)(q + 16 * b) = f32x4_t{a0[4 * b], a1[4 * b], a0[4 * b + 1], a1[4 * b + 1]};
+      *(f32x4_t*)(q + 16 * b + 4) = f32x4_t{a0[4 * b + 2], a1[4 * b + 2], a0[4 * b + 3], a1[4 * b + 3]};
+    }
+  }
+  __syncthreads();
+  for (int r = t / LPR; r < 32; r += 512 / LPR) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.f;
+    const float* q = red + r * kPitch + (t % LPR) * V;
+    for (int w = 0; w < waves; ++w)
+#pragma unroll
+      for (int h = 0; h < V / 4; ++h) {
+        const f32x4_t s = *(const f32x4_t*)(q + w * 32 * kPitch + 4 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * h + i] += s[i];
+      }
+    const int64_t m = m0 + (int64_t)r * m_step;
+    if (m < M) finish(e, m, n0 + (t % LPR) * V, N, v);
+  }
+}
+
+// A wavefront's blocks first, first + 8, ... of the contraction, U at a time: all their loads stand before the first use.
+template <int U, typename Step, typename Load, typename Use>
+__device__ __forceinline__ void in_steps(int first, int blocks, Load load, Use use) {
+  int kb = first;
+  for (; kb + (U - 1) * kSmallWaves < blocks; kb += U * kSmallWaves) {
+    Step s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(kb + u * kSmallWaves, s[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) use(s[u]);
+  }
+  for (; kb < blocks; kb += kSmallWaves) {
+    Step s;
+    load(kb, s);
+    use(s);
+  }
+}
+
+template <typename T, bool BACKWARD>
+__global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
+  constexpr int R = kPiece<T>;
+  __shared__ __attribute__((aligned(16))) float red[kSmallWaves * 32 * 68];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, lk = lane >> 5;
+  f32x16_t acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  // this workgroup's tile, share of the contraction and blocks of it
+  int n0, tm, first, blocks, waves, split;
+  auto place = [&](const SmallPart<T>& part, int id, int K) {
+    split = part.splits > 1 ? id / part.tiles : 0;
+    const int tile = id - split * part.tiles;
+    tm = tile / part.nt;
+    n0 = (tile - tm * part.nt) * 64;
+    first = split * part.steps;
+    blocks = min((K + kBlockK<T> - 1) / kBlockK<T>, first + part.steps);
+    waves = min(kSmallWaves, blocks - first);
+  };
+  auto epilogue = [&](const SmallPart<T>& part) {
+    Epilogue<T> e = part.e;
+    if (e.part) e.part += split * e.part_stride;
+    return e;
+  };
+  if constexpr (!BACKWARD) {
+    const int K = g.d_in;
+    place(g.a, blockIdx.x, K);
+    const int m0 = tm * 32;
+    const T* const xr = g.x + (int64_t)min(m0 + l32, g.rows - 1) * g.ldx;
+    struct Step { RowPart<T> a; ColumnPart<T> b; };
+    const ColumnPlace c = column_place(n0 + 2 * l32, g.d_out);
+    in_steps<4, Step>(first + wave, blocks,
+        [&](int kb, Step& s) {
+          const int k = kb * kBlockK<T> + lk * R;
+          s.a.load(xr, k, K);
+          s.b.load(g.w, g.ldw, k, K, c, g.d_out);
+        },
+        [&](Step& s) {
+          acc[0][0] = multiply(s.b.frag(0), s.a.frag(), acc[0][0]);
+          acc[0][1] = multiply(s.b.frag(1), s.a.frag(), acc[0][1]);
+        });
+    small_finish<T>(epilogue(g.a), acc[0][0], acc[0][1], red, waves, m0, 1, g.rows, n0, g.d_out);
+    return;
+  }
+  const int dx_blocks = g.a.tiles * g.a.splits;
+  if ((int)blockIdx.x < dx_blocks) {                        // dx = dz W^T
+    const int K = g.d_out;
+    place(g.a, blockIdx.x, K);
+    const int m0 = tm * 32;
+    const int64_t row = min(m0 + l32, g.rows - 1);
+    const T* const dr = g.dz.dy + row * g.dz.lddy;
+    const T* const zr = g.dz.z + row * g.dz.ldz;
+    const T* const w0 = g.w + (int64_t)min(n0 + 2 * l32, g.d_in - 1) * g.ldw;
+    const T* const w1 = g.w + (int64_t)min(n0 + 2 * l32 + 1, g.d_in - 1) * g.ldw;
+    struct Step { RowPart<T> a, z, b0, b1; };
+    in_steps<4, Step>(first + wave, blocks,
+        [&](int kb, Step& s) {
+          const int k = kb * kBlockK<T> + lk * R;
+          s.a.load(dr, k, K);
+          if (g.dz.act != ABS_ACT_NONE) s.z.load(zr, k, K);
+          s.b0.load(w0, k, K);
+          s.b1.load(w1, k, K);
+        },
+        [&](Step& s) {
+          if (g.dz.act != ABS_ACT_NONE) s.a.slope(s.z, g.dz.act);
+          acc[0][0] = multiply(s.b0.frag(), s.a.frag(), acc[0][0]);
+          acc[0][1] = multiply(s.b1.frag(), s.a.frag(), acc[0][1]);
+        });
+    small_finish<T>(epilogue(g.a), acc[0][0], acc[0][1], red, waves, m0, 1, g.rows, n0, g.d_in);
+    return;
+  }
+  // dW = x^T dz, and db in the first row of tiles
+  const int K = g.rows;
+  place(g.b, (int)blockIdx.x - dx_blocks, K);
+  const int m0 = tm * 64;
+  float s0 = 0.f, s1 = 0.f;
+  struct Step { ColumnPart<T> a, b, z; };
+  const ColumnPlace ca = column_place(m0 + 2 * l32, g.d_in), cb = column_place(n0 + 2 * l32, g.d_out);
+  in_steps<2, Step>(first + wave, blocks,
+      [&](int kb, Step& s) {
+        const int k = kb * kBlockK<T> + lk * R;
+        s.a.load(g.x, g.ldx, k, K, ca, g.d_in);
+        s.b.load(g.dz.dy, g.dz.lddy, k, K, cb, g.d_out);
+        if (g.dz.act != ABS_ACT_NONE) s.z.load(g.dz.z, g.dz.ldz, k, K, cb, g.d_out);
+      },
+      [&](Step& s) {
+        if (g.dz.act != ABS_ACT_NONE) s.b.slope(s.z, g.dz.act, s0, s1);
+        else if (g.db && m0 == 0) s.b.sum(s0, s1);
+        const Frag<T> fa0 = s.a.frag(0), fa1 = s.a.frag(1), fb0 = s.b.frag(0), fb1 = s.b.frag(1);
+        acc[0][0] = multiply(fb0, fa0, acc[0][0]);
+        acc[0][1] = multiply(fb1, fa0, acc[0][1]);
+        acc[1][0] = multiply(fb0, fa1, acc[1][0]);
+        acc[1][1] = multiply(fb1, fa1, acc[1][1]);
+      });
+  if (g.db && m0 == 0) {
+    s0 += __shfl_xor(s0, 32);
+    s1 += __shfl_xor(s1, 32);
+    if (lane < 32) { red[wave * 64 + 2 * l32] = s0; red[wave * 64 + 2 * l32 + 1] = s1; }
+    __syncthreads();
+    if (t < 64 && n0 + t < g.d_out) {
+      float s = 0.f;
+      for (int w = 0; w < waves; ++w) s += red[w * 64 + t];
+      g.db[(int64_t)split * g.d_out + n0 + t] = s;
+    }
+    __syncthreads();
+  }
+  if (!g.dw) return;
+  const Epilogue<T> e = epilogue(g.b);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {                             // rows m0 + i, m0 + i + 2, ...
+    if (i) __syncthreads();
+    small_finish<T>(e, acc[i][0], acc[i][1], red, waves, m0 + i, 2, g.d_in, n0, g.d_out);
   }
 }
 
@@ -509,7 +809,6 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(const T* x, int64_t ld
 template <typename T, int V>
 __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t lddy, const T* z, int64_t ldz, T* dz, int64_t lddz, int64_t rows,
                                                         int N, int act, float* sums) {
-  typedef OpVec<T, V> Vec;
   __shared__ float red[8][32 * V + 1];
   const int t = threadIdx.x, c = t & 31, rl = t >> 5;
   const int n = ((int)blockIdx.x * 32 + c) * V;
@@ -517,18 +816,19 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t ldd
 #pragma unroll
   for (int e = 0; e < V; ++e) s[e] = 0.f;
   if (n < N) {
+#pragma unroll 2
     for (int64_t m = (int64_t)blockIdx.y * 8 + rl; m < rows; m += (int64_t)gridDim.y * 8) {
-      const Vec d = *(const Vec*)(dy + m * lddy + n);
-      Vec zv, o;
-      if (act != ABS_ACT_NONE) zv = *(const Vec*)(z + m * ldz + n);
+      Piece<T, V> d, h, o;
+      d.load(dy + m * lddy + n);
+      if (act != ABS_ACT_NONE) h.load(z + m * ldz + n);
+      float f[V], g[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        float v = op_widen(d.e[e]);
-        if (act != ABS_ACT_NONE) v *= op_act_slope(op_widen(zv.e[e]), act);
-        s[e] += v;
-        op_narrow(v, o.e[e]);
-      }
-      if (dz) *(Vec*)(dz + m * lddz + n) = o;
+      for (int e = 0; e < V; ++e) { f[e] = d.at(e); g[e] = act != ABS_ACT_NONE ? h.at(e) : 0.f; }
+      op_slope_all<V>(f, g, act);
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += f[e];
+      o.set(f);
+      if (dz) o.store(dz + m * lddz + n);
     }
   }
   if (!sums) return;
@@ -551,6 +851,7 @@ __global__ __launch_bounds__(256) void linear_db_kernel(const float* sums, int s
   const int c = threadIdx.x & 31, r = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
   float v = 0.f;
   if (n < N)
+#pragma unroll 8
     for (int k = r; k < shares; k += 8) v += sums[(int64_t)k * N + n];
   red[r][c] = v;
   __syncthreads();
@@ -568,10 +869,13 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(const T* src, int64_t 
   const int64_t pieces = ldd / V, total = rows * pieces;
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
     const int64_t m = q / pieces, c = (q - m * pieces) * V;
-    OpVec<T, V> o;
+    Loose<T, V> o;
+    if (c + V <= cols) o = *(const Loose<T, V>*)(src + m * ld + c);
+    else {
 #pragma unroll
-    for (int e = 0; e < V; ++e) o.e[e] = c + e < cols ? src[m * ld + c + e] : T(0);
-    *(OpVec<T, V>*)(dst + m * ldd + c) = o;
+      for (int e = 0; e < V; ++e) o.e[e] = c + e < cols ? src[m * ld + c + e] : T(0);
+    }
+    *(Loose<T, V>*)(dst + m * ldd + c) = o;
   }
 }
 
@@ -583,8 +887,6 @@ __global__ __launch_bounds__(256) void linear_zero_kernel(T* p, int64_t ld, int6
 unsigned few_blocks(int64_t threads) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((threads + 255) / 256, 1 << 16)); }
 
 // ---------------------------------------------------------------------- the plan
-constexpr int kFewRows = 8;                  // up to here linear_rows_kernel
-
 struct Product {                              // one product on a tile kernel
   bool big;
   int mt, nt, nsplit, steps_per_split;
@@ -619,9 +921,23 @@ Product plan_product(int64_t M, int64_t N, int64_t K, int dtype) {
   return q;
 }
 
+// Which products linear_small_kernel takes (us, it / the tile kernels with their copies, dz and joins; bf16 unless said).  Forward
+// 810 x 520 x 300 6.4 / 14.9, 1024^3 10.3 / 20.9, 2048 x 2048 x 512 20 / 24, 4096 x 1024 x 1024 32 / 20; fp32 2048 x 512 x 512
+// 22 / 27, 1024^3 38 / 35.  Backward 200 x 256 x 256 8.3 / 20, 1000^3 41 / 50, 4096 x 512 x 512 55 / 51, 2048 x 2048 x 512 91 / 38; fp32
+// 2048 x 512 x 512 52 / 59, 1000^3 83 / 75.  A dW of many tiles with few rows each is not for it: 8 x 4096 x 4096 80 / 35.
+bool small_product(const abs_linear& p, bool backward) {
+  const bool half = p.dtype == ABS_X_BF16;
+  const double macs = (double)p.rows * p.d_in * p.d_out;
+  if (p.d_in < 2 || p.d_out < 2) return false;                       // (columns are read in pairs)
+  return backward ? macs <= (half ? 1.1e9 : 8e8) && (double)p.d_in * p.d_out <= 4.3e6 : macs <= (half ? 2.2e9 : 9e8);
+}
+
+struct SmallProduct { int nt, tiles, splits, steps; size_t part_bytes; };
+
 struct LinearPlan {
-  bool pack_x, pack_w, few, dz;
-  int V, run, runs, sum_rows;
+  bool small, pack_x, pack_w, dz;
+  int sum_rows;
+  SmallProduct sa, sb;                        // the forward product or dx; dW
   Product fwd, dx, dw;
   int64_t in8, out8;                          // d_in, d_out in whole pieces
   size_t off_x, off_w, off_dz, off_sums, off_part, bytes;
@@ -637,24 +953,36 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
   const bool w_whole = w_ok && p.d_out % piece == 0 && p.ldw % piece == 0;
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = op_round_up(o + bytes, 256); return at; };
+  q.small = small_product(p, backward);
+  if (q.small) {
+    const int block = p.dtype == ABS_X_BF16 ? 16 : 8;
+    auto split = [&](int64_t M, int64_t N, int64_t K, int rows_of_tile) {
+      SmallProduct s{};
+      s.nt = (int)((N + 63) / 64);
+      s.tiles = (int)((M + rows_of_tile - 1) / rows_of_tile) * s.nt;
+      // a long contraction of few tiles in shares, four blocks a wavefront at least
+      const int64_t blocks = (K + block - 1) / block, each = 4 * kSmallWaves;
+      const int64_t shares = blocks <= (p.dtype == ABS_X_BF16 && rows_of_tile == 32 ? 4 : 2) * each ? 1 : std::max<int64_t>(1, std::min<int64_t>((blocks + each - 1) / each, 640 / s.tiles));
+      s.steps = (int)((blocks + shares - 1) / shares);
+      s.splits = (int)((blocks + s.steps - 1) / s.steps);
+      s.part_bytes = s.splits > 1 ? op_round_up((size_t)s.splits * M * op_round_up(N, 4) * 4, 256) : 0;
+      return s;
+    };
+    q.sa = backward ? split(p.rows, p.d_in, p.d_out, 32) : split(p.rows, p.d_out, p.d_in, 32);
+    if (backward) q.sb = split(p.d_in, p.d_out, p.rows, 64);
+    q.off_part = take(q.sa.part_bytes);
+    q.off_dz = take(q.sb.part_bytes);
+    q.off_sums = take(q.sb.splits > 1 ? (size_t)q.sb.splits * p.d_out * 4 : 0);
+    q.bytes = o;
+    return q;
+  }
   if (!backward) {
-    q.few = p.rows <= kFewRows;
-    if (q.few) {
-      q.V = w_whole ? piece : 1;
-      // runs of the contraction: about two workgroups per CU
-      const int blocks = (p.d_out + 8 * q.V - 1) / (8 * q.V);
-      const int want = std::max(1, 512 / blocks);
-      q.run = std::max(64, (int)op_round_up((p.d_in + want - 1) / want, 32));
-      q.runs = (p.d_in + q.run - 1) / q.run;
-      q.off_part = take((size_t)q.runs * p.rows * op_round_up(p.d_out, 4) * 4);
-    } else {
-      q.pack_x = !x_whole;
-      q.pack_w = !w_whole;
-      if (q.pack_x) q.off_x = take((size_t)p.rows * q.in8 * size);
-      if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
-      q.fwd = plan_product(p.rows, p.d_out, p.d_in, p.dtype);
-      q.off_part = take(q.fwd.part_bytes);
-    }
+    q.pack_x = !x_whole;
+    q.pack_w = !w_whole;
+    if (q.pack_x) q.off_x = take((size_t)p.rows * q.in8 * size);
+    if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
+    q.fwd = plan_product(p.rows, p.d_out, p.d_in, p.dtype);
+    q.off_part = take(q.fwd.part_bytes);
   } else {
     q.pack_x = !x_whole;
     q.pack_w = !w_whole;
@@ -662,8 +990,9 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
     q.dz = p.act != ABS_ACT_NONE || !(dy_ok && p.d_out % piece == 0 && p.lddy % piece == 0);
     if (q.dz) q.off_dz = take((size_t)p.rows * q.out8 * size);
-    const int cols = (p.d_out + 31) / 32;
-    q.sum_rows = (int)std::max<int64_t>(1, std::min<int64_t>((p.rows + 31) / 32, std::max(1, 4096 / cols)));
+    // eight workgroups on every CU, 16 rows each at least
+    const int cols = p.d_out % piece == 0 ? (p.d_out / piece + 31) / 32 : (p.d_out + 31) / 32;
+    q.sum_rows = (int)std::max<int64_t>(1, std::min<int64_t>((p.rows + 15) / 16, std::max(1, 2048 / cols)));
     q.off_sums = take((size_t)q.sum_rows * p.d_out * 4);
     q.dx = plan_product(p.rows, p.d_in, p.d_out, p.dtype);
     q.dw = plan_product(p.d_in, p.d_out, p.rows, p.dtype);
@@ -694,6 +1023,16 @@ hipError_t pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* d
   return hipGetLastError();
 }
 
+// (a job without shares is left out)
+template <typename T>
+hipError_t launch_join(const Join<T>& a, const Join<T>& b, hipStream_t s) {
+  const Join<T>& one = a.shares ? a : b;
+  auto threads = [](const Join<T>& j) { return j.shares ? std::max(j.M * ((j.N + kPiece<T> - 1) / kPiece<T>), j.db ? j.N : 0) : 0; };
+  const bool both = a.shares && b.shares;
+  linear_join_kernel<T><<<dim3(few_blocks(std::max(threads(a), threads(b))), both ? 2 : 1), 256, 0, s>>>(one, b);
+  return hipGetLastError();
+}
+
 template <typename T, bool ATR, bool BTR>
 hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, hipStream_t s) {
   g.mt = q.mt; g.nt = q.nt; g.nsplit = q.nsplit; g.steps_per_split = q.steps_per_split;
@@ -711,33 +1050,29 @@ hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, hipStream_t
   else linear_tile_kernel<T, ATR, BTR, 4><<<grid, 256, 0, s>>>(g);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && q.nsplit > 1) {
-    linear_join_kernel<T><<<few_blocks(g.M * ((g.N + kPiece<T> - 1) / kPiece<T>)), 256, 0, s>>>(join, g.M, g.N, q.nsplit);
-    e = hipGetLastError();
+    e = launch_join(Join<T>{join, g.M, g.N, q.nsplit, nullptr, nullptr}, Join<T>{}, s);
   }
   return e;
 }
 
-// a 16-byte piece of columns as one access, in every array
 template <typename T>
-bool pieces_ok(int64_t N, std::initializer_list<std::pair<const void*, int64_t>> arrays) {
-  if (N % kPiece<T>) return false;
-  for (const auto& a : arrays)
-    if (a.first && (a.second % kPiece<T> || !op_aligned(a.first, 16))) return false;
-  return true;
+SmallArgs<T> small_args(const abs_linear& p, const void* x, const void* w) {
+  SmallArgs<T> g{};
+  g.x = (const T*)x; g.w = (const T*)w; g.ldx = p.ldx; g.ldw = p.ldw;
+  g.rows = (int)p.rows; g.d_in = p.d_in; g.d_out = p.d_out;
+  return g;
 }
-
-template <typename T, int V>
-hipError_t launch_rows(const abs_linear& p, const LinearPlan& q, const void* x, const void* w, float* part, hipStream_t s) {
-  const dim3 grid((unsigned)((p.d_out + 8 * V - 1) / (8 * V)), (unsigned)q.runs);
-  const int64_t ldpart = (int64_t)op_round_up(p.d_out, 4);
-#define ABS_ROWS(R_) linear_rows_kernel<T, V, R_><<<grid, 256, 0, s>>>((const T*)x, p.ldx, (const T*)w, p.ldw, (int)p.rows, p.d_in, p.d_out, q.run, \
-                                                                       part, ldpart, p.rows * ldpart)
-  if (p.rows == 1) ABS_ROWS(1);
-  else if (p.rows <= 2) ABS_ROWS(2);
-  else if (p.rows <= 4) ABS_ROWS(4);
-  else ABS_ROWS(8);
-#undef ABS_ROWS
-  return hipGetLastError();
+// one product of linear_small_kernel, and what joins its shares (join.shares stays 0 where there is one)
+template <typename T>
+SmallPart<T> small_part(const SmallProduct& q, const Epilogue<T>& e, float* part, int64_t M, int64_t N, Join<T>& join) {
+  SmallPart<T> s{e, q.nt, q.tiles, q.splits, q.steps};
+  if (q.splits > 1) {
+    s.e.part = part;
+    s.e.ldpart = (int64_t)op_round_up(N, 4);
+    s.e.part_stride = M * s.e.ldpart;
+    join = Join<T>{s.e, M, N, q.splits, nullptr, nullptr};
+  }
+  return s;
 }
 
 template <typename T>
@@ -746,17 +1081,15 @@ hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, 
   Epilogue<T> e{};
   e.bias = b; e.r = (const T*)r; e.y = (T*)y; e.z = (T*)z;
   e.ldr = p.ldr; e.ldy = p.ldy; e.ldz = p.ldz; e.act = p.act;
-  e.vec = pieces_ok<T>(p.d_out, {{r, p.ldr}, {y, p.ldy}, {z, p.ldz}}) && (!b || op_aligned(b, 16));
-  float* part = (float*)(ws + q.off_part);
-  if (q.few) {
-    hipError_t err = q.V == kPiece<T> ? launch_rows<T, kPiece<T>>(p, q, x, w, part, s) : launch_rows<T, 1>(p, q, x, w, part, s);
-    if (err != hipSuccess) return err;
-    e.part = part;
-    e.ldpart = (int64_t)op_round_up(p.d_out, 4);
-    e.part_stride = p.rows * e.ldpart;
-    linear_join_kernel<T><<<few_blocks(p.rows * ((p.d_out + kPiece<T> - 1) / kPiece<T>)), 256, 0, s>>>(e, p.rows, p.d_out, q.runs);
-    return hipGetLastError();
+  if (q.small) {
+    SmallArgs<T> g = small_args<T>(p, x, w);
+    Join<T> join{};
+    g.a = small_part(q.sa, e, (float*)(ws + q.off_part), p.rows, p.d_out, join);
+    linear_small_kernel<T, false><<<dim3((unsigned)(q.sa.tiles * q.sa.splits)), 512, 0, s>>>(g);
+    const hipError_t err = hipGetLastError();
+    return err == hipSuccess && q.sa.splits > 1 ? launch_join(join, Join<T>{}, s) : err;
   }
+  float* part = (float*)(ws + q.off_part);
   GemmArgs<T> g{};
   g.A = (const T*)x; g.lda = p.ldx; g.B = (const T*)w; g.ldb = p.ldw;
   hipError_t err = hipSuccess;
@@ -773,13 +1106,34 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
                         float* db, char* ws, hipStream_t s) {
   constexpr int V = kPiece<T>;
   hipError_t err = hipSuccess;
+  if (q.small) {
+    SmallArgs<T> g = small_args<T>(p, x, w);
+    g.dz = {(const T*)dy, (const T*)z, p.lddy, p.ldz, p.act};
+    Epilogue<T> ea{}, eb{};
+    ea.y = (T*)dx; ea.ldy = p.lddx;
+    eb.y = (T*)dw; eb.ldy = p.lddw;
+    Join<T> ja{}, jb{};
+    if (dx) g.a = small_part(q.sa, ea, (float*)(ws + q.off_part), p.rows, p.d_in, ja);
+    if (dw || db) {
+      g.b = small_part(q.sb, eb, (float*)(ws + q.off_dz), dw ? p.d_in : 0, p.d_out, jb);
+      if (!dw) g.b.tiles = g.b.nt;                            // (db alone: the first row of dW's tiles)
+      g.dw = dw != nullptr;
+      g.db = db && q.sb.splits > 1 ? (float*)(ws + q.off_sums) : db;
+      if (db && q.sb.splits > 1) { jb.db_part = g.db; jb.db = db; }
+    }
+    const int blocks = g.a.tiles * g.a.splits + g.b.tiles * g.b.splits;
+    if (blocks == 0) return hipSuccess;
+    linear_small_kernel<T, true><<<dim3((unsigned)blocks), 512, 0, s>>>(g);
+    err = hipGetLastError();
+    return err == hipSuccess && (ja.shares || jb.shares) ? launch_join(ja, jb, s) : err;
+  }
   const T* dz = (const T*)dy;
   int64_t lddz = p.lddy;
   const bool products = dx || dw;
   float* sums = db ? (float*)(ws + q.off_sums) : nullptr;
   if ((q.dz && products) || db) {
     T* out = q.dz && products ? (T*)(ws + q.off_dz) : nullptr;
-    const bool whole = p.d_out % V == 0 && p.lddy % V == 0 && op_aligned(dy, 16) && (p.act == ABS_ACT_NONE || (p.ldz % V == 0 && op_aligned(z, 16)));
+    const bool whole = p.d_out % V == 0;
     const int per = whole ? 32 * V : 32;
     const dim3 grid((unsigned)((p.d_out + per - 1) / per), (unsigned)q.sum_rows);
     if (whole) linear_dz_kernel<T, V><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
@@ -801,7 +1155,7 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     g.A = dz; g.lda = lddz; g.B = (const T*)w; g.ldb = p.ldw;
     if (q.pack_w) { g.B = (const T*)(ws + q.off_w); g.ldb = q.out8; err = pack<T>(w, p.ldw, p.d_in, p.d_out, ws + q.off_w, q.out8, s); }
     g.M = p.rows; g.N = p.d_in; g.K = p.d_out;
-    g.e.y = (T*)dx; g.e.ldy = p.lddx; g.e.vec = pieces_ok<T>(p.d_in, {{dx, p.lddx}});
+    g.e.y = (T*)dx; g.e.ldy = p.lddx;
     if (err == hipSuccess) err = run_product<T, false, false>(q.dx, g, part, s);
   }
   if (err == hipSuccess && dw) {
@@ -809,7 +1163,7 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     g.A = (const T*)x; g.lda = p.ldx; g.B = dz; g.ldb = lddz;
     if (q.pack_x) { g.A = (const T*)(ws + q.off_x); g.lda = q.in8; err = pack<T>(x, p.ldx, p.rows, p.d_in, ws + q.off_x, q.in8, s); }
     g.M = p.d_in; g.N = p.d_out; g.K = p.rows; g.mc = q.in8; g.nc = q.out8;
-    g.e.y = (T*)dw; g.e.ldy = p.lddw; g.e.vec = pieces_ok<T>(p.d_out, {{dw, p.lddw}});
+    g.e.y = (T*)dw; g.e.ldy = p.lddw;
     if (err == hipSuccess) err = run_product<T, true, true>(q.dw, g, part, s);
   }
   return err;

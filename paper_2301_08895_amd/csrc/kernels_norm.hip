@@ -2,7 +2,7 @@
 //
 // What bounds it is memory: the forward pass has to read and write every element once, the backward pass to read x and dy
 // and write dx.  So a group's values stay in registers between the statistics and their use wherever they fit:
-//  * lanes go along the channels in pieces of V elements (16 bytes where alignment and group width allow), groups padded
+//  * lanes go along the channels in pieces of V elements (16 bytes where the group width allows), groups padded
 //    to a power of two of lanes (SP), several groups side by side (TX = SP gpc lanes: 128 bytes of a position and more, so
 //    that lines are used whole) and PL positions on top: D = TX PL lanes hold one sample's share of gpc groups, NV
 //    pieces each.  A workgroup holds T / D samples.
@@ -654,7 +654,7 @@ int norm_widest(int dtype, bool backward) { return dtype == ABS_X_BF16 && !backw
 
 int pow2_up(int64_t x) { int p = 1; while (p < x) p <<= 1; return p; }
 
-// V: elements of a piece that all pointers, pitches and the group width allow (the same for every operand).
+// V: elements of a piece.
 NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
   NormPlan q{};
   const int size = op_size(p.dtype), per = p.channels / p.groups;
@@ -745,15 +745,11 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
   return q;
 }
 
-// the widest piece for a struct's sizes and pitches (pointers are looked at by the calls)
-int norm_piece(const abs_group_norm& p, bool backward, bool res, uintptr_t pointers) {
-  const int size = op_size(p.dtype), per = p.channels / p.groups;
-  for (int V = norm_widest(p.dtype, backward); V > 1; V /= 2) {
-    if (per % V || p.ldx % V || (pointers & (uintptr_t)(V * size - 1))) continue;
-    if (!backward && p.ldy % V == 0) return V;
-    if (backward && p.lddy % V == 0 && p.lddx % V == 0 && (!res || p.lddres % V == 0)) return V;
-  }
-  return 1;
+// the widest piece that a group is a whole number of (at any pitch and alignment)
+int norm_piece(const abs_group_norm& p, bool backward) {
+  int V = norm_widest(p.dtype, backward);
+  while (p.channels / p.groups % V) V /= 2;
+  return V;
 }
 
 const char* norm_problem(const abs_group_norm* p, bool backward) {
@@ -771,14 +767,6 @@ const char* norm_problem(const abs_group_norm* p, bool backward) {
   constexpr int64_t most = 1ll << 40;
   if (p->ldx >= most || (backward ? p->lddy >= most || p->lddx >= most : p->ldy >= most)) return "group norm: a pitch is 2^40 or more";
   return nullptr;
-}
-
-// the largest workspace over the pieces the pointers may force
-size_t norm_workspace(const abs_group_norm& p, bool backward) {
-  size_t most = 0;
-  for (int V = norm_widest(p.dtype, backward); V >= 1; V /= 2)
-    if ((p.channels / p.groups) % V == 0) most = std::max(most, norm_plan(p, backward, V).bytes);
-  return most;
 }
 
 template <typename T>
@@ -883,7 +871,7 @@ extern "C" {
 
 size_t abs_group_norm_workspace_size(const abs_group_norm* p, int32_t backward) {
   if (const char* why = norm_problem(p, backward != 0)) { op_fail(ABS_E_ARG, why); return 0; }
-  return p->n ? norm_workspace(*p, backward != 0) : 0;
+  return p->n ? norm_plan(*p, backward != 0, norm_piece(*p, backward != 0)).bytes : 0;
 }
 
 int abs_group_norm_forward(const abs_group_norm* p, const void* d_x, const float* d_gamma, const float* d_beta,
@@ -897,7 +885,7 @@ int abs_group_norm_forward(const abs_group_norm* p, const void* d_x, const float
   const uintptr_t all = (uintptr_t)d_x | (uintptr_t)d_y;
   if (all & (uintptr_t)(op_size(p->dtype) - 1) || ((uintptr_t)d_gamma | (uintptr_t)d_beta | (uintptr_t)d_mean | (uintptr_t)d_rstd) & 3)
     return op_fail(ABS_E_ARG, "group norm: a pointer is not aligned to its elements");
-  const NormPlan q = norm_plan(*p, false, norm_piece(*p, false, false, all));
+  const NormPlan q = norm_plan(*p, false, norm_piece(*p, false));
   if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "group norm: d_workspace must be 256-byte aligned");
   if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "group norm: workspace too small");
   hipError_t e;
@@ -932,7 +920,7 @@ int abs_group_norm_backward(const abs_group_norm* p, const void* d_x, const floa
     return op_hip("abs_group_norm_backward", hipGetLastError());
   }
   if (!d_x || !d_dy || !d_dx || !d_mean || !d_rstd) return op_fail(ABS_E_ARG, "group norm: a device pointer is NULL");
-  const NormPlan q = norm_plan(*p, true, norm_piece(*p, true, d_dres != nullptr, all));
+  const NormPlan q = norm_plan(*p, true, norm_piece(*p, true));
   if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "group norm: d_workspace must be 256-byte aligned");
   if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "group norm: workspace too small");
   hipError_t e;

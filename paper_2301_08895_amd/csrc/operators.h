@@ -37,22 +37,17 @@ __device__ __forceinline__ uint16_t op_bf16(float f) {
 __device__ __forceinline__ void op_narrow(float f, uint16_t& v) { v = op_bf16(f); }
 __device__ __forceinline__ void op_narrow(float f, float& v) { v = f; }
 
-// V elements that are loaded and stored as one piece
-template <typename T, int V>
-struct alignas(sizeof(T) * V) OpVec { T e[V]; };
+// N consecutive elements at any alignment of theirs, loaded or stored as one access (the memory system takes it at any address)
+template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Loose { T e[N]; };
 
-// The same held in whole registers: left as an array of 16-bit elements the compiler gives every one a register of its own.
-typedef uint32_t op_u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t op_u32x4 __attribute__((ext_vector_type(4)));
+// V elements held in whole registers: left as an array of 16-bit elements the compiler gives every one a register of its own.
 template <typename T, int V>
 struct Piece {
   static constexpr int kBytes = V * (int)sizeof(T), kWords = kBytes < 4 ? 1 : kBytes / 4;
   uint32_t w[kWords];
   __device__ __forceinline__ void load(const void* p) {
-    if constexpr (kBytes == 16) { const op_u32x4 v = *(const op_u32x4*)p; w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; w[3] = v[3]; }
-    else if constexpr (kBytes == 8) { const op_u32x2 v = *(const op_u32x2*)p; w[0] = v[0]; w[1] = v[1]; }
-    else if constexpr (kBytes == 4) w[0] = *(const uint32_t*)p;
-    else w[0] = *(const uint16_t*)p;
+    if constexpr (kBytes < 4) w[0] = *(const uint16_t*)p;
+    else { const Loose<T, V> l = *(const Loose<T, V>*)p; __builtin_memcpy(w, &l, kBytes); }
   }
   __device__ __forceinline__ float at(int e) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
@@ -80,10 +75,8 @@ struct Piece {
     }
   }
   __device__ __forceinline__ void store(void* p) const {
-    if constexpr (kBytes == 16) *(op_u32x4*)p = op_u32x4{w[0], w[1], w[2], w[3]};
-    else if constexpr (kBytes == 8) *(op_u32x2*)p = op_u32x2{w[0], w[1]};
-    else if constexpr (kBytes == 4) *(uint32_t*)p = w[0];
-    else *(uint16_t*)p = (uint16_t)w[0];
+    if constexpr (kBytes < 4) *(uint16_t*)p = (uint16_t)w[0];
+    else { Loose<T, V> l; __builtin_memcpy(&l, w, kBytes); *(Loose<T, V>*)p = l; }
   }
 };
 

@@ -27,7 +27,9 @@ def rows_of(rows, cols, dtype, pad=0, scale=1.0, lead=0):
 
 # one element, one row, ends of pieces / k-steps / tiles on either side, few and many rows, a contraction in shares
 SIZES = [(1, 1, 1), (1, 64, 8), (1, 2048, 520), (3, 65, 7), (8, 200, 33), (9, 7, 129), (17, 128, 128), (64, 72, 40), (127, 63, 127),
-         (128, 64, 256), (129, 65, 257), (130, 1000, 24), (257, 520, 300), (300, 1, 5), (33, 4100, 16), (512, 264, 640)]
+         (128, 64, 256), (129, 65, 257), (130, 1000, 24), (257, 520, 300), (300, 1, 5), (33, 4100, 16), (512, 264, 640),
+         # either side of where one launch takes the whole pass; its contractions in shares; tile kernels on ragged operands
+         (3, 9000, 40), (9001, 30, 18), (700, 1601, 1100), (1500, 1030, 1440), (6000, 515, 770), (2100, 2050, 2046), (5, 2100, 2101)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])

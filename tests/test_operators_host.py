@@ -60,28 +60,30 @@ def test_linear_refuses_pointers_and_pitches():
     assert f(C.byref(_linear(ldy=7)), P, P, None, None, P, None, P, big, None) == -1
     assert f(C.byref(_linear(ldz=7)), P, P, None, None, P, P, P, big, None) == -1
     assert f(C.byref(_linear(ldr=7)), P, P, None, P, P, None, P, big, None) == -1
-    need = _lib.abs_linear_workspace_size(C.byref(ok), 0, 1)
-    assert need > 0
-    assert f(C.byref(ok), P, P, None, None, P, None, P, need - 1, None) == -2
-    assert f(C.byref(ok), P, P, None, None, P, None, None, need, None) == -1
-    assert f(C.byref(ok), P, P, None, None, P, None, P + 16, need, None) == -1
+    wide = _linear(rows=40000, d_in=511, d_out=512, ldx=512, ldw=512, ldy=512)
+    need = _lib.abs_linear_workspace_size(C.byref(wide), 0, 1)
+    assert f(C.byref(wide), P, P, None, None, P, None, P, need - 1, None) == -2
+    assert f(C.byref(wide), P, P, None, None, P, None, None, need, None) == -1
+    assert f(C.byref(wide), P, P, None, None, P, None, P + 16, need, None) == -1
     assert b(C.byref(_linear(act=2)), P, P, None, P, P, P, P, P, big, None) == -1      # an activation without z
     assert b(C.byref(ok), P, P, None, None, P, P, P, P, big, None) == -1
     assert b(C.byref(ok), None, P, None, P, P, P, P, P, big, None) == -1               # dW needs x
     assert b(C.byref(ok), P, None, None, P, P, P, P, P, big, None) == -1               # dx needs W
     for name in ("lddy", "lddx", "lddw"):
         assert b(C.byref(_linear(**{name: 7})), P, P, None, P, P, P, P, P, big, None) == -1
-    need = _lib.abs_linear_workspace_size(C.byref(ok), 1, 1)
-    assert b(C.byref(ok), P, P, None, P, P, P, P, P, need - 1, None) == -2
+    wide = _linear(rows=40000, d_in=512, d_out=512, ldx=512, ldw=512, lddy=512, lddx=512, lddw=512)
+    need = _lib.abs_linear_workspace_size(C.byref(wide), 1, 1)
+    assert need > 0 and b(C.byref(wide), P, P, None, P, P, P, P, P, need - 1, None) == -2
 
 
 def test_linear_workspace_counts_copies_of_ragged_rows():
-    whole, ragged = _linear(rows=5000), _linear(rows=5000, d_in=15, ldx=15)
-    size = lambda p, back, aligned: _lib.abs_linear_workspace_size(C.byref(p), back, aligned)
-    assert size(whole, 0, 1) == 0                       # read in place
-    assert size(whole, 0, 0) >= 5000 * 16 * 2           # a start that is not a whole piece: a copy
-    assert size(ragged, 0, 1) >= 5000 * 16 * 2
-    assert size(_linear(rows=0), 0, 1) == 0 and size(_linear(rows=0), 1, 1) == 0
+    size = lambda back, aligned, **over: _lib.abs_linear_workspace_size(C.byref(_linear(**over)), back, aligned)
+    big = dict(rows=40000, d_in=512, d_out=512, ldx=512, ldw=512)
+    assert size(0, 1, **big) == 0                                 # read in place
+    assert size(0, 0, **big) >= 40000 * 512 * 2                   # a start that is not a whole piece: a copy
+    assert size(0, 1, **dict(big, d_in=511)) >= 40000 * 512 * 2   # nor is a row's length
+    assert size(0, 1) == 0 and size(1, 0, d_in=15) == 0           # small products: operands at any alignment, one launch
+    assert size(0, 1, rows=0) == 0 and size(1, 1, rows=0) == 0
 
 
 @pytest.mark.parametrize("over", [dict(dtype=2), dict(act=9), dict(n=-1), dict(spatial=0), dict(n=1 << 20, spatial=1 << 12), dict(channels=0),
