@@ -28,7 +28,8 @@
  * abs_get_model, abs_trace, abs_rounds_done, abs_kernel_stats, abs_mlp_round_plan
  * (reading results and bookkeeping out), abs_last_error, abs_batch_last_error,
  * abs_destroy, abs_batch_destroy, abs_evaluate_static (abs_evaluate without allocations),
- * abs_calibrate_mfma (a measurement aid).
+ * abs_calibrate_mfma (a measurement aid).  The operators of hidden layers (abs_linear_*, abs_group_norm_*, abs_dropout_*) and
+ * abs_create_blocks, an MLP built of them, are networks beyond the paper's own.
  */
 #ifndef ABS_H
 #define ABS_H
@@ -158,6 +159,34 @@ size_t abs_workspace_size(const abs_config* cfg);
  */
 int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const float* d_w0,
                void* d_workspace, size_t workspace_bytes, void* hip_stream, abs_ctx** out);
+
+/*
+ * An MLP whose hidden layers are residual blocks.  With cfg an ABS_MODEL_MLP configuration (U <= 1) of dims
+ * {d_0, ..., d_L}, the handle's network is
+ *   a_1 = x W_0 + b_0,
+ *   u_l = dropout(act(group norm(a_l; gamma_l, beta_l))),              1 <= l < L
+ *   a_{l+1} = u_l W_l + b_l, plus a_l where residual = 1, l < L - 1 and d_l = d_{l+1},
+ * softmax cross-entropy on a_L; held-out evaluation leaves dropout out.  Normalisation is per sample, so it needs
+ * nothing from the other workers' data.  Model vector (d_w0, abs_get_model): W_0, b_0, then per layer l >= 1
+ * gamma_l [d_l], beta_l [d_l], W_l [d_l, d_{l+1}], b_l.  bf16 operands, activations and matrix gradients (one per
+ * model version of a round), fp32 accumulation, statistics and master parameters.  Masks: abs_dropout's with the
+ * handle's seed at offset 8 t + l over round t's stacked minibatches (uploads grouped by model version, oldest first).
+ *  groups     of every hidden layer: divides d_1 .. d_{L-1}
+ *  act        ABS_ACT_*;  residual 0 / 1;  drop: probability in 65536ths, 0 = none;  eps > 0: of the normalisation
+ * All other calls take the handle like any MLP's (a batch's handles all with or all without blocks); a pass of
+ * abs_evaluate is N x B rows.  The workspace is abs_blocks_workspace_size() bytes (0: invalid).
+ */
+typedef struct abs_blocks {
+  int32_t groups;
+  int32_t act;
+  int32_t residual;
+  int32_t drop;
+  float   eps;
+  int32_t reserved;                   /* must be 0 */
+} abs_blocks;
+size_t abs_blocks_workspace_size(const abs_config* cfg, const abs_blocks* blocks);
+int abs_create_blocks(const abs_config* cfg, const abs_blocks* blocks, const void* d_X, const void* d_y,
+                      const float* d_w0, void* d_workspace, size_t workspace_bytes, void* hip_stream, abs_ctx** out);
 
 /* Advance n_rounds parameter-server rounds (Algorithm 1, server part, with the
  * workers' U local steps of Eq. 2 and the update of Eq. 3).  Returns when the
@@ -333,7 +362,7 @@ int abs_calibrate_mfma(int32_t data_mode, int32_t iters, int32_t workgroups, flo
                        void* hip_stream, double* h_ms, double* h_tflops);
 
 /*
- * Operators of a network's hidden layers: the product of a layer with bias, activation and residual in one
+ * Operators of a network's hidden layers (abs_create_blocks' networks are made of them): the product of a layer with bias, activation and residual in one
  * pass, group normalisation with an activation behind it, and dropout whose mask is a function of a counter;
  * each with its gradient.  They need no handle: sizes travel in a small struct, matrices are row-major DEVICE
  * arrays owned by the caller with a row pitch in elements (ld*, at least the row's length), in the dtype the

@@ -9,7 +9,8 @@ from .binding import (AbsConfig, AbsError, abs_config_bytes, abs_workspace_size,
                       abs_last_error, abs_destroy, abs_draw_time_ticks, abs_draw_batch_rows,
                       make_config, trace_stride, Simulation, library_path,
                       abs_batch_create, abs_batch_round, abs_batch_destroy, abs_batch_workspace_size, Batch,
-                      abs_mlp_round_plan, abs_evaluate_static, abs_calibrate_mfma)
+                      abs_mlp_round_plan, abs_evaluate_static, abs_calibrate_mfma, AbsBlocks, make_blocks,
+                      abs_blocks_workspace_size, abs_create_blocks)
 from .operators import (ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, linear_forward, linear_backward, group_norm_forward,
                         group_norm_backward, dropout_forward, dropout_backward, dropout_kept)
 
@@ -18,6 +19,7 @@ __all__ = ["AbsConfig", "AbsError", "abs_config_bytes", "abs_workspace_size", "a
            "abs_last_error", "abs_destroy", "abs_draw_time_ticks", "abs_draw_batch_rows",
            "make_config", "trace_stride", "Simulation", "library_path",
            "abs_batch_create", "abs_batch_round", "abs_batch_destroy", "abs_batch_workspace_size", "Batch",
-           "abs_mlp_round_plan", "abs_evaluate_static", "abs_calibrate_mfma",
+           "abs_mlp_round_plan", "abs_evaluate_static", "abs_calibrate_mfma", "AbsBlocks", "make_blocks",
+           "abs_blocks_workspace_size", "abs_create_blocks",
            "ACT_NONE", "ACT_RELU", "ACT_SILU", "ACT_GELU", "linear_forward", "linear_backward", "group_norm_forward",
            "group_norm_backward", "dropout_forward", "dropout_backward", "dropout_kept"]

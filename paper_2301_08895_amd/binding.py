@@ -63,6 +63,12 @@ class AbsDropout(C.Structure):
                 ("ldy", C.c_int64), ("ldr", C.c_int64), ("seed", C.c_uint64), ("offset", C.c_uint64)]
 
 
+class AbsBlocks(C.Structure):
+    """Mirror of `abs_blocks` in include/abs.h."""
+    _fields_ = [("groups", C.c_int32), ("act", C.c_int32), ("residual", C.c_int32), ("drop", C.c_int32), ("eps", C.c_float),
+                ("reserved", C.c_int32)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -81,6 +87,11 @@ def _load():
     lib.abs_workspace_size.argtypes = [cfgp]
     lib.abs_create.restype = C.c_int
     lib.abs_create.argtypes = [cfgp, vp, vp, vp, vp, sz, vp, C.POINTER(vp)]
+    blkp = C.POINTER(AbsBlocks)
+    lib.abs_blocks_workspace_size.restype = sz
+    lib.abs_blocks_workspace_size.argtypes = [cfgp, blkp]
+    lib.abs_create_blocks.restype = C.c_int
+    lib.abs_create_blocks.argtypes = [cfgp, blkp, vp, vp, vp, vp, sz, vp, C.POINTER(vp)]
     lib.abs_round.restype = C.c_int
     lib.abs_round.argtypes = [vp, i32]
     lib.abs_evaluate.restype = C.c_int
@@ -198,6 +209,27 @@ def abs_create(cfg: AbsConfig, d_X: int, d_y: int, d_w0: int, d_workspace: int,
     out = C.c_void_p()
     rc = _lib.abs_create(C.byref(cfg), d_X, d_y, d_w0, d_workspace, workspace_bytes, hip_stream,
                          C.byref(out))
+    _check(rc, None)
+    return out.value
+
+
+def make_blocks(b: dict) -> AbsBlocks:
+    """AbsBlocks from a workload's "blocks" record (keys as in workloads.with_blocks)."""
+    return AbsBlocks(b["groups"], b["act"], b["residual"], b["drop"], b["eps"], 0)
+
+
+def abs_blocks_workspace_size(cfg: AbsConfig, blocks: AbsBlocks) -> int:
+    n = _lib.abs_blocks_workspace_size(C.byref(cfg), C.byref(blocks))
+    if n == 0:
+        raise AbsError(-1, _lib.abs_last_error(None).decode())
+    return n
+
+
+def abs_create_blocks(cfg: AbsConfig, blocks: AbsBlocks, d_X: int, d_y: int, d_w0: int, d_workspace: int,
+                      workspace_bytes: int, hip_stream: int) -> int:
+    out = C.c_void_p()
+    rc = _lib.abs_create_blocks(C.byref(cfg), C.byref(blocks), d_X, d_y, d_w0, d_workspace, workspace_bytes, hip_stream,
+                                C.byref(out))
     _check(rc, None)
     return out.value
 
@@ -320,8 +352,12 @@ class Simulation:
         self.N = p["N"]
         self.cfg = make_config(p, device_mode, profile, k_replay)
         self.handle = None
+        blocks = make_blocks(p["blocks"]) if p.get("blocks") else None      # an MLP of residual blocks
         if not device_mode:
-            self.handle = abs_create(self.cfg, None, None, None, None, 0, None)
+            if blocks is not None:
+                self.handle = abs_create_blocks(self.cfg, blocks, None, None, None, None, 0, None)
+            else:
+                self.handle = abs_create(self.cfg, None, None, None, None, 0, None)
             self.P = None
             return
         if not torch.cuda.is_available():
@@ -339,14 +375,15 @@ class Simulation:
             shared[device] = hit
         self.d_X, self.d_y, self.d_w0 = hit[3:]
         self.P = int(inputs["w0"].size)
-        self.ws_bytes = abs_workspace_size(self.cfg)
+        self.ws_bytes = abs_workspace_size(self.cfg) if blocks is None else abs_blocks_workspace_size(self.cfg, blocks)
         self.d_ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=dev)
         base = self.d_ws.data_ptr()
         self.ws_ptr = (base + 255) // 256 * 256
         self.stream = torch.cuda.current_stream(dev)
         torch.cuda.synchronize(dev)
-        self.handle = abs_create(self.cfg, self.d_X.data_ptr(), self.d_y.data_ptr(), self.d_w0.data_ptr(),
-                                 self.ws_ptr, self.ws_bytes, self.stream.cuda_stream)
+        args = (self.d_X.data_ptr(), self.d_y.data_ptr(), self.d_w0.data_ptr(), self.ws_ptr, self.ws_bytes,
+                self.stream.cuda_stream)
+        self.handle = abs_create(self.cfg, *args) if blocks is None else abs_create_blocks(self.cfg, blocks, *args)
 
     def round(self, n: int = 1):
         abs_round(self.handle, n)

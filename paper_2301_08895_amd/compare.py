@@ -14,6 +14,11 @@ regression workloads all these simulations advance together as one batch (abs_ba
 
     python -m paper_2301_08895_amd.compare --config 2 --sweep-a 0,-1,-2,-3 --seeds 8 --rounds 600
 
+With --blocks G the MLP workloads' hidden layers are residual blocks (group normalisation in G groups, silu,
+dropout, product, residual: abs_create_blocks).
+
+    python -m paper_2301_08895_amd.compare --config 4 --blocks 32 --dropout 0.1 --methods abs,k_async --rounds 200 --M 20000
+
 Everything runs on the GPU through libabs (abs_round / abs_batch_round, abs_trace, abs_evaluate).
 """
 from __future__ import annotations
@@ -116,11 +121,20 @@ def main(argv=None):
     ap.add_argument("--a", type=int, default=None, help="constant of Eq. 4 for the abs variants")
     ap.add_argument("--json", action="store_true", help="one JSON object per read-out instead of the table")
     ap.add_argument("--sweep-a", default=None, help="comma-separated values of a: sweep Eq. 4's constant for the paper's method")
+    ap.add_argument("--blocks", type=int, default=None, metavar="GROUPS",
+                    help="MLP workloads: hidden layers as residual blocks, normalised in that many groups")
+    ap.add_argument("--dropout", type=float, default=0.1, help="with --blocks: the probability that an activation is dropped")
     ap.add_argument("--seeds", type=int, default=4, help="simulation seeds per value of --sweep-a")
     a = ap.parse_args(argv)
     p = workloads.preset(a.config)
     if a.M:
         p["M"] = a.M
+    if a.blocks is not None:
+        if p["model"] != workloads.presets.MODEL_MLP:
+            ap.error("--blocks needs an MLP workload (--config 3, 4 or 5)")
+        if not 0.0 <= a.dropout < 1.0:
+            ap.error("--dropout must be in [0, 1)")
+        p = workloads.with_blocks(p, a.blocks, drop=min(65535, round(a.dropout * 65536)))
     every = max(1, a.every)
     if a.sweep_a is not None:
         sweep_a(p, [int(v) for v in a.sweep_a.split(",")], max(1, a.seeds), a.rounds, every, a.eval_rows, a.target)

@@ -185,7 +185,8 @@ const char* abs_impl::kernel_kind_name(int kind) {
       "linreg_round", "softmax_rows", "softmax_update", "mlp_gather_t", "mlp_fwd_l1",
       "mlp_fwd_hidden", "mlp_fwd_logits", "mlp_logits_ce", "mlp_dgrad_out", "mlp_dgrad", "mlp_wgrad_l1", "mlp_wgrad",
       "mlp_update", "local_steps", "delta_update", "evaluate", "mlp_wgrad_out",
-      "cnn_conv_fwd", "cnn_dense", "cnn_dense_wgrad", "cnn_conv_bwd", "cnn_conv_wgrad", "cnn_combine"};
+      "cnn_conv_fwd", "cnn_dense", "cnn_dense_wgrad", "cnn_conv_bwd", "cnn_conv_wgrad", "cnn_combine",
+      "blocks_linear", "blocks_norm", "blocks_dropout", "blocks_loss", "blocks_update"};
   return kind >= 0 && kind < KK_COUNT ? names[kind] : "?";
 }
 
@@ -201,6 +202,8 @@ struct abs_ctx : public LaunchHook {
   RegPlan rplan{};
   MlpArgs margs{};
   CnnArgs cargs{};
+  bool blocks = false;            // an MLP of residual blocks: bargs in place of margs
+  BlocksArgs bargs{};
   LossMailbox* h_box = nullptr;   // pinned, device-visible [2]: abs_round posts round t's losses to the one of its parity
   LossMailbox* d_box = nullptr;   // the device's address of h_box
   // The newest version that a launch may have written, rounds that failed included: the ring holds version v while v > written - R.
@@ -330,18 +333,32 @@ size_t abs_workspace_size(const abs_config* cfg) {
   return p.total;
 }
 
-int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const float* d_w0,
-               void* d_workspace, size_t workspace_bytes, void* hip_stream, abs_ctx** out) {
+size_t abs_blocks_workspace_size(const abs_config* cfg, const abs_blocks* blocks) {
+  if (!cfg || !blocks) { g_create_error = "cfg / blocks is NULL"; return 0; }
+  std::string why;
+  if (!validate(*cfg, why)) { g_create_error = why; return 0; }
+  BlocksPlan p; const char* w = nullptr;
+  if (!blocks_plan(*cfg, *blocks, p, &w)) { g_create_error = w; return 0; }
+  return p.total;
+}
+
+static int create(const abs_config* cfg, const abs_blocks* blocks, const void* d_X, const void* d_y, const float* d_w0,
+                  void* d_workspace, size_t workspace_bytes, void* hip_stream, abs_ctx** out) {
   if (out) *out = nullptr;
   if (!cfg || !out) { g_create_error = "cfg / out is NULL"; return ABS_E_ARG; }
   std::string why;
   if (!validate(*cfg, why)) { g_create_error = why; return ABS_E_ARG; }
   std::unique_ptr<abs_ctx> c(new abs_ctx());
+  if (blocks) {
+    const char* w = nullptr;
+    if (!blocks_plan(*cfg, *blocks, c->bargs.plan, &w)) { g_create_error = w; return ABS_E_ARG; }
+    c->blocks = true;
+  }
   c->cfg = *cfg;
   if (c->cfg.U == 0) c->cfg.U = 1;
   c->sched.reset(new Scheduler(*cfg));
   c->cfg.k_replay = nullptr;
-  c->P = param_count(*cfg);
+  c->P = blocks ? c->bargs.plan.P : param_count(*cfg);
   c->R = cfg->tau_cap + 3;
   c->stream = (hipStream_t)hip_stream;
   if (!cfg->device_mode) { *out = c.release(); return ABS_OK; }
@@ -350,7 +367,7 @@ int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const fl
   if (((uintptr_t)d_workspace & 255) || ((uintptr_t)d_X & 15)) {
     g_create_error = "d_workspace must be 256-byte aligned and d_X 16-byte aligned"; return ABS_E_ARG;
   }
-  const size_t need = abs_workspace_size(cfg);
+  const size_t need = blocks ? c->bargs.plan.total : abs_workspace_size(cfg);
   if (workspace_bytes < need) { g_create_error = "workspace too small"; return ABS_E_WORKSPACE; }
   c->ws = (char*)d_workspace;
   c->dX = d_X; c->dy = d_y;
@@ -370,7 +387,15 @@ int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const fl
 
   const uint64_t shard = (uint64_t)(cfg->M / cfg->N);
   const uint64_t bkey = stream_key(cfg->seed, kStreamBatch);
-  if (cfg->model == ABS_MODEL_MLP) {
+  if (blocks) {
+    c->bargs.ws = c->ws;
+    c->bargs.X = (const uint16_t*)d_X;
+    c->bargs.y = (const int32_t*)d_y;
+    c->bargs.shard_rows = shard;
+    c->bargs.batch_key = bkey;
+    c->slot_stride = c->bargs.plan.slot_stride;
+    c->off_ring = c->bargs.plan.off_ring;
+  } else if (cfg->model == ABS_MODEL_MLP) {
     const char* w = nullptr;
     mlp_plan(*cfg, c->margs.plan, &w);
     c->margs.ws = c->ws;
@@ -400,7 +425,10 @@ int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const fl
   // w^0 into ring slot 0 (Algorithm 1, initialisation)
   e = hipMemcpyAsync(c->ws + c->off_ring, d_w0, c->P * sizeof(float), hipMemcpyDeviceToDevice, c->stream);
   if (e != hipSuccess) return fail("hipMemcpyAsync(w0)", e);
-  if (cfg->model == ABS_MODEL_MLP) {
+  if (blocks) {
+    e = blocks_prepare(c->bargs, c->stream);
+    if (e != hipSuccess) return fail("blocks_prepare", e);
+  } else if (cfg->model == ABS_MODEL_MLP) {
     e = mlp_prepare(c->margs, c->stream);
     if (e != hipSuccess) return fail("mlp_prepare", e);
   }
@@ -408,6 +436,18 @@ int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const fl
   if (e != hipSuccess) return fail("hipStreamSynchronize", e);
   *out = c.release();
   return ABS_OK;
+}
+
+int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const float* d_w0,
+               void* d_workspace, size_t workspace_bytes, void* hip_stream, abs_ctx** out) {
+  return create(cfg, nullptr, d_X, d_y, d_w0, d_workspace, workspace_bytes, hip_stream, out);
+}
+
+int abs_create_blocks(const abs_config* cfg, const abs_blocks* blocks, const void* d_X, const void* d_y, const float* d_w0,
+                      void* d_workspace, size_t workspace_bytes, void* hip_stream, abs_ctx** out) {
+  if (out) *out = nullptr;
+  if (!blocks) { g_create_error = "blocks is NULL"; return ABS_E_ARG; }
+  return create(cfg, blocks, d_X, d_y, d_w0, d_workspace, workspace_bytes, hip_stream, out);
 }
 
 // The device's view of round t of one simulation: the K^t uploads with the ring slot of their model
@@ -526,7 +566,10 @@ int abs_round(abs_ctx* ctx, int32_t n_rounds) {
     if (t >= ctx->enqueued) {
       ctx->written = std::max(ctx->written, t + 1);
       hipError_t e;
-      if (cfg.model == ABS_MODEL_MLP) {
+      if (ctx->blocks) {
+        ctx->bargs.mailbox = d_box;
+        e = launch_blocks_round(ctx->bargs, rd, ctx->stream, ctx);
+      } else if (cfg.model == ABS_MODEL_MLP) {
         ctx->margs.mailbox = d_box;
         e = launch_mlp_round(ctx->margs, rd, ctx->stream, ctx);
       } else if (cfg.model == ABS_MODEL_CNN) {
@@ -648,7 +691,7 @@ const char* batch_problem(abs_ctx** ctxs, int32_t n) {
     if (!c->cfg.device_mode) return "schedule-only handles cannot be batched";
     if (c->cfg.profile) return "batched rounds are not profiled per kernel (profile must be 0)";
     if (c->cfg.model != c0->cfg.model || c->cfg.dims[0] != c0->cfg.dims[0] || c->cfg.dims[1] != c0->cfg.dims[1] ||
-        c->cfg.B != c0->cfg.B || c->cfg.N != c0->cfg.N || c->cfg.U != c0->cfg.U || c->stream != c0->stream)
+        c->cfg.B != c0->cfg.B || c->cfg.N != c0->cfg.N || c->cfg.U != c0->cfg.U || c->stream != c0->stream || c->blocks != c0->blocks)
       return "all simulations of a batch need the same model, dims, N, B, U and stream";
   }
   return nullptr;
@@ -1013,12 +1056,14 @@ static int enqueue_evaluation(abs_ctx* ctx, int64_t version, const void* d_X, co
   const uint32_t slot = (uint32_t)(version % ctx->R);
   const bool mlp = cfg.model == ABS_MODEL_MLP, cnn = cfg.model == ABS_MODEL_CNN;
   e.X = d_X; e.y = d_y; e.n_rows = n_rows;
-  e.cap = mlp ? ctx->margs.plan.Mp : cnn ? ctx->cargs.plan.N * ctx->cargs.plan.B : kEvalChunk;
+  e.cap = ctx->blocks ? cfg.N * cfg.B : mlp ? ctx->margs.plan.Mp : cnn ? ctx->cargs.plan.N * ctx->cargs.plan.B : kEvalChunk;
   e.acc = (double*)scratch;
   e.rowloss = (float*)(scratch + 256);
   e.correct = (float*)(scratch + 256 + ((size_t)e.cap * 4 + 255) / 256 * 256);
   hipError_t err;
-  if (mlp) {
+  if (ctx->blocks) {
+    err = launch_blocks_eval(ctx->bargs, slot, e, ctx->stream, hook);
+  } else if (mlp) {
     err = launch_mlp_eval(ctx->margs, slot, e, ctx->stream, hook);
   } else if (cnn) {
     err = launch_cnn_eval(ctx->cargs, slot, e, ctx->stream, hook);
@@ -1034,7 +1079,7 @@ int abs_evaluate(abs_ctx* ctx, int64_t version, const void* d_X, const void* d_y
                  double* h_loss, double* h_accuracy) {
   if (!ctx || !h_loss || !h_accuracy) return ABS_E_ARG;
   const bool mlp = ctx->cfg.model == ABS_MODEL_MLP, cnn = ctx->cfg.model == ABS_MODEL_CNN;
-  char* scratch = ctx->ws ? ctx->ws + (mlp ? ctx->margs.plan.off_eval : cnn ? ctx->cargs.plan.off_eval : ctx->rplan.off_eval) : nullptr;
+  char* scratch = ctx->ws ? ctx->ws + (ctx->blocks ? ctx->bargs.plan.off_eval : mlp ? ctx->margs.plan.off_eval : cnn ? ctx->cargs.plan.off_eval : ctx->rplan.off_eval) : nullptr;
   EvalArgs e;
   const int rc = enqueue_evaluation(ctx, version, d_X, d_y, n_rows, scratch, ctx, e);
   if (rc != ABS_OK) return rc;
@@ -1051,6 +1096,7 @@ int abs_evaluate_static(abs_ctx* ctx, int64_t version, const void* d_X, const vo
                         double* d_out) {
   if (!ctx || !d_out) return ABS_E_ARG;
   const long pass_rows = !ctx->cfg.device_mode ? 0
+                         : ctx->blocks ? (long)ctx->cfg.N * ctx->cfg.B
                          : ctx->cfg.model == ABS_MODEL_MLP ? (long)ctx->margs.plan.Mp
                          : ctx->cfg.model == ABS_MODEL_CNN ? (long)ctx->cargs.plan.N * ctx->cargs.plan.B : 0;
   if (pass_rows > kStaticEvalRows) {

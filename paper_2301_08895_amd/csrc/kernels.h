@@ -46,6 +46,11 @@ enum KernelKind {
   KK_CNN_CONV_BWD,
   KK_CNN_CONV_WGRAD,
   KK_CNN_COMBINE,
+  KK_BLOCKS_LINEAR,
+  KK_BLOCKS_NORM,
+  KK_BLOCKS_DROPOUT,
+  KK_BLOCKS_LOSS,
+  KK_BLOCKS_UPDATE,
   KK_COUNT
 };
 const char* kernel_kind_name(int kind);
@@ -220,5 +225,36 @@ hipError_t cnn_prepare();       // once per process: LDS opt-in of the kernels
 hipError_t launch_cnn_round(const CnnArgs& a, const RoundDesc& rd, hipStream_t s, LaunchHook* hook);
 // forward pass of ring slot `slot` over e.n_rows evaluation rows, N B rows at a time (e.cap >= N B)
 hipError_t launch_cnn_eval(const CnnArgs& a, uint32_t slot, const EvalArgs& e, hipStream_t s, LaunchHook* hook);
+
+// ---- MLP of residual blocks: the library's operators in a chain ------------------------------
+struct BlocksPlan {
+  abs_blocks opt;
+  int L, B, N, R;
+  int d[8], ldw[8];                   // layer widths; row pitch of the bf16 copy of W_l
+  uint64_t seed;
+  size_t P, slot_stride;              // parameters; floats between ring slots
+  size_t w_off[8], b_off[8], gamma_off[8];   // W_l, b_l, gamma_l (beta_l behind it) inside a slot (floats)
+  size_t shadow_stride, shadow_off[8];       // bf16 copies of a version's matrices (elements)
+  // byte offsets into the workspace
+  size_t off_ring, off_shadow, off_label;
+  size_t off_a[8], off_u[8];          // a_l (l = 0: the gathered rows), u_l: bf16 [N B][d_l]
+  size_t off_mean[8], off_rstd[8];
+  size_t off_da[2], off_du;           // gradients of a_{l+1} / a_l in turn, of u_l
+  size_t off_dw, off_dv;              // one version's gradient of a matrix (bf16), of vectors (fp32)
+  size_t off_rowloss, off_ops, ops_bytes, off_eval, total;
+};
+bool blocks_plan(const abs_config& cfg, const abs_blocks& blocks, BlocksPlan& plan, const char** why);
+struct BlocksArgs {
+  BlocksPlan plan;
+  char* ws;
+  const uint16_t* X;                  // bf16 payload [M, d0]
+  const int32_t* y;
+  uint64_t shard_rows, batch_key;
+  LossMailbox* mailbox;
+};
+hipError_t blocks_prepare(const BlocksArgs& a, hipStream_t s);
+hipError_t launch_blocks_round(const BlocksArgs& a, const RoundDesc& rd, hipStream_t s, LaunchHook* hook);
+// forward pass of ring slot `slot` without dropout over e.n_rows evaluation rows, N B rows at a time (e.cap >= N B)
+hipError_t launch_blocks_eval(const BlocksArgs& a, uint32_t slot, const EvalArgs& e, hipStream_t s, LaunchHook* hook);
 
 }  // namespace abs_impl

@@ -162,3 +162,41 @@ def test_tensors_off_the_gpu_and_wrong_numbers_are_refused():
 def test_structs_match_the_library():
     # (abs_linear: two 32-bit and ten 64-bit words and two more; the sizes the header's layouts give)
     assert C.sizeof(AbsLinear) == 8 + 8 + 8 + 8 * 8 and C.sizeof(AbsGroupNorm) == 8 + 16 + 16 + 40 and C.sizeof(AbsDropout) == 8 + 7 * 8
+
+
+def _blocks_preset(**over):
+    import workloads
+    p = workloads.scaled_preset(3, M=400, dims=[16, 24, 24, 4], N=4, B=8, n_slow=1, k_mode=1)
+    q = workloads.with_blocks(p, groups=8)
+    q["blocks"].update({k: v for k, v in over.items() if k in q["blocks"]})
+    q.update({k: v for k, v in over.items() if k not in q["blocks"]})
+    return q
+
+
+@pytest.mark.parametrize("over", [dict(groups=0), dict(groups=7), dict(act=4), dict(residual=2), dict(drop=65536), dict(drop=-1),
+                                  dict(eps=0.0), dict(eps=float("nan")), dict(U=2), dict(N=0)])
+def test_blocks_refuse(over):
+    p = _blocks_preset(**over)
+    with pytest.raises(lib.AbsError) as e:
+        lib.Simulation(p, None, device_mode=0)
+    assert e.value.code == -1
+    with pytest.raises(lib.AbsError):
+        lib.abs_blocks_workspace_size(lib.make_config(p), lib.make_blocks(p["blocks"]))
+
+
+def test_blocks_follow_the_same_schedule_and_count_their_parameters():
+    import numpy as np
+    import workloads
+    p = _blocks_preset()
+    sim = lib.Simulation(p, None, device_mode=0)
+    plain = lib.Simulation({k: v for k, v in p.items() if k != "blocks"}, None, device_mode=0)
+    for s in (sim, plain):
+        s.round(20)
+    a, b = sim.trace(), plain.trace()
+    a[:, 10] = b[:, 10] = 0                    # the loss word: there are no losses without a device
+    assert np.array_equal(a, b)
+    assert workloads.param_count(p) == workloads.make_inputs(p)["w0"].size == 16 * 24 + 24 + 48 + 24 * 24 + 24 + 48 + 24 * 4 + 4
+    size = lambda q: lib.abs_blocks_workspace_size(lib.make_config(q), lib.make_blocks(q["blocks"]))
+    assert 0 < size(p) < size(dict(p, N=8)) < size(dict(p, N=8, tau_cap=12))
+    for s in (sim, plain):
+        s.close()

@@ -1,6 +1,7 @@
 """Seeded dataset / initial-weight generators for the presets.
 
 Linear least squares: X ~ N(0,1), w* ~ N(0,1), y = X w* + N(0, 0.01^2), w0 = 0.
+Residual blocks: gamma_l = 1, beta_l = 0 before W_l.
 Classification: a Gaussian mixture, class means ~ N(0, I), unit variance,
 labels uniform; softmax starts from w0 = 0, MLP and CNN weights W_l ~ N(0, 2/fan_in), b = 0.
 bf16 datasets are the fp32 draw rounded to nearest-even and handed over as the
@@ -66,6 +67,8 @@ def make_inputs(p: dict):
     else:
         parts = []
         for l in range(len(dims) - 1):
+            if p.get("blocks") and l:                # residual blocks: gamma = 1, beta = 0 in front of W_l
+                parts += [np.ones(dims[l], dtype=np.float32), np.zeros(dims[l], dtype=np.float32)]
             W = irng.standard_normal((dims[l], dims[l + 1]), dtype=np.float32)
             W *= np.float32(np.sqrt(2.0 / dims[l]))
             parts += [W.ravel(), np.zeros(dims[l + 1], dtype=np.float32)]

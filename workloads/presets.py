@@ -77,8 +77,20 @@ def scaled_preset(i: int, **over) -> dict:
     return p
 
 
+def with_blocks(p: dict, groups: int = 32, act: int = 2, residual: int = 1, drop: int = 6554, eps: float = 1e-5) -> dict:
+    """An MLP workload whose hidden layers are residual blocks: group normalisation in `groups` groups, activation
+    (0 none, 1 relu, 2 silu, 3 gelu), dropout (`drop` in 65536ths), product, residual."""
+    if p["model"] != MODEL_MLP:
+        raise ValueError("blocks are for the MLP workloads")
+    q = copy.deepcopy(p)
+    q["blocks"] = dict(groups=groups, act=act, residual=residual, drop=drop, eps=eps)
+    return q
+
+
 def param_count(p: dict) -> int:
     d = p["dims"]
+    if p.get("blocks"):
+        return sum(d[l] * d[l + 1] + d[l + 1] + (2 * d[l] if l else 0) for l in range(len(d) - 1))
     if p["model"] == MODEL_LINEAR:
         return d[0]
     if p["model"] == MODEL_CNN:
