@@ -36,7 +36,8 @@ struct NormArgs {
   int PP;                                                // positions of a part
   uint32_t work;                                         // workgroup's shares: (samples / samples of a workgroup) x parts x chunks
   float* part;                                           // [n][G][parts][2]: mean and squared distances, or the two sums
-  float* rows;                                           // backward: [row_count][2][C] shares of dgamma, dbeta
+  float *rows_g, *rows_b;                                // backward: [row_count] shares of dgamma, dbeta, row_step floats apart (one share: theirs)
+  int64_t row_step;
   uint32_t row_count;
 };
 
@@ -448,7 +449,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
       }
     }
   }
-  if (!a.rows) return;
+  if (!a.rows_g) return;
   // the lanes that share a channel: positions and samples of the workgroup
   const int t = threadIdx.x, lanes = min(a.TX, 64), stack = blockDim.x / (a.TX > 64 ? a.TX : 64);
   if (CV == 1) {
@@ -480,13 +481,13 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     if (t >= a.TX) return;
   }
   if (g < a.G) {
-    float* o = a.rows + (int64_t)row * 2 * a.C + g * a.per;
+    const int64_t o = (int64_t)row * a.row_step + g * a.per;
 #pragma unroll
     for (int j = 0; j < CV; ++j)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const int s = q.slot + j * a.SP;
-        if (s < a.slots) { o[s * V + e] = sg[j * V + e]; o[a.C + s * V + e] = sb[j * V + e]; }
+        if (s < a.slots) { a.rows_g[o + s * V + e] = sg[j * V + e]; a.rows_b[o + s * V + e] = sb[j * V + e]; }
       }
   }
 }
@@ -634,8 +635,8 @@ __global__ __launch_bounds__(256) void norm_plain_share_kernel(NormArgs<T> a) {
       const float dh = op_widen(a.dy[at * a.lddy + c]) * op_act_slope(norm_h(xh, gam, bet), a.act);
       sg += dh * xh; sb += dh;
     }
-    a.rows[(int64_t)r * 2 * a.C + c] = sg;
-    a.rows[(int64_t)r * 2 * a.C + a.C + c] = sb;
+    a.rows_g[(int64_t)r * a.row_step + c] = sg;
+    a.rows_b[(int64_t)r * a.row_step + c] = sb;
   }
 }
 
@@ -732,7 +733,9 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
       // as many workgroups as the CUs hold at once (1024 lanes each by their registers); a workgroup per share where a share has
       // so many positions that its two numbers per channel do not count
       const uint32_t fill = std::max(1u, 256u * (1024u / (uint32_t)q.threads) / q.chunks), all = q.work / q.chunks;
-      q.row_count = std::min((int64_t)q.threads / q.D * q.PL * q.NP >= 64 && all <= 4096 ? all : std::min(all, fill), all);
+      q.row_count = (int64_t)q.threads / q.D * q.PL * q.NP >= 64 && all <= 4096 ? all : std::min(all, fill);
+      // little work is one workgroup's per chunk: its sums are dgamma and dbeta, and the launch that adds shares is spared
+      if (!q.split && all <= 4) q.row_count = 1;
       q.blocks = q.row_count * q.chunks;
     } else {
       q.blocks = std::min(q.work, 1u << 20);
@@ -740,7 +743,7 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
     if (q.split) o = op_round_up((size_t)p.n * p.groups * q.parts * 8, 256);
   }
   q.off_rows = o;
-  if (backward) o += op_round_up((size_t)std::max(q.row_count, 1u) * 2 * p.channels * 4, 256);
+  if (backward && q.row_count > 1) o += op_round_up((size_t)q.row_count * 2 * p.channels * 4, 256);
   q.bytes = o;
   return q;
 }
@@ -803,7 +806,7 @@ template <typename T, int V>
 hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
   const dim3 grid(q.blocks), block((unsigned)q.threads);
   const int stack = q.threads / std::max(q.TX, 64);
-  const size_t lds = a.rows && q.CV == 1 && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;     // 32 KB at most
+  const size_t lds = a.rows_g && q.CV == 1 && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;     // 32 KB at most
   if constexpr (V == 1) {
     if (q.CV == kWide) { norm_backward_kernel<T, 1, 1, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
   }
@@ -827,11 +830,16 @@ template <typename T>
 hipError_t norm_run(const abs_group_norm& p, bool backward, NormArgs<T> a, const NormPlan& q, char* ws, float* dgamma, float* dbeta,
                     hipStream_t s) {
   norm_fill(a, p, q, ws);
-  a.rows = backward && dgamma ? (float*)(ws + q.off_rows) : nullptr;
+  if (backward && dgamma) {
+    const bool one = q.row_count == 1;
+    a.rows_g = one ? dgamma : (float*)(ws + q.off_rows);
+    a.rows_b = one ? dbeta : a.rows_g + p.channels;
+    a.row_step = 2 * (int64_t)p.channels;
+  }
   hipError_t e = hipSuccess;
   if (q.plain) {
     if (backward) {
-      if (a.rows) {
+      if (a.rows_g) {
         norm_plain_share_kernel<T><<<dim3((unsigned)((p.channels + 255) / 256), q.row_count), 256, 0, s>>>(a);
         e = hipGetLastError();
       }
@@ -850,8 +858,8 @@ hipError_t norm_run(const abs_group_norm& p, bool backward, NormArgs<T> a, const
       default: e = backward ? norm_backward_v<T, 1>(a, q, s) : norm_forward_v<T, 1>(a, q, s); break;
     }
   }
-  if (e == hipSuccess && a.rows) {
-    norm_share_sum_kernel<<<dim3((unsigned)((p.channels + 31) / 32), 2), 1024, 0, s>>>(a.rows, q.row_count, p.channels, dgamma, dbeta);
+  if (e == hipSuccess && a.rows_g && q.row_count > 1) {
+    norm_share_sum_kernel<<<dim3((unsigned)((p.channels + 31) / 32), 2), 1024, 0, s>>>(a.rows_g, q.row_count, p.channels, dgamma, dbeta);
     e = hipGetLastError();
   }
   return e;

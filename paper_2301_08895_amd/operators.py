@@ -58,9 +58,9 @@ def _pitch(t, what: str, shape, dtype, dev: int) -> int:
         _bad(f"{what} must be a tensor of x's device and dtype")
     if t.shape != shape:
         _bad(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    cols = shape[-1]
     if t.is_contiguous():
-        return cols
+        return shape[-1]
+    cols = shape[-1]
     stride = t.stride()
     if cols > 1 and stride[-1] != 1:
         _bad(f"{what}: the elements of a row must be neighbours")
@@ -97,6 +97,11 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _like(x, shape):
+    """A dense tensor of that shape, of x's dtype and device."""
+    return _empty_like(x) if x.is_contiguous() and x.shape == shape else x.new_empty(shape)
+
+
 def _workspace(n: int, device):
     """(tensor that holds the bytes, 256-byte aligned address)."""
     if n == 0:
@@ -117,14 +122,17 @@ def _run(dev: int, fn, *args):
 def _layer(x, w, act):
     """What both passes of a layer say about x and w: (struct, device, d_in, d_out, shape of y)."""
     code, dev = _first(x, "x", 1)
-    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[0] != x.shape[-1]:
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
         _bad("linear: w must be [d_in, d_out] and x [..., d_in]")
-    d_in, d_out = w.shape
+    xs, ws = x.shape, w.shape
+    d_in, d_out = ws
+    if xs[-1] != d_in:
+        _bad("linear: w must be [d_in, d_out] and x [..., d_in]")
     if not 1 <= d_in <= 1 << 20 or not 1 <= d_out <= 1 << 20:
         _bad("linear: d_in and d_out must be in [1, 2^20]")
-    p = AbsLinear(code, _whole(act, 0, 3, "act"), x.numel() // d_in, d_in, d_out,
-                  _pitch(x, "x", x.shape, x.dtype, dev), _pitch(w, "w", w.shape, x.dtype, dev))
-    return p, dev, d_in, d_out, (x.shape[:-1] + (d_out,) if x.dim() > 1 else torch.Size((d_out,)))
+    shape = (xs[0], d_out) if len(xs) == 2 else tuple(xs[:-1]) + (d_out,)
+    return AbsLinear(code, _whole(act, 0, 3, "act"), x.numel() // d_in, d_in, d_out, _pitch(x, "x", xs, x.dtype, dev),
+                     _pitch(w, "w", ws, x.dtype, dev)), dev, d_in, d_out, shape
 
 
 def linear_forward(x, w, b=None, *, act=ACT_NONE, residual=None, keep_z=False, out=None):
@@ -135,10 +143,10 @@ def linear_forward(x, w, b=None, *, act=ACT_NONE, residual=None, keep_z=False, o
     if residual is not None:
         p.ldr = _pitch(residual, "residual", shape, x.dtype, dev)
     if out is None:
-        y, p.ldy = _empty(shape, dtype=x.dtype, device=x.device), d_out
+        y, p.ldy = _like(x, shape), d_out
     else:
         y, p.ldy = out, _pitch(out, "out", shape, x.dtype, dev)
-    z = _empty(shape, dtype=x.dtype, device=x.device) if keep_z else None
+    z = _like(x, shape) if keep_z else None
     p.ldz = d_out
     xp, wp, ref = x.data_ptr(), w.data_ptr(), _byref(p)
     n = _lib.abs_linear_workspace_size(ref, 0, (xp | wp) & 15 == 0)
@@ -158,8 +166,8 @@ def linear_backward(x, w, dy, *, act=ACT_NONE, z=None, need_dx=True, need_dw=Tru
         _bad("linear: the backward pass of an activation needs z")
     else:
         p.ldz = _pitch(z, "z", shape, x.dtype, dev)
-    dx = _empty(x.shape, dtype=x.dtype, device=x.device) if need_dx else None
-    dw = _empty(w.shape, dtype=x.dtype, device=x.device) if need_dw else None
+    dx = _like(x, x.shape) if need_dx else None
+    dw = _like(w, w.shape) if need_dw else None
     db = _empty((d_out,), dtype=torch.float32, device=x.device) if need_db else None
     p.lddx, p.lddw = d_in, d_out
     xp, wp, dp, ref = x.data_ptr(), w.data_ptr(), dy.data_ptr(), _byref(p)
@@ -190,7 +198,7 @@ def group_norm_forward(x, gamma, beta, groups, *, eps=1e-5, act=ACT_NONE, out=No
     [n, groups].  x [n, ..., channels]; gamma, beta float32 [channels] or both None; out may be x."""
     p, dev, gp, bp = _normed(x, gamma, beta, groups, eps, act)
     if out is None:
-        y, p.ldy = _empty(x.shape, dtype=x.dtype, device=x.device), p.channels
+        y, p.ldy = _like(x, x.shape), p.channels
     else:
         y, p.ldy = out, _pitch(out, "out", x.shape, x.dtype, dev)
     ref = _byref(p)
@@ -214,12 +222,12 @@ def group_norm_backward(x, gamma, beta, mean, rstd, dy, *, act=ACT_NONE, residua
     if residual is not None:
         p.lddres = _pitch(residual, "residual", x.shape, x.dtype, dev)
     if out is None:
-        dx, p.lddx = _empty(x.shape, dtype=x.dtype, device=x.device), p.channels
+        dx, p.lddx = _like(x, x.shape), p.channels
     else:
         dx, p.lddx = out, _pitch(out, "out", x.shape, x.dtype, dev)
     dgamma = dbeta = None
     if need_dgamma:
-        dgamma = _empty((p.channels,), dtype=torch.float32, device=x.device)
+        dgamma = _empty_like(gamma) if gamma is not None else _empty((p.channels,), dtype=torch.float32, device=x.device)
         dbeta = _empty_like(dgamma)
     ref = _byref(p)
     n = _lib.abs_group_norm_workspace_size(ref, 1)
@@ -234,10 +242,11 @@ _WORD = 2 ** 64 - 1
 
 def _dropped(x, drop, seed, offset):
     code, dev = _first(x, "x", 1)
-    cols = x.shape[-1]
+    shape = x.shape
+    cols = shape[-1]
     if cols < 1:
         _bad("dropout: x must be [..., cols]")
-    pitch = _pitch(x, "x", x.shape, x.dtype, dev)
+    pitch = _pitch(x, "x", shape, x.dtype, dev)
     return AbsDropout(code, _whole(drop, 0, 65535, "drop"), x.numel() // cols, cols, pitch, cols, cols, seed & _WORD, offset & _WORD), dev
 
 
@@ -250,7 +259,7 @@ def dropout_forward(x, drop, seed, offset, *, residual=None, out=None):
     if residual is not None:
         p.ldr, rp = _pitch(residual, "residual", x.shape, x.dtype, dev), residual.data_ptr()
     if out is None:
-        out = _empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _like(x, x.shape)
     else:
         p.ldy = _pitch(out, "out", x.shape, x.dtype, dev)
     _run(dev, _lib.abs_dropout_forward, _byref(p), x.data_ptr(), rp, out.data_ptr())
@@ -261,7 +270,7 @@ def dropout_backward(dy, drop, seed, offset, *, out=None):
     """dx for a gradient dy of dropout_forward's y (the residual's gradient is dy); out may be dy."""
     p, dev = _dropped(dy, drop, seed, offset)
     if out is None:
-        out = _empty(dy.shape, dtype=dy.dtype, device=dy.device)
+        out = _like(dy, dy.shape)
     else:
         p.ldy = _pitch(out, "out", dy.shape, dy.dtype, dev)
     _run(dev, _lib.abs_dropout_backward, _byref(p), dy.data_ptr(), out.data_ptr())

@@ -105,11 +105,12 @@ def test_group_norm_refuses_pointers_and_pitches():
     assert f(C.byref(ok), P, P, P, P + 1, P, P, P, big, None) == -1
     assert f(C.byref(ok), P, P + 2, P, P, P, P, P, big, None) == -1
     assert f(C.byref(_norm(ldy=7)), P, P, P, P, P, P, P, big, None) == -1
-    need = _lib.abs_group_norm_workspace_size(C.byref(ok), 1)
+    many = _norm(n=5000)
+    need = _lib.abs_group_norm_workspace_size(C.byref(many), 1)
     assert need > 0
     args = lambda p, at, n, dres=None: (C.byref(p), P, P, P, P, P, P, dres, P, P, P, at, n, None)
-    assert b(*args(ok, P, need - 1)) == -2
-    assert b(*args(ok, None, need)) == -1
+    assert b(*args(many, P, need - 1)) == -2
+    assert b(*args(many, None, need)) == -1
     assert b(*args(_norm(lddres=7), P, big, P)) == -1
     assert b(*args(_norm(lddy=7), P, big)) == -1
     assert b(*args(_norm(lddx=7), P, big)) == -1
