@@ -321,14 +321,14 @@ __device__ __forceinline__ bf16x8_t big_fragment(const uint16_t* half, int w, in
   return *(const bf16x8_t*)(half + row * 64 + ((((s << 2) | lk) ^ ((lr >> 1) & 7)) << 3));
 }
 
+// `block`: this workgroup's number among the product's
 template <bool ATR, bool BTR>
-__global__ __launch_bounds__(512, 1) void linear_big_kernel(GemmArgs<uint16_t> g) {
-  __shared__ __attribute__((aligned(1024))) uint16_t smem[8 * kHalf];          // [stage][A0 A1], then [stage][B0 B1]
+__device__ __forceinline__ void big_product(const GemmArgs<uint16_t>& g, int block, uint16_t* smem) {   // [stage][A0 A1], then [stage][B0 B1]
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 2, wn = wave & 3;
   const int total = g.mt * g.nt * g.nsplit, per = (total + 7) / 8;
-  const int id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
-  if (((int)blockIdx.x >> 3) >= per || id >= total) return;
+  const int id = (block & 7) * per + (block >> 3);
+  if ((block >> 3) >= per || id >= total) return;
   const int split = id / (g.mt * g.nt), tile = id - split * (g.mt * g.nt);
   const int64_t m0 = (int64_t)(tile / g.nt) * kBig, n0 = (int64_t)(tile % g.nt) * kBig;
   const int64_t k0 = (int64_t)split * g.steps_per_split * 64;
@@ -427,6 +427,20 @@ __global__ __launch_bounds__(512, 1) void linear_big_kernel(GemmArgs<uint16_t> g
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+constexpr int kBigLds = 8 * kHalf;
+template <bool ATR, bool BTR>
+__global__ __launch_bounds__(512, 1) void linear_big_kernel(GemmArgs<uint16_t> g) {
+  __shared__ __attribute__((aligned(1024))) uint16_t smem[kBigLds];
+  big_product<ATR, BTR>(g, blockIdx.x, smem);
+}
+// dW and dx of one layer side by side: with the longer contraction cut so that all CUs get as many k-steps, they leave fewer shares
+// and fewer CUs idle than one after the other.  The longer runs come first.
+__global__ __launch_bounds__(512, 1) void linear_big_pair_kernel(GemmArgs<uint16_t> dw, GemmArgs<uint16_t> dx, int dw_blocks) {
+  __shared__ __attribute__((aligned(1024))) uint16_t smem[kBigLds];
+  if ((int)blockIdx.x < dw_blocks) big_product<true, true>(dw, blockIdx.x, smem);
+  else big_product<false, false>(dx, (int)blockIdx.x - dw_blocks, smem);
 }
 
 // ---------------------------------------------------------------------- shares of the contraction, added in their order
@@ -932,15 +946,41 @@ bool small_product(const abs_linear& p, bool backward) {
   return backward ? macs <= (half ? 1.1e9 : 8e8) && (double)p.d_in * p.d_out <= 4.3e6 : macs <= (half ? 2.2e9 : 9e8);
 }
 
+// dx and dW on large tiles in one launch (see linear_big_pair_kernel); false where the tiles would be mostly empty or too few
+bool plan_pair(const abs_linear& p, Product& dx, Product& dw) {
+  if (p.dtype != ABS_X_BF16) return false;
+  auto tiles = [](Product& q, int64_t M, int64_t N) {
+    q.mt = (int)((M + kBig - 1) / kBig);
+    q.nt = (int)((N + kBig - 1) / kBig);
+    return (double)M * (double)N >= 0.7 * (double)q.mt * q.nt * kBig * kBig;
+  };
+  Product a{}, b{};
+  if (!tiles(a, p.rows, p.d_in) || !tiles(b, p.d_in, p.d_out)) return false;
+  const int64_t ka = (p.d_out + 63) / 64, kb = (p.rows + 63) / 64, work = (int64_t)a.mt * a.nt * ka + (int64_t)b.mt * b.nt * kb;
+  const int64_t each = (work + 255) / 256;                       // k-steps per CU
+  if (each < 24) return false;
+  auto cut = [&](Product& q, int64_t M, int64_t N, int64_t steps) {
+    const int64_t split = std::min<int64_t>((steps + each - 1) / each, 16);
+    q.big = true;
+    q.steps_per_split = (int)((steps + split - 1) / split);
+    q.nsplit = (int)((steps + q.steps_per_split - 1) / q.steps_per_split);
+    if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
+  };
+  cut(a, p.rows, p.d_in, ka);
+  cut(b, p.d_in, p.d_out, kb);
+  dx = a; dw = b;
+  return true;
+}
+
 struct SmallProduct { int nt, tiles, splits, steps; size_t part_bytes; };
 
 struct LinearPlan {
-  bool small, pack_x, pack_w, dz;
+  bool small, pair, pack_x, pack_w, dz;
   int sum_rows;
   SmallProduct sa, sb;                        // the forward product or dx; dW
-  Product fwd, dx, dw;
+  Product fwd, dx, dw, pair_dx, pair_dw;
   int64_t in8, out8;                          // d_in, d_out in whole pieces
-  size_t off_x, off_w, off_dz, off_sums, off_part, bytes;
+  size_t off_x, off_w, off_dz, off_sums, off_part, off_part2, bytes;
 };
 
 // aligned: the pointers are; need_copy of x / w and, for the backward pass, of dy into dz
@@ -997,6 +1037,14 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     q.dx = plan_product(p.rows, p.d_in, p.d_out, p.dtype);
     q.dw = plan_product(p.d_in, p.d_out, p.rows, p.dtype);
     q.off_part = take(std::max(q.dx.part_bytes, q.dw.part_bytes));
+    q.off_part2 = q.off_part;
+    Product a, b;
+    if (plan_pair(p, a, b)) {                 // (used where both are asked for)
+      q.pair = true;
+      q.pair_dx = a; q.pair_dw = b;
+      q.off_part2 = q.off_part + op_round_up(b.part_bytes, 256);
+      o = std::max(o, op_round_up(q.off_part2 + a.part_bytes, 256));
+    }
   }
   q.bytes = o;
   return q;
@@ -1033,26 +1081,28 @@ hipError_t launch_join(const Join<T>& a, const Join<T>& b, hipStream_t s) {
   return hipGetLastError();
 }
 
+// g with the plan's tiles and, where its contraction is cut, shares that go to `part` and join into what g wanted
+template <typename T>
+Join<T> set_product(const Product& q, GemmArgs<T>& g, float* part) {
+  g.mt = q.mt; g.nt = q.nt; g.nsplit = q.nsplit; g.steps_per_split = q.steps_per_split;
+  if (q.nsplit == 1) return Join<T>{};
+  g.e.ldpart = (int64_t)op_round_up(g.N, 4);
+  g.e.part_stride = g.M * g.e.ldpart;
+  g.e.part = part;
+  return Join<T>{g.e, g.M, g.N, q.nsplit, nullptr, nullptr};
+}
+int product_blocks(const Product& q) { return (q.mt * q.nt * q.nsplit + 7) / 8 * 8; }
+
 template <typename T, bool ATR, bool BTR>
 hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, hipStream_t s) {
-  g.mt = q.mt; g.nt = q.nt; g.nsplit = q.nsplit; g.steps_per_split = q.steps_per_split;
-  const int total = q.mt * q.nt * q.nsplit;
-  Epilogue<T> join = g.e;
-  join.ldpart = (int64_t)op_round_up(g.N, 4);
-  join.part_stride = g.M * join.ldpart;
-  join.part = part;
-  if (q.nsplit > 1) g.e = join;
-  else g.e.part = nullptr;
-  const dim3 grid((unsigned)((total + 7) / 8 * 8));
+  const Join<T> join = set_product(q, g, part);
+  const dim3 grid((unsigned)product_blocks(q));
   if (q.big) {
     if constexpr (sizeof(T) == 2) linear_big_kernel<ATR, BTR><<<grid, 512, 0, s>>>(g);
-  } else if (total > 256) linear_tile_kernel<T, ATR, BTR, 2><<<grid, 256, 0, s>>>(g);
+  } else if (q.mt * q.nt * q.nsplit > 256) linear_tile_kernel<T, ATR, BTR, 2><<<grid, 256, 0, s>>>(g);
   else linear_tile_kernel<T, ATR, BTR, 4><<<grid, 256, 0, s>>>(g);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && q.nsplit > 1) {
-    e = launch_join(Join<T>{join, g.M, g.N, q.nsplit, nullptr, nullptr}, Join<T>{}, s);
-  }
-  return e;
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess && join.shares ? launch_join(join, Join<T>{}, s) : e;
 }
 
 template <typename T>
@@ -1150,22 +1200,31 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     if (out) { dz = out; lddz = q.out8; }
   }
   float* part = (float*)(ws + q.off_part);
+  GemmArgs<T> ga{}, gb{};
   if (err == hipSuccess && dx) {
-    GemmArgs<T> g{};
-    g.A = dz; g.lda = lddz; g.B = (const T*)w; g.ldb = p.ldw;
-    if (q.pack_w) { g.B = (const T*)(ws + q.off_w); g.ldb = q.out8; err = pack<T>(w, p.ldw, p.d_in, p.d_out, ws + q.off_w, q.out8, s); }
-    g.M = p.rows; g.N = p.d_in; g.K = p.d_out;
-    g.e.y = (T*)dx; g.e.ldy = p.lddx;
-    if (err == hipSuccess) err = run_product<T, false, false>(q.dx, g, part, s);
+    ga.A = dz; ga.lda = lddz; ga.B = (const T*)w; ga.ldb = p.ldw;
+    if (q.pack_w) { ga.B = (const T*)(ws + q.off_w); ga.ldb = q.out8; err = pack<T>(w, p.ldw, p.d_in, p.d_out, ws + q.off_w, q.out8, s); }
+    ga.M = p.rows; ga.N = p.d_in; ga.K = p.d_out;
+    ga.e.y = (T*)dx; ga.e.ldy = p.lddx;
   }
   if (err == hipSuccess && dw) {
-    GemmArgs<T> g{};
-    g.A = (const T*)x; g.lda = p.ldx; g.B = dz; g.ldb = lddz;
-    if (q.pack_x) { g.A = (const T*)(ws + q.off_x); g.lda = q.in8; err = pack<T>(x, p.ldx, p.rows, p.d_in, ws + q.off_x, q.in8, s); }
-    g.M = p.d_in; g.N = p.d_out; g.K = p.rows; g.mc = q.in8; g.nc = q.out8;
-    g.e.y = (T*)dw; g.e.ldy = p.lddw;
-    if (err == hipSuccess) err = run_product<T, true, true>(q.dw, g, part, s);
+    gb.A = (const T*)x; gb.lda = p.ldx; gb.B = dz; gb.ldb = lddz;
+    if (q.pack_x) { gb.A = (const T*)(ws + q.off_x); gb.lda = q.in8; err = pack<T>(x, p.ldx, p.rows, p.d_in, ws + q.off_x, q.in8, s); }
+    gb.M = p.d_in; gb.N = p.d_out; gb.K = p.rows; gb.mc = q.in8; gb.nc = q.out8;
+    gb.e.y = (T*)dw; gb.e.ldy = p.lddw;
   }
+  if (err != hipSuccess) return err;
+  if constexpr (sizeof(T) == 2) {
+    if (q.pair && dx && dw) {
+      const Join<T> jb = set_product(q.pair_dw, gb, part), ja = set_product(q.pair_dx, ga, (float*)(ws + q.off_part2));
+      const int first = product_blocks(q.pair_dw);
+      linear_big_pair_kernel<<<dim3((unsigned)(first + product_blocks(q.pair_dx))), 512, 0, s>>>(gb, ga, first);
+      err = hipGetLastError();
+      return err == hipSuccess && (ja.shares || jb.shares) ? launch_join(ja, jb, s) : err;
+    }
+  }
+  if (dx) err = run_product<T, false, false>(q.dx, ga, part, s);
+  if (err == hipSuccess && dw) err = run_product<T, true, true>(q.dw, gb, part, s);
   return err;
 }
 
