@@ -7,6 +7,7 @@
 #include "operators.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace abs_impl {
 namespace {
@@ -171,16 +172,18 @@ __device__ __forceinline__ f32x16_t multiply(f32x4_t a, f32x4_t b, f32x16_t c) {
   return c;
 }
 
+template <typename T> constexpr int kTileOperand = kTile * kStep<T>;       // elements of an operand's step (16 KB)
+
+// `block`: this workgroup's number among the product's
 template <typename T, bool ATR, bool BTR, int RING>
-__global__ __launch_bounds__(256, RING <= 2 ? 2 : 1) void linear_tile_kernel(GemmArgs<T> g) {
-  constexpr int kOperand = kTile * kStep<T>;                // elements of an operand's step (16 KB)
-  __shared__ __attribute__((aligned(1024))) T smem[RING * 2 * kOperand];
+__device__ __forceinline__ void tile_product(const GemmArgs<T>& g, int block, T* smem) {
+  constexpr int kOperand = kTileOperand<T>;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   // workgroups go round the eight XCDs: each takes a run of neighbouring tiles, columns fastest
   const int total = g.mt * g.nt * g.nsplit, per = (total + 7) / 8;
-  const int id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
-  if (((int)blockIdx.x >> 3) >= per || id >= total) return;
+  const int id = (block & 7) * per + (block >> 3);
+  if ((block >> 3) >= per || id >= total) return;
   const int split = id / (g.mt * g.nt), tile = id - split * (g.mt * g.nt);
   const int64_t m0 = (int64_t)(tile / g.nt) * kTile, n0 = (int64_t)(tile % g.nt) * kTile;
   const int64_t k0 = (int64_t)split * g.steps_per_split * kStep<T>;
@@ -430,12 +433,24 @@ __device__ __forceinline__ void big_product(const GemmArgs<uint16_t>& g, int blo
 }
 
 constexpr int kBigLds = 8 * kHalf;
+template <typename T, bool ATR, bool BTR, int RING>
+__global__ __launch_bounds__(256, RING <= 2 ? 2 : 1) void linear_tile_kernel(GemmArgs<T> g) {
+  __shared__ __attribute__((aligned(1024))) T smem[RING * 2 * kTileOperand<T>];
+  tile_product<T, ATR, BTR, RING>(g, blockIdx.x, smem);
+}
+// dW and dx of one layer side by side, two workgroups of either on a CU
+template <typename T>
+__global__ __launch_bounds__(256, 2) void linear_tile_pair_kernel(GemmArgs<T> dw, GemmArgs<T> dx, int dw_blocks) {
+  __shared__ __attribute__((aligned(1024))) T smem[2 * 2 * kTileOperand<T>];
+  if ((int)blockIdx.x < dw_blocks) tile_product<T, true, true, 2>(dw, blockIdx.x, smem);
+  else tile_product<T, false, false, 2>(dx, (int)blockIdx.x - dw_blocks, smem);
+}
 template <bool ATR, bool BTR>
 __global__ __launch_bounds__(512, 1) void linear_big_kernel(GemmArgs<uint16_t> g) {
   __shared__ __attribute__((aligned(1024))) uint16_t smem[kBigLds];
   big_product<ATR, BTR>(g, blockIdx.x, smem);
 }
-// dW and dx of one layer side by side: with the longer contraction cut so that all CUs get as many k-steps, they leave fewer shares
+// The same on large tiles: with the longer contraction cut so that all CUs get as many k-steps, they leave fewer shares
 // and fewer CUs idle than one after the other.  The longer runs come first.
 __global__ __launch_bounds__(512, 1) void linear_big_pair_kernel(GemmArgs<uint16_t> dw, GemmArgs<uint16_t> dx, int dw_blocks) {
   __shared__ __attribute__((aligned(1024))) uint16_t smem[kBigLds];
@@ -906,33 +921,79 @@ struct Product {                              // one product on a tile kernel
   int mt, nt, nsplit, steps_per_split;
   size_t part_bytes;
 };
-Product plan_product(int64_t M, int64_t N, int64_t K, int dtype) {
+// A product's plan is the cheapest by a model of what was measured (us; bf16, fp32 in brackets).  A k-step of 64 (32) takes a CU 1.4
+// on one large tile, 0.78 (2.2) on one 128 x 128 tile and 1.04 (4.1) on two of those at a time; a workgroup's start and end cost 12,
+// 5 (8) and 7 (8); shares cost a launch of 3 and their bytes, written and read, at 6 TB/s.  Model / measured: 8192 x 2048 x
+// 2048 57 / 62 large, 81 / 81 small tiles; 4096 x 2048 x 2048 57 / 54 and 40 / 41; 2048^3 30 / 30 in one run, 38 / 36 in two shares;
+// 256 x 4096 x 4096 26 / 25 in four; fp32 4096 x 1024 x 1024 78 / 78.
+struct TileCost { double start, step, start2, step2, big_start, big_step; };
+TileCost tile_cost(int dtype) { return dtype == ABS_X_BF16 ? TileCost{5, 0.78, 7, 1.04, 12, 1.4} : TileCost{8, 2.2, 8, 4.1, 0, 0}; }
+double join_cost(int64_t split, int64_t M, int64_t N) { return split > 1 ? 3 + (double)split * M * N * 8 / 6e6 : 0; }
+
+Product cut_product(int64_t M, int64_t N, int64_t K, int dtype, bool big, int64_t split) {
   Product q{};
-  const int step = dtype == ABS_X_BF16 ? 64 : 32;
-  if (dtype == ABS_X_BF16) {
-    q.mt = (int)((M + kBig - 1) / kBig);
-    q.nt = (int)((N + kBig - 1) / kBig);
-    const int64_t tiles = (int64_t)q.mt * q.nt, steps = (K + 63) / 64;
-    const int64_t split = tiles >= 192 ? 1 : std::max<int64_t>(1, std::min<int64_t>({8, 256 / tiles, steps / 8}));
-    // whole tiles for most CUs, and little of them beyond the result
-    if (tiles * split >= 192 && (double)M * (double)N >= 0.7 * (double)tiles * kBig * kBig) {
-      q.big = true;
-      q.steps_per_split = (int)((steps + split - 1) / split);
-      q.nsplit = (int)((steps + q.steps_per_split - 1) / q.steps_per_split);
-      if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
-      return q;
-    }
-  }
-  q.mt = (int)((M + kTile - 1) / kTile);
-  q.nt = (int)((N + kTile - 1) / kTile);
-  const int64_t tiles = (int64_t)q.mt * q.nt, steps = (K + step - 1) / step;
-  // few tiles: shares of the contraction, at least four k-steps each, until every CU has one
-  int64_t split = 1;
-  if (tiles < 256 && steps >= 8) split = std::max<int64_t>(1, std::min<int64_t>({16, 256 / tiles, steps / 4}));
+  const int tile = big ? kBig : kTile, step = dtype == ABS_X_BF16 ? 64 : 32;
+  q.big = big;
+  q.mt = (int)((M + tile - 1) / tile);
+  q.nt = (int)((N + tile - 1) / tile);
+  const int64_t steps = (K + step - 1) / step;
   q.steps_per_split = (int)((steps + split - 1) / split);
-  q.nsplit = std::max(1, (int)((steps + q.steps_per_split - 1) / q.steps_per_split));
+  q.nsplit = (int)((steps + q.steps_per_split - 1) / q.steps_per_split);
   if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
   return q;
+}
+constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16};
+
+Product plan_product(int64_t M, int64_t N, int64_t K, int dtype, double* cost_out) {
+  const TileCost c = tile_cost(dtype);
+  Product best{};
+  double least = 1e30;
+  for (int big = dtype == ABS_X_BF16 ? 1 : 0; big >= 0; --big)
+    for (int split : kCuts) {
+      const Product q = cut_product(M, N, K, dtype, big != 0, split);
+      if (q.nsplit != split || (split > 1 && q.steps_per_split < 4)) continue;
+      const double units = (double)q.mt * q.nt * q.nsplit, steps = q.steps_per_split;
+      const double us = (big ? std::ceil(units / 256) * (c.big_start + c.big_step * steps)
+                             : units <= 256 ? c.start + c.step * steps : std::ceil(units / 512) * (c.start2 + c.step2 * steps)) +
+                        join_cost(q.nsplit, M, N);
+      if (us < least) { least = us; best = q; }
+    }
+  if (cost_out) *cost_out = least;
+  return best;
+}
+
+// When the last of `nb` runs of tb us and then `na` of ta us ends, each taking the first of `slots` places that is free.
+double last_end(int64_t nb, double tb, int64_t na, double ta, int64_t slots) {
+  const int64_t each = nb / slots, more = nb % slots;             // `more` places take one more of the first kind
+  const double early = each * tb, late = early + (more ? tb : 0);
+  double end = late;
+  int64_t fit_early = 0, fit_late = 0;                            // runs of the second kind that places of either sort have taken
+  while (fit_early * (slots - more) + fit_late * more < na) {
+    const double e = early + (fit_early + 1) * ta, l = late + (fit_late + 1) * ta;
+    if (e <= l) ++fit_early; else ++fit_late;
+    end = std::max(end, std::min(e, l));
+  }
+  return end;
+}
+
+// dx and dW in one launch, or, where that is cheaper, one after the other (false).  Workgroups of both kinds share the CUs, dW's first,
+// a step costing 1.15 of what it does alone on large tiles.  Model / measured, bf16: 8192 x 2048 x 2048 127 / 128 (apart 139 / 160).
+bool plan_pair(const abs_linear& p, double apart, Product& dx, Product& dw) {
+  const TileCost c = tile_cost(p.dtype);
+  double least = apart + 3;                                       // (their two launches' gap)
+  bool found = false;
+  for (int big = p.dtype == ABS_X_BF16 ? 1 : 0; big >= 0; --big)
+    for (int sa : kCuts)
+      for (int sb : kCuts) {
+        const Product a = cut_product(p.rows, p.d_in, p.d_out, p.dtype, big != 0, sa), b = cut_product(p.d_in, p.d_out, p.rows, p.dtype, big != 0, sb);
+        if (a.nsplit != sa || b.nsplit != sb || (sa > 1 && a.steps_per_split < 4) || (sb > 1 && b.steps_per_split < 4)) continue;
+        const double start = big ? c.big_start : c.start2, step = big ? 1.15 * c.big_step : c.step2;
+        const double us = last_end((int64_t)b.mt * b.nt * sb, start + step * b.steps_per_split, (int64_t)a.mt * a.nt * sa,
+                                   start + step * a.steps_per_split, big ? 256 : 512) +
+                          std::max(join_cost(sa, p.rows, p.d_in), join_cost(sb, p.d_in, p.d_out));
+        if (us < least) { least = us; dx = a; dw = b; found = true; }
+      }
+  return found;
 }
 
 // Which products linear_small_kernel takes (us, it / the tile kernels with their copies, dz and joins; bf16 unless said).  Forward
@@ -944,32 +1005,6 @@ bool small_product(const abs_linear& p, bool backward) {
   const double macs = (double)p.rows * p.d_in * p.d_out;
   if (p.d_in < 2 || p.d_out < 2) return false;                       // (columns are read in pairs)
   return backward ? macs <= (half ? 1.1e9 : 8e8) && (double)p.d_in * p.d_out <= 4.3e6 : macs <= (half ? 2.2e9 : 9e8);
-}
-
-// dx and dW on large tiles in one launch (see linear_big_pair_kernel); false where the tiles would be mostly empty or too few
-bool plan_pair(const abs_linear& p, Product& dx, Product& dw) {
-  if (p.dtype != ABS_X_BF16) return false;
-  auto tiles = [](Product& q, int64_t M, int64_t N) {
-    q.mt = (int)((M + kBig - 1) / kBig);
-    q.nt = (int)((N + kBig - 1) / kBig);
-    return (double)M * (double)N >= 0.7 * (double)q.mt * q.nt * kBig * kBig;
-  };
-  Product a{}, b{};
-  if (!tiles(a, p.rows, p.d_in) || !tiles(b, p.d_in, p.d_out)) return false;
-  const int64_t ka = (p.d_out + 63) / 64, kb = (p.rows + 63) / 64, work = (int64_t)a.mt * a.nt * ka + (int64_t)b.mt * b.nt * kb;
-  const int64_t each = (work + 255) / 256;                       // k-steps per CU
-  if (each < 24) return false;
-  auto cut = [&](Product& q, int64_t M, int64_t N, int64_t steps) {
-    const int64_t split = std::min<int64_t>((steps + each - 1) / each, 16);
-    q.big = true;
-    q.steps_per_split = (int)((steps + split - 1) / split);
-    q.nsplit = (int)((steps + q.steps_per_split - 1) / q.steps_per_split);
-    if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
-  };
-  cut(a, p.rows, p.d_in, ka);
-  cut(b, p.d_in, p.d_out, kb);
-  dx = a; dw = b;
-  return true;
 }
 
 struct SmallProduct { int nt, tiles, splits, steps; size_t part_bytes; };
@@ -1021,7 +1056,7 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     q.pack_w = !w_whole;
     if (q.pack_x) q.off_x = take((size_t)p.rows * q.in8 * size);
     if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
-    q.fwd = plan_product(p.rows, p.d_out, p.d_in, p.dtype);
+    q.fwd = plan_product(p.rows, p.d_out, p.d_in, p.dtype, nullptr);
     q.off_part = take(q.fwd.part_bytes);
   } else {
     q.pack_x = !x_whole;
@@ -1034,12 +1069,13 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     const int cols = p.d_out % piece == 0 ? (p.d_out / piece + 31) / 32 : (p.d_out + 31) / 32;
     q.sum_rows = (int)std::max<int64_t>(1, std::min<int64_t>((p.rows + 15) / 16, std::max(1, 2048 / cols)));
     q.off_sums = take((size_t)q.sum_rows * p.d_out * 4);
-    q.dx = plan_product(p.rows, p.d_in, p.d_out, p.dtype);
-    q.dw = plan_product(p.d_in, p.d_out, p.rows, p.dtype);
+    double ca, cb;
+    q.dx = plan_product(p.rows, p.d_in, p.d_out, p.dtype, &ca);
+    q.dw = plan_product(p.d_in, p.d_out, p.rows, p.dtype, &cb);
     q.off_part = take(std::max(q.dx.part_bytes, q.dw.part_bytes));
     q.off_part2 = q.off_part;
     Product a, b;
-    if (plan_pair(p, a, b)) {                 // (used where both are asked for)
+    if (plan_pair(p, ca + cb, a, b)) {        // (used where both are asked for)
       q.pair = true;
       q.pair_dx = a; q.pair_dw = b;
       q.off_part2 = q.off_part + op_round_up(b.part_bytes, 256);
@@ -1214,14 +1250,14 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     gb.e.y = (T*)dw; gb.e.ldy = p.lddw;
   }
   if (err != hipSuccess) return err;
-  if constexpr (sizeof(T) == 2) {
-    if (q.pair && dx && dw) {
-      const Join<T> jb = set_product(q.pair_dw, gb, part), ja = set_product(q.pair_dx, ga, (float*)(ws + q.off_part2));
-      const int first = product_blocks(q.pair_dw);
-      linear_big_pair_kernel<<<dim3((unsigned)(first + product_blocks(q.pair_dx))), 512, 0, s>>>(gb, ga, first);
-      err = hipGetLastError();
-      return err == hipSuccess && (ja.shares || jb.shares) ? launch_join(ja, jb, s) : err;
-    }
+  if (q.pair && dx && dw) {
+    const Join<T> jb = set_product(q.pair_dw, gb, part), ja = set_product(q.pair_dx, ga, (float*)(ws + q.off_part2));
+    const int first = product_blocks(q.pair_dw);
+    const dim3 grid((unsigned)(first + product_blocks(q.pair_dx)));
+    if (!q.pair_dw.big) linear_tile_pair_kernel<T><<<grid, 256, 0, s>>>(gb, ga, first);
+    else if constexpr (sizeof(T) == 2) linear_big_pair_kernel<<<grid, 512, 0, s>>>(gb, ga, first);
+    err = hipGetLastError();
+    return err == hipSuccess && (ja.shares || jb.shares) ? launch_join(ja, jb, s) : err;
   }
   if (dx) err = run_product<T, false, false>(q.dx, ga, part, s);
   if (err == hipSuccess && dw) err = run_product<T, true, true>(q.dw, gb, part, s);
