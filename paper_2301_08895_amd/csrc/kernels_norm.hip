@@ -41,21 +41,13 @@ struct NormArgs {
   uint32_t row_count;
 };
 
-// The exact order of operations that defines h: three roundings, nothing contracted, so that a value at relu's corner is on the same
-// side in both passes.
-__device__ __forceinline__ float norm_xhat(float x, float mean, float rstd) {
-#pragma clang fp contract(off)
-  const float d = x - mean;
-  return d * rstd;
-}
-__device__ __forceinline__ float norm_h(float xhat, float gamma, float beta) {
-#pragma clang fp contract(off)
-  const float s = xhat * gamma;
-  return s + beta;
-}
+// h = gamma rstd (x - mean) + beta, of the distance d = x - mean and s = gamma rstd: the same three roundings everywhere, so that a
+// value at relu's corner is on the same side in every pass.
+__device__ __forceinline__ float norm_h(float d, float s, float beta) { return fmaf(d, s, beta); }
 
 // v + v of the lane whose number differs in bit OFF; kFlat: the lanes that differ in lower bits hold equal values already, so a
-// mirror image does.  Cross-lane adds where there are such, LDS's swizzle (no addresses) for the others.
+// mirror image does.  Cross-lane adds where there are such, swaps of rows or halves (which need no address either) and LDS's swizzle for
+// the others.
 template <int OFF, bool kFlat>
 __device__ __forceinline__ float add_xor(float v) {
 #define ABS_DPP(ctrl_) v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl_, 0xF, 0xF, true))
@@ -63,8 +55,13 @@ __device__ __forceinline__ float add_xor(float v) {
   else if constexpr (OFF == 2) return ABS_DPP(0x4E);                   // quad_perm [2, 3, 0, 1]
   else if constexpr (OFF == 4 && kFlat) return ABS_DPP(0x141);         // row_half_mirror
   else if constexpr (OFF == 8 && kFlat) return ABS_DPP(0x140);         // row_mirror
-  else if constexpr (OFF < 32) return v + __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), (OFF << 10) | 0x1F));
-  else return v + __shfl_xor(v, 32);
+  else if constexpr (OFF < 16) return v + __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), (OFF << 10) | 0x1F));
+  else {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const unsigned u = (unsigned)__float_as_int(v);
+    const u32x2 r = OFF == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(r.x) + __uint_as_float(r.y);                // (even and odd rows, or the halves)
+  }
 #undef ABS_DPP
 }
 // ... over all bits that are set in `bits` (uniform)
@@ -104,6 +101,12 @@ __device__ __forceinline__ float group_sum(float v, int SP, int TX, int D, float
 // Where a thread stands: its sample inside the workgroup, positions p, p + PL, ..., group and piece.
 struct Place {
   int sb, p, g, slot;
+  // how many of the lane's positions p, p + PL, ... lie below `positions`; none for a lane behind the group's pieces (the comparison of a
+  // constant with this number is all that a piece costs: PL is a power of two, and positions kept for it would each take a register)
+  template <typename A>
+  __device__ __forceinline__ int pieces(int positions, const A& a) const {
+    return p < positions && slot < a.slots ? ((positions - p - 1) >> (31 - __builtin_clz(a.PL))) + 1 : 0;
+  }
 };
 template <typename T>
 __device__ __forceinline__ Place place_of(const NormArgs<T>& a) {
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
     const int g = (int)chunk * a.gpc + q.g;
     const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
     const bool live = i < a.n && g < a.G;
-    const int have = live ? count_pos : 0;                             // positions of this lane's sample
+    const int count = live ? q.pieces(count_pos, a) : 0;               // of this lane
     const int64_t col0 = (int64_t)chunk * a.gpc * a.per;
     const char* const src = (const char*)(a.x + (i0 * a.S + pos0) * a.ldx + col0);
     const uint32_t lane_col = (uint32_t)(q.g * a.per + q.slot * V);
@@ -156,31 +159,31 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
       for (int k = 0; k < NP; ++k) {
 #pragma unroll
         for (int j = 0; j < CV; ++j)
-          if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) v[k * CV + j].load(src + (off + (uint32_t)(j * a.SP * V * (int)sizeof(T))));
+          if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) v[k * CV + j].load(src + (off + (uint32_t)(j * a.SP * V * (int)sizeof(T))));
         off += step;
         asm volatile("" : "+v"(off));
       }
     }
-    const float count = (float)count_pos * (float)a.per;
+    const float elements = (float)count_pos * (float)a.per;
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int j = 0; j < CV; ++j)
-        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
+        if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
           float one = 0.f;
 #pragma unroll
           for (int e = 0; e < V; ++e) one += v[k * CV + j].at(e);
           sum += one;
           v[k * CV + j].hide();
         }
-    const float mean = group_sum(sum, a.SP, a.TX, a.D, red[0]) / count;
+    const float mean = group_sum(sum, a.SP, a.TX, a.D, red[0]) / elements;
     float dist = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int j = 0; j < CV; ++j)
-        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
+        if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
           float one = 0.f;
 #pragma unroll
           for (int e = 0; e < V; ++e) { const float d = v[k * CV + j].at(e) - mean; one += d * d; }
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
         o[0] = mean; o[1] = dist;
       }
     } else {
-      const float rstd = rsqrtf(dist / count + a.eps);
+      const float rstd = rsqrtf(dist / elements + a.eps);
       if (first && a.mean) { a.mean[i * a.G + g] = mean; a.rstd[i * a.G + g] = rstd; }
       char* const dst = (char*)(a.y + (i0 * a.S + pos0) * a.ldy + col0);
       const uint32_t step = (uint32_t)a.PL * (uint32_t)a.ldy * (uint32_t)sizeof(T);
@@ -212,11 +215,11 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
           uint32_t off = ((uint32_t)(q.sb * (uint32_t)a.S + q.p) * (uint32_t)a.ldy + lane_col + (uint32_t)(j * a.SP * V)) * (uint32_t)sizeof(T);
 #pragma unroll
           for (int k = 0; k < NP; ++k) {
-            if (q.p + k * a.PL < have) {
+            if (k < count) {
               float h[V];
               Vec o;
 #pragma unroll
-              for (int e = 0; e < V; ++e) h[e] = fmaf(v[k * CV + j].at(e) - mean, gam[e], bet[e]);
+              for (int e = 0; e < V; ++e) h[e] = norm_h(v[k * CV + j].at(e) - mean, gam[e], bet[e]);
               op_act_all<V>(h, a.act);
               o.set(h);
               o.store(dst + off);
@@ -271,7 +274,7 @@ __global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
       v.load(src);
       float h[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = fmaf(v.at(e) - mean, gam[e], bet[e]);
+      for (int e = 0; e < V; ++e) h[e] = norm_h(v.at(e) - mean, gam[e], bet[e]);
       op_act_all<V>(h, a.act);
       o.set(h);
       o.store(dst);
@@ -281,30 +284,33 @@ __global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
   }
 }
 
-// dh of one piece, and xhat
+// dh of one piece, and the distances d from the mean.  s: gamma rstd
 template <typename T, int V>
-__device__ __forceinline__ void norm_dh(const Piece<T, V>& x, const Piece<T, V>& dy, float mean, float rstd, const float* gam, const float* bet,
-                                        int act, float* xh, float* dh) {
+__device__ __forceinline__ void norm_dh(const Piece<T, V>& x, const Piece<T, V>& dy, float mean, const float* s, const float* bet, int act,
+                                        float* d, float* dh) {
   float h[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    xh[e] = norm_xhat(x.at(e), mean, rstd);
+    d[e] = x.at(e) - mean;
     dh[e] = dy.at(e);
   }
   if (act != ABS_ACT_NONE) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = norm_h(xh[e], gam[e], bet[e]);
+    for (int e = 0; e < V; ++e) h[e] = norm_h(d[e], s[e], bet[e]);
     op_slope_all<V>(dh, h, act);
   }
 }
 
 // Backward.  A workgroup keeps its chunk of channels for all its samples, so that the shares of dgamma and dbeta add up in
 // registers and leave once per workgroup.  APPLY as in the forward pass: else only the parts' two sums (and the shares).
-// dh gamma stays in fp32 registers between the sums and dx.
+// dh stays in fp32 registers between the sums and dx.  What is added per element are dh and dh d alone, per channel of the lane's piece:
+// with s = gamma rstd the group's two sums are S1 = sum_c s_c sum dh and S2 = sum_c s_c sum (dh d), a channel's share of dgamma is
+// rstd sum (dh d), and dx = s dh - S1 / N - d rstd^2 S2 / N.
 template <typename T, int V, int NP, int CV, bool APPLY>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
   constexpr bool kKeep = APPLY && NP * V <= 32;
+  constexpr bool kLean = NP * V >= 32;            // no registers for what only the next share needs: sums in LDS, parameters read again
   __shared__ float red[2][16 * 64];
   extern __shared__ float share[];
   const Place q = place_of(a);
@@ -313,23 +319,41 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   place_work(blockIdx.x, a.chunks, a.row_count, row, chunk);
   const int g = (int)chunk * a.gpc + q.g;
   float gam[CV * V], bet[CV * V], sg[CV * V], sb[CV * V];
+  auto parameters = [&]() {
 #pragma unroll
-  for (int j = 0; j < CV; ++j)
+    for (int j = 0; j < CV; ++j) {
+      int s = q.slot + j * a.SP;
+      asm volatile("" : "+v"(s));
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int s = q.slot + j * a.SP;
-      const bool ok = a.gamma && g < a.G && s < a.slots;
-      gam[j * V + e] = ok ? a.gamma[g * a.per + s * V + e] : 1.f;
-      bet[j * V + e] = ok ? a.beta[g * a.per + s * V + e] : 0.f;
-      sg[j * V + e] = sb[j * V + e] = 0.f;
+      for (int e = 0; e < V; ++e) { gam[j * V + e] = 1.f; bet[j * V + e] = 0.f; }
+      if (a.gamma && g < a.G && s < a.slots) {
+        Piece<float, V> pg, pb;
+        pg.load(a.gamma + g * a.per + s * V);
+        pb.load(a.beta + g * a.per + s * V);
+#pragma unroll
+        for (int e = 0; e < V; ++e) { gam[j * V + e] = pg.at(e); bet[j * V + e] = pb.at(e); }
+      }
     }
+  };
+  if (!kLean) {
+    parameters();
+#pragma unroll
+    for (int e = 0; e < CV * V; ++e) sg[e] = sb[e] = 0.f;
+  }
   const uint32_t work = a.work / a.chunks;
   const float inv = 1.0f / ((float)a.S * (float)a.per);
   const int64_t col0 = (int64_t)chunk * a.gpc * a.per;
   const uint32_t lane_col = (uint32_t)(q.g * a.per + q.slot * V), lane_pos = (uint32_t)(q.sb * (uint32_t)a.S + q.p);
   // a lane's first piece in each array, as 32-bit offsets from the workgroup's place there
   auto offset = [&](int64_t ld) { return (lane_pos * (uint32_t)ld + lane_col) * (uint32_t)sizeof(T); };
-  const uint32_t ox0 = offset(a.ldx), od0 = offset(a.lddy), or0 = offset(a.lddres), oy0 = offset(a.ldy);
+  uint32_t ox0, od0, or0, oy0;
+  if (!kLean) { ox0 = offset(a.ldx); od0 = offset(a.lddy); or0 = offset(a.lddres); oy0 = offset(a.ldy); }
+  auto first = [&](uint32_t kept, int64_t ld) {
+    if (!kLean) return kept;
+    uint32_t pos = lane_pos;
+    asm volatile("" : "+v"(pos));
+    return (pos * (uint32_t)ld + lane_col) * (uint32_t)sizeof(T);
+  };
   const uint32_t wide = (uint32_t)(a.SP * V) * (uint32_t)sizeof(T);                            // to the next of CV pieces
   auto walk = [&](uint32_t& off, int64_t ld) {
     off += (uint32_t)a.PL * (uint32_t)ld * (uint32_t)sizeof(T);
@@ -338,7 +362,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   // What a workgroup's next share needs is asked for before this one's is worked on, where that is few registers: with single
   // positions a share is over in the time of a load.
   constexpr bool kAhead = NP * CV * Vec::kWords <= 4;
-  struct Fetched { Vec x[NP * CV], dy[NP * CV], res[kAhead ? NP * CV : 1]; float mean, rstd; int have; int64_t stat; uint32_t part; };
+  struct Fetched { Vec x[NP * CV], dy[NP * CV], res[kAhead ? NP * CV : 1]; float mean, rstd; int count; int64_t stat; uint32_t part; };
   // Uniform places of the share to be fetched: samples a.row_count shares on, or parts of them.
   const int64_t base = col0 * (int64_t)sizeof(T);
   struct Spot { const char *x, *dy, *res; char* y; int64_t i0; };
@@ -354,13 +378,13 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     f.part = a.parts == 1 ? 0u : b % a.parts;
     const int64_t i = p.i0 + q.sb;
     const bool live = i < a.n && g < a.G;
-    f.have = live ? (int)min((int64_t)a.PP, a.S - (int64_t)f.part * a.PP) : 0;
-    uint32_t ox = ox0, od = od0, orr = or0;
+    f.count = live ? q.pieces((int)min((int64_t)a.PP, a.S - (int64_t)f.part * a.PP), a) : 0;
+    uint32_t ox = first(ox0, a.ldx), od = first(od0, a.lddy), orr = kAhead ? first(or0, a.lddres) : 0;
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
 #pragma unroll
       for (int j = 0; j < CV; ++j)
-        if (q.p + k * a.PL < f.have && q.slot + j * a.SP < a.slots) {
+        if (k < f.count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
           f.x[k * CV + j].load(p.x + (ox + j * wide));
           f.dy[k * CV + j].load(p.dy + (od + j * wide));
           if (APPLY && kAhead && a.dres) f.res[kAhead ? k * CV + j : 0].load(p.res + (orr + j * wide));
@@ -385,61 +409,80 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     Vec* const vx = now.x;
     Vec* const vd = now.dy;
     const float mean = now.mean, rstd = now.rstd;
-    const int have = now.have;
-    float s1 = 0.f, s2 = 0.f;
-    float kept[kKeep ? NP * CV * V : 1];
+    const int count = now.count;
+    if (kLean) parameters();
+    float kept[kKeep ? NP * CV * V : 1], s[CV * V], lb[CV * V], lg[CV * V];
+#pragma unroll
+    for (int e = 0; e < CV * V; ++e) { s[e] = gam[e] * rstd; lb[e] = lg[e] = 0.f; }
 #pragma unroll
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int j = 0; j < CV; ++j)
-        if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
-          float xh[V], dh[V];
-          norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, rstd, gam + j * V, bet + j * V, a.act, xh, dh);
+        if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
+          float d[V], dh[V];
+          norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, s + j * V, bet + j * V, a.act, d, dh);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float w = dh[e] * gam[j * V + e];
-            sb[j * V + e] += dh[e];
-            sg[j * V + e] = fmaf(dh[e], xh[e], sg[j * V + e]);
-            s1 += w;
-            s2 = fmaf(w, xh[e], s2);
-            if (kKeep) kept[(k * CV + j) * V + e] = w;
+            lb[j * V + e] += dh[e];
+            lg[j * V + e] = fmaf(dh[e], d[e], lg[j * V + e]);
+            if (kKeep) kept[(k * CV + j) * V + e] = dh[e];
           }
           vx[k * CV + j].hide();
           if (!kKeep) vd[k * CV + j].hide();
         }
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < CV * V; ++e) {
+      s1 = fmaf(s[e], lb[e], s1);
+      s2 = fmaf(s[e], lg[e], s2);
+      if (!kLean) {
+        sb[e] += lb[e];
+        sg[e] = fmaf(rstd, lg[e], sg[e]);
+      }
+    }
+    if (kLean) {                                    // a lane's own place, first written and then added to
+      uint32_t at = threadIdx.x * (2 * V);
+      asm volatile("" : "+v"(at));
+      float* const own = share + at;
+#pragma unroll
+      for (int e = 0; e < V; ++e) { sg[e] = sb[e] = 0.f; }
+      if (b != row) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) { sg[e] = own[e]; sb[e] = own[V + e]; }
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) { own[e] = fmaf(rstd, lg[e], sg[e]); own[V + e] = lb[e] + sb[e]; }
+    }
     s1 = group_sum(s1, a.SP, a.TX, a.D, red[0]);
     s2 = group_sum(s2, a.SP, a.TX, a.D, red[1]);
     if (!APPLY) {
-      if (have > 0 && q.p == 0 && q.slot == 0) {
+      if (count > 0 && q.p == 0 && q.slot == 0) {
         float* o = a.part + (now.stat * a.parts + now.part) * 2;
         o[0] = s1; o[1] = s2;
       }
     } else {
-      // dx = rstd w - (rstd m2) xhat - rstd m1
-      const float c1 = -rstd * (s1 * inv), c2 = -rstd * (s2 * inv);
-      uint32_t oy = oy0, orr = or0;
+      const float c1 = -(s1 * inv), c2 = -rstd * (rstd * (s2 * inv));
+      uint32_t oy = first(oy0, a.ldy), orr = a.dres ? first(or0, a.lddres) : 0;
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
 #pragma unroll
         for (int j = 0; j < CV; ++j)
-          if (q.p + k * a.PL < have && q.slot + j * a.SP < a.slots) {
-            float xh[V], w[V];
+          if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
+            float d[V], w[V];
             if constexpr (kKeep) {
 #pragma unroll
               for (int e = 0; e < V; ++e) {
-                xh[e] = norm_xhat(vx[k * CV + j].at(e), mean, rstd);
+                d[e] = vx[k * CV + j].at(e) - mean;
                 w[e] = kept[(k * CV + j) * V + e];
               }
             } else {
-              norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, rstd, gam + j * V, bet + j * V, a.act, xh, w);
-#pragma unroll
-              for (int e = 0; e < V; ++e) w[e] *= gam[j * V + e];
+              norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, s + j * V, bet + j * V, a.act, d, w);
             }
             Vec o, r;
             if (a.dres) { if constexpr (kAhead) r = now.res[k * CV + j]; else r.load(here.res + (orr + j * wide)); }
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-              w[e] = fmaf(rstd, w[e], fmaf(c2, xh[e], c1));
+              w[e] = fmaf(s[j * V + e], w[e], fmaf(c2, d[e], c1));
               if (a.dres) w[e] += r.at(e);
             }
             o.set(w);
@@ -450,6 +493,11 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     }
   }
   if (!a.rows_g) return;
+  if (kLean) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) { sg[e] = share[threadIdx.x * (2 * V) + e]; sb[e] = share[threadIdx.x * (2 * V) + V + e]; }
+    __syncthreads();
+  }
   // the lanes that share a channel: positions and samples of the workgroup
   const int t = threadIdx.x, lanes = min(a.TX, 64), stack = blockDim.x / (a.TX > 64 ? a.TX : 64);
   if (CV == 1) {
@@ -507,11 +555,11 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
 #pragma unroll 8
     for (uint32_t k = 0; k < a.parts; ++k) { m1 += st[k].x; m2 += st[k].y; }
     const float mean = a.mean[i * a.G + g], rstd = a.rstd[i * a.G + g];
-    const float c1 = -rstd * (m1 * inv), c2 = -rstd * (m2 * inv);
-    float gam[V], bet[V];
+    const float c1 = -(m1 * inv), c2 = -rstd * (rstd * (m2 * inv));
+    float sc[V], bet[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      gam[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] : 1.f;
+      sc[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] * rstd : rstd;
       bet[e] = a.gamma ? a.beta[g * a.per + q.slot * V + e] : 0.f;
     }
     const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
@@ -525,11 +573,11 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
       Vec vx, vd, o, r;
       vx.load(px); vd.load(pd);
       if (pr) r.load(pr);
-      float xh[V], dh[V];
-      norm_dh<T, V>(vx, vd, mean, rstd, gam, bet, a.act, xh, dh);
+      float d[V], dh[V];
+      norm_dh<T, V>(vx, vd, mean, sc, bet, a.act, d, dh);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        dh[e] = fmaf(rstd, dh[e] * gam[e], fmaf(c2, xh[e], c1));
+        dh[e] = fmaf(sc[e], dh[e], fmaf(c2, d[e], c1));
         if (pr) dh[e] += r.at(e);
       }
       o.set(dh);
@@ -595,22 +643,22 @@ __global__ __launch_bounds__(1024) void norm_plain_kernel(NormArgs<T> a) {
       for (int64_t pos = 0; pos < a.S; ++pos)
         for (int c = threadIdx.x; c < a.per; c += blockDim.x) {
           const float gam = a.gamma ? a.gamma[c0 + c] : 1.f, bet = a.gamma ? a.beta[c0 + c] : 0.f;
-          const float xh = norm_xhat(op_widen(a.x[(i * a.S + pos) * a.ldx + c0 + c]), mean, rstd);
-          const float w = op_widen(a.dy[(i * a.S + pos) * a.lddy + c0 + c]) * op_act_slope(norm_h(xh, gam, bet), a.act) * gam;
-          s1 += w; s2 += w * xh;
+          const float d = op_widen(a.x[(i * a.S + pos) * a.ldx + c0 + c]) - mean, s = gam * rstd;
+          const float w = op_widen(a.dy[(i * a.S + pos) * a.lddy + c0 + c]) * op_act_slope(norm_h(d, s, bet), a.act) * s;
+          s1 += w; s2 += w * d;
         }
       m1 = block_sum(s1, red) * inv;
-      m2 = block_sum(s2, red) * inv;
+      m2 = rstd * (rstd * (block_sum(s2, red) * inv));
     }
     for (int64_t pos = 0; pos < a.S; ++pos)
       for (int c = threadIdx.x; c < a.per; c += blockDim.x) {
         const int64_t at = i * a.S + pos;
         const float gam = a.gamma ? a.gamma[c0 + c] : 1.f, bet = a.gamma ? a.beta[c0 + c] : 0.f;
-        const float xh = norm_xhat(op_widen(a.x[at * a.ldx + c0 + c]), mean, rstd), h = norm_h(xh, gam, bet);
+        const float d = op_widen(a.x[at * a.ldx + c0 + c]) - mean, s = gam * rstd, h = norm_h(d, s, bet);
         float v;
         if (!BACKWARD) v = op_act(h, a.act);
         else {
-          v = rstd * (op_widen(a.dy[at * a.lddy + c0 + c]) * op_act_slope(h, a.act) * gam - m1 - xh * m2);
+          v = op_widen(a.dy[at * a.lddy + c0 + c]) * op_act_slope(h, a.act) * s - m1 - d * m2;
           if (a.dres) v += op_widen(a.dres[at * a.lddres + c0 + c]);
         }
         op_narrow(v, a.y[at * a.ldy + c0 + c]);
@@ -631,9 +679,9 @@ __global__ __launch_bounds__(256) void norm_plain_share_kernel(NormArgs<T> a) {
     float sg = 0.f, sb = 0.f;
     for (int64_t at = r; at < total; at += a.row_count) {
       const int64_t i = at / a.S;
-      const float xh = norm_xhat(op_widen(a.x[at * a.ldx + c]), a.mean[i * a.G + g], a.rstd[i * a.G + g]);
-      const float dh = op_widen(a.dy[at * a.lddy + c]) * op_act_slope(norm_h(xh, gam, bet), a.act);
-      sg += dh * xh; sb += dh;
+      const float d = op_widen(a.x[at * a.ldx + c]) - a.mean[i * a.G + g], rstd = a.rstd[i * a.G + g];
+      const float dh = op_widen(a.dy[at * a.lddy + c]) * op_act_slope(norm_h(d, gam * rstd, bet), a.act);
+      sg += dh * (d * rstd); sb += dh;
     }
     a.rows_g[(int64_t)r * a.row_step + c] = sg;
     a.rows_b[(int64_t)r * a.row_step + c] = sb;
@@ -806,7 +854,8 @@ template <typename T, int V>
 hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
   const dim3 grid(q.blocks), block((unsigned)q.threads);
   const int stack = q.threads / std::max(q.TX, 64);
-  const size_t lds = a.rows_g && q.CV == 1 && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;     // 32 KB at most
+  const size_t lds = q.NP * V >= 32                      ? (size_t)q.threads * V * 8        // (kLean; 32 KB at most either way)
+                     : a.rows_g && q.CV == 1 && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;
   if constexpr (V == 1) {
     if (q.CV == kWide) { norm_backward_kernel<T, 1, 1, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
   }
