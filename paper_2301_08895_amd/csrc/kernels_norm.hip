@@ -699,7 +699,7 @@ struct NormPlan {
 
 // The widest piece: 16 bytes; backward four elements, since a lane keeps four sums and parameters per channel of its piece (eight bf16
 // elements take 112 registers and more where four take 74).
-int norm_widest(int dtype, bool backward) { return dtype == ABS_X_BF16 && !backward ? 8 : 4; }
+int norm_widest(const abs_group_norm& p, bool backward) { return p.dtype == ABS_X_BF16 && (!backward || p.spatial == 1) ? 8 : 4; }
 
 int pow2_up(int64_t x) { int p = 1; while (p < x) p <<= 1; return p; }
 
@@ -798,7 +798,7 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
 
 // the widest piece that a group is a whole number of (at any pitch and alignment)
 int norm_piece(const abs_group_norm& p, bool backward) {
-  int V = norm_widest(p.dtype, backward);
+  int V = norm_widest(p, backward);
   while (p.channels / p.groups % V) V /= 2;
   return V;
 }
@@ -864,7 +864,8 @@ hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t 
     if (q.split) norm_backward_kernel<T, V, NP_, 1, false><<<grid, block, lds, s>>>(a);  \
     else         norm_backward_kernel<T, V, NP_, 1, true><<<grid, block, lds, s>>>(a);   \
   }
-  ABS_NORM_B(1) ABS_NORM_B(4) ABS_NORM_B(8)
+  ABS_NORM_B(1)
+  if constexpr (V <= 4) { ABS_NORM_B(4) ABS_NORM_B(8) }
 #undef ABS_NORM_B
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && q.split) {
@@ -900,7 +901,7 @@ hipError_t norm_run(const abs_group_norm& p, bool backward, NormArgs<T> a, const
   } else {
     switch (q.V) {
       case 8:
-        if constexpr (sizeof(T) == 2) e = norm_forward_v<T, 8>(a, q, s);
+        if constexpr (sizeof(T) == 2) e = backward ? norm_backward_v<T, 8>(a, q, s) : norm_forward_v<T, 8>(a, q, s);
         break;
       case 4: e = backward ? norm_backward_v<T, 4>(a, q, s) : norm_forward_v<T, 4>(a, q, s); break;
       case 2: e = backward ? norm_backward_v<T, 2>(a, q, s) : norm_forward_v<T, 2>(a, q, s); break;
