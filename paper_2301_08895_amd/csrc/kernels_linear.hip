@@ -459,20 +459,35 @@ __global__ __launch_bounds__(512, 1) void linear_big_pair_kernel(GemmArgs<uint16
 }
 
 // ---------------------------------------------------------------------- shares of the contraction, added in their order
+// db: rows of column sums, added in their order, 32 columns x 8 rows at a time
+struct DbShares { const float* sums; int shares, N; float* db; };
+__device__ __forceinline__ void add_db(const DbShares& d) {
+  __shared__ float red[8][33];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  for (int n0 = blockIdx.x * 32; n0 < d.N; n0 += gridDim.x * 32) {
+    const int n = n0 + c;
+    float v = 0.f;
+    if (n < d.N)
+#pragma unroll 8
+      for (int k = r; k < d.shares; k += 8) v += d.sums[(int64_t)k * d.N + n];
+    red[r][c] = v;
+    __syncthreads();
+    if (r == 0 && n < d.N) {
+      for (int k = 1; k < 8; ++k) v += red[k][c];
+      d.db[n] = v;
+    }
+    __syncthreads();
+  }
+}
+
 template <typename T>
-struct Join { Epilogue<T> e; int64_t M, N; int shares; const float* db_part; float* db; };       // db: the shares of db as well
+struct Join { Epilogue<T> e; int64_t M, N; int shares; };
 template <typename T>
-__global__ __launch_bounds__(256) void linear_join_kernel(Join<T> first, Join<T> second) {
+__global__ __launch_bounds__(256) void linear_join_kernel(Join<T> first, Join<T> second, DbShares d) {
   constexpr int V = kPiece<T>;
   const Join<T>& j = blockIdx.y ? second : first;
   const int shares = j.shares;
-  if (j.db_part)
-    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < j.N; n += (int64_t)gridDim.x * 256) {
-      float s = 0.f;
-#pragma unroll 8
-      for (int k = 0; k < shares; ++k) s += j.db_part[k * j.N + n];
-      j.db[n] = s;
-    }
+  if (d.db && blockIdx.y == 0) add_db(d);
   Epilogue<T> e = j.e;
   const float* const part = e.part;
   e.part = nullptr;
@@ -875,20 +890,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t ldd
   }
 }
 
-__global__ __launch_bounds__(256) void linear_db_kernel(const float* sums, int shares, int N, float* db) {
-  __shared__ float red[8][33];
-  const int c = threadIdx.x & 31, r = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
-  float v = 0.f;
-  if (n < N)
-#pragma unroll 8
-    for (int k = r; k < shares; k += 8) v += sums[(int64_t)k * N + n];
-  red[r][c] = v;
-  __syncthreads();
-  if (r == 0 && n < N) {
-    for (int k = 1; k < 8; ++k) v += red[k][c];
-    db[n] = v;
-  }
-}
+__global__ __launch_bounds__(256) void linear_db_kernel(DbShares d) { add_db(d); }
 
 // ---------------------------------------------------------------------- an operand whose rows are not whole 16-byte pieces: a copy that is
 // (columns beyond the end are zero: they meet zeros or leave through columns that are not stored)
@@ -1107,13 +1109,19 @@ hipError_t pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* d
   return hipGetLastError();
 }
 
-// (a job without shares is left out)
+// What is left after the products: shares to be joined (a job without them is left out) and db's.
 template <typename T>
-hipError_t launch_join(const Join<T>& a, const Join<T>& b, hipStream_t s) {
+hipError_t launch_join(const Join<T>& a, const Join<T>& b, const DbShares& d, hipStream_t s) {
+  if (!a.shares && !b.shares) {
+    if (!d.db) return hipSuccess;
+    linear_db_kernel<<<dim3((unsigned)((d.N + 31) / 32)), 256, 0, s>>>(d);
+    return hipGetLastError();
+  }
   const Join<T>& one = a.shares ? a : b;
-  auto threads = [](const Join<T>& j) { return j.shares ? std::max(j.M * ((j.N + kPiece<T> - 1) / kPiece<T>), j.db ? j.N : 0) : 0; };
+  auto threads = [](const Join<T>& j) { return j.shares ? j.M * ((j.N + kPiece<T> - 1) / kPiece<T>) : 0; };
   const bool both = a.shares && b.shares;
-  linear_join_kernel<T><<<dim3(few_blocks(std::max(threads(a), threads(b))), both ? 2 : 1), 256, 0, s>>>(one, b);
+  const int64_t most = std::max(std::max(threads(a), threads(b)), d.db ? (int64_t)d.N * 8 : 0);
+  linear_join_kernel<T><<<dim3(few_blocks(most), both ? 2 : 1), 256, 0, s>>>(one, b, d);
   return hipGetLastError();
 }
 
@@ -1125,12 +1133,12 @@ Join<T> set_product(const Product& q, GemmArgs<T>& g, float* part) {
   g.e.ldpart = (int64_t)op_round_up(g.N, 4);
   g.e.part_stride = g.M * g.e.ldpart;
   g.e.part = part;
-  return Join<T>{g.e, g.M, g.N, q.nsplit, nullptr, nullptr};
+  return Join<T>{g.e, g.M, g.N, q.nsplit};
 }
 int product_blocks(const Product& q) { return (q.mt * q.nt * q.nsplit + 7) / 8 * 8; }
 
 template <typename T, bool ATR, bool BTR>
-hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, hipStream_t s) {
+hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, const DbShares& d, hipStream_t s) {
   const Join<T> join = set_product(q, g, part);
   const dim3 grid((unsigned)product_blocks(q));
   if (q.big) {
@@ -1138,7 +1146,7 @@ hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, hipStream_t
   } else if (q.mt * q.nt * q.nsplit > 256) linear_tile_kernel<T, ATR, BTR, 2><<<grid, 256, 0, s>>>(g);
   else linear_tile_kernel<T, ATR, BTR, 4><<<grid, 256, 0, s>>>(g);
   const hipError_t e = hipGetLastError();
-  return e == hipSuccess && join.shares ? launch_join(join, Join<T>{}, s) : e;
+  return e == hipSuccess ? launch_join(join, Join<T>{}, d, s) : e;
 }
 
 template <typename T>
@@ -1156,7 +1164,7 @@ SmallPart<T> small_part(const SmallProduct& q, const Epilogue<T>& e, float* part
     s.e.part = part;
     s.e.ldpart = (int64_t)op_round_up(N, 4);
     s.e.part_stride = M * s.e.ldpart;
-    join = Join<T>{s.e, M, N, q.splits, nullptr, nullptr};
+    join = Join<T>{s.e, M, N, q.splits};
   }
   return s;
 }
@@ -1173,7 +1181,7 @@ hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, 
     g.a = small_part(q.sa, e, (float*)(ws + q.off_part), p.rows, p.d_out, join);
     linear_small_kernel<T, false><<<dim3((unsigned)(q.sa.tiles * q.sa.splits)), 512, 0, s>>>(g);
     const hipError_t err = hipGetLastError();
-    return err == hipSuccess && q.sa.splits > 1 ? launch_join(join, Join<T>{}, s) : err;
+    return err == hipSuccess ? launch_join(join, Join<T>{}, DbShares{}, s) : err;
   }
   float* part = (float*)(ws + q.off_part);
   GemmArgs<T> g{};
@@ -1184,7 +1192,7 @@ hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, 
   if (err != hipSuccess) return err;
   g.M = p.rows; g.N = p.d_out; g.K = p.d_in; g.nc = q.out8; g.mc = 0;
   g.e = e;
-  return run_product<T, false, true>(q.fwd, g, part, s);
+  return run_product<T, false, true>(q.fwd, g, part, DbShares{}, s);
 }
 
 template <typename T>
@@ -1199,23 +1207,25 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     ea.y = (T*)dx; ea.ldy = p.lddx;
     eb.y = (T*)dw; eb.ldy = p.lddw;
     Join<T> ja{}, jb{};
+    DbShares d{};
     if (dx) g.a = small_part(q.sa, ea, (float*)(ws + q.off_part), p.rows, p.d_in, ja);
     if (dw || db) {
       g.b = small_part(q.sb, eb, (float*)(ws + q.off_dz), dw ? p.d_in : 0, p.d_out, jb);
       if (!dw) g.b.tiles = g.b.nt;                            // (db alone: the first row of dW's tiles)
       g.dw = dw != nullptr;
       g.db = db && q.sb.splits > 1 ? (float*)(ws + q.off_sums) : db;
-      if (db && q.sb.splits > 1) { jb.db_part = g.db; jb.db = db; }
+      if (db && q.sb.splits > 1) d = DbShares{g.db, q.sb.splits, p.d_out, db};
     }
     const int blocks = g.a.tiles * g.a.splits + g.b.tiles * g.b.splits;
     if (blocks == 0) return hipSuccess;
     linear_small_kernel<T, true><<<dim3((unsigned)blocks), 512, 0, s>>>(g);
     err = hipGetLastError();
-    return err == hipSuccess && (ja.shares || jb.shares) ? launch_join(ja, jb, s) : err;
+    return err == hipSuccess ? launch_join(ja, jb, d, s) : err;
   }
   const T* dz = (const T*)dy;
   int64_t lddz = p.lddy;
   const bool products = dx || dw;
+  DbShares d{};
   float* sums = db ? (float*)(ws + q.off_sums) : nullptr;
   if ((q.dz && products) || db) {
     T* out = q.dz && products ? (T*)(ws + q.off_dz) : nullptr;
@@ -1225,12 +1235,9 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     if (whole) linear_dz_kernel<T, V><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
     else       linear_dz_kernel<T, 1><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
     err = hipGetLastError();
+    if (db) d = DbShares{sums, q.sum_rows, p.d_out, db};
     if (err == hipSuccess && out && q.out8 != p.d_out) {       // the pieces' ends meet zeros in dx
       linear_zero_kernel<T><<<few_blocks(p.rows * (q.out8 - p.d_out)), 256, 0, s>>>(out + p.d_out, q.out8, p.rows, q.out8 - p.d_out);
-      err = hipGetLastError();
-    }
-    if (err == hipSuccess && db) {
-      linear_db_kernel<<<dim3((unsigned)((p.d_out + 31) / 32)), 256, 0, s>>>(sums, q.sum_rows, p.d_out, db);
       err = hipGetLastError();
     }
     if (out) { dz = out; lddz = q.out8; }
@@ -1257,11 +1264,11 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     if (!q.pair_dw.big) linear_tile_pair_kernel<T><<<grid, 256, 0, s>>>(gb, ga, first);
     else if constexpr (sizeof(T) == 2) linear_big_pair_kernel<<<grid, 512, 0, s>>>(gb, ga, first);
     err = hipGetLastError();
-    return err == hipSuccess && (ja.shares || jb.shares) ? launch_join(ja, jb, s) : err;
+    return err == hipSuccess ? launch_join(ja, jb, d, s) : err;
   }
-  if (dx) err = run_product<T, false, false>(q.dx, ga, part, s);
-  if (err == hipSuccess && dw) err = run_product<T, true, true>(q.dw, gb, part, s);
-  return err;
+  if (dx) { err = run_product<T, false, false>(q.dx, ga, part, d, s); d = DbShares{}; }
+  if (err == hipSuccess && dw) { err = run_product<T, true, true>(q.dw, gb, part, d, s); d = DbShares{}; }
+  return err == hipSuccess ? launch_join(Join<T>{}, Join<T>{}, d, s) : err;
 }
 
 }  // namespace
