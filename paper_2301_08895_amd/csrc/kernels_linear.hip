@@ -50,8 +50,10 @@ struct GemmArgs {
 };
 
 // V neighbouring columns of a row, V the elements of a 16-byte piece.  (Called from loops that are not unrolled: the activations are long.)
+// `bias`, `res`: theirs, where the columns are whole.
 template <typename T>
-__device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t n, int64_t N, float* v) {
+__device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t n, int64_t N, float* v, const Piece<float, kPiece<T>>& bias,
+                                       const Piece<T, kPiece<T>>& res) {
   constexpr int V = kPiece<T>;
   if (e.part) {
     if (n < N) {                                  // (rows of shares are padded to whole quads)
@@ -60,18 +62,16 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t 
         if (n + 4 * q < N) *(f32x4_t*)(e.part + m * e.ldpart + n + 4 * q) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
     }
   } else if (n + V <= N) {
-    Piece<T, V> r, o;
-    if (e.r) r.load(e.r + m * e.ldr + n);
+    Piece<T, V> o;
     if (e.bias) {
-      const Loose<float, V> b = *(const Loose<float, V>*)(e.bias + n);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] += b.e[i];
+      for (int i = 0; i < V; ++i) v[i] += bias.at(i);
     }
     if (e.z) { o.set(v); o.store(e.z + m * e.ldz + n); }
     op_act_all<V>(v, e.act);
     if (e.r) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] += r.at(i);
+      for (int i = 0; i < V; ++i) v[i] += res.at(i);
     }
     o.set(v);
     o.store(e.y + m * e.ldy + n);
@@ -89,6 +89,58 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t 
   }
 }
 
+template <typename T>
+__device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t n, int64_t N, float* v) {
+  Piece<float, kPiece<T>> bias{};
+  Piece<T, kPiece<T>> res{};
+  if (!e.part && n + kPiece<T> <= N) {
+    if (e.r) res.load(e.r + m * e.ldr + n);
+    if (e.bias) bias.load(e.bias + n);
+  }
+  finish(e, m, n, N, v, bias, res);
+}
+
+// A wavefront's results of BLOCKS x 32 rows and 64 columns pass through LDS, 32 rows at a time (`stage`: the function that puts those there),
+// so that they leave as whole 16-byte pieces of rows.  The bias and all rows of the residual are asked for at once, before the
+// first row is worked on: asked for row by row, each costs a turn to memory (32768 x 2048 x 2048 with residual and z: 302 against 312 us).
+constexpr int kOutPitch = 64 + 4;           // floats of a row of a wavefront's staged results
+template <typename T, int BLOCKS, typename Stage>
+__device__ __forceinline__ void finish_rows(const Epilogue<T>& e, int64_t m0, int64_t n0, int64_t M, int64_t N, float* out, int lane, Stage stage) {
+  constexpr int V = kPiece<T>, LPR = 64 / V, kStride = 64 / LPR, kTurns = 32 / kStride;        // LPR: lanes of a row
+  const int64_t m1 = m0 + lane / LPR, n = n0 + (lane % LPR) * V;
+  Piece<float, V> bias{};
+  Piece<T, V> res[BLOCKS][kTurns] = {};
+  if (!e.part && n + V <= N) {
+    if (e.bias) bias.load(e.bias + n);
+    if (e.r) {
+#pragma unroll
+      for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+          const int64_t m = m1 + i * 32 + k * kStride;
+          if (m < M) res[i][k].load(e.r + m * e.ldr + n);
+        }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i) {
+    stage(i);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int k = 0; k < kTurns; ++k) {
+      const int64_t m = m1 + i * 32 + k * kStride;
+      float v[V];
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) *(f32x4_t*)&v[4 * q] = *(const f32x4_t*)&out[(lane / LPR + k * kStride) * kOutPitch + (lane % LPR) * V + 4 * q];
+      if (m < M) finish(e, m, n, N, v, bias, res[i][0]);
+#pragma unroll
+      for (int h = 1; h < kTurns; ++h) res[i][h - 1] = res[i][h];      // (the loop stays a loop: the next row's is first)
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // ---------------------------------------------------------------------- the tile kernel
 // 128 x 128 of the result per workgroup, 4 wavefronts of 64 x 64 (2 x 2 blocks of 32 x 32), a k-step of 128 bytes per row.
 // Tiles travel global -> LDS through a ring of RING steps.  An operand [row][k]: a row of a step is 128 bytes, its
@@ -97,7 +149,6 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t 
 // b ^ ((k >> 2) & 1) (the two halves of a wavefront read rows 4 apart).  The operands of the matrix instruction are swapped
 // (columns first), so that a lane ends up with four neighbouring columns of one row.
 constexpr int kTile = 128;
-constexpr int kOutPitch = 64 + 4;           // floats of a row of a wavefront's staged results
 
 template <typename T, bool TR>
 struct TileOperand {
@@ -228,32 +279,18 @@ __device__ __forceinline__ void tile_product(const GemmArgs<T>& g, int block, T*
       acc[1][1] = multiply(b1, a1, acc[1][1]);
     }
   }
-  // Register r of a lane: column 8 (r / 4) + 4 (lane / 32) + r % 4, row lane % 32 of its block.  Each wavefront's 32 x 64 results
-  // pass through LDS, so that they leave as whole 16-byte pieces of rows.
-  __syncthreads();
-  float* const stage_out = (float*)smem + wave * (32 * kOutPitch);
+  // Register r of a lane: column 8 (r / 4) + 4 (lane / 32) + r % 4, row lane % 32 of its block.
+  float* const out = (float*)smem + wave * (32 * kOutPitch);
   Epilogue<T> e = g.e;
   if (e.part) e.part += split * e.part_stride;
-  constexpr int V = kPiece<T>, LPR = 64 / V;              // lanes of a row
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  finish_rows<T, 2>(e, m0 + wm * 64, n0 + wn * 64, g.M, g.N, out, lane, [&](int i) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        *(f32x4_t*)&stage_out[(lane & 31) * kOutPitch + j * 32 + 8 * q + 4 * (lane >> 5)] =
+        *(f32x4_t*)&out[(lane & 31) * kOutPitch + j * 32 + 8 * q + 4 * (lane >> 5)] =
             f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int r = lane / LPR; r < 32; r += 64 / LPR) {
-      const int64_t m = m0 + wm * 64 + i * 32 + r, n = n0 + wn * 64 + (lane % LPR) * V;
-      float v[V];
-#pragma unroll
-      for (int q = 0; q < V / 4; ++q) *(f32x4_t*)&v[4 * q] = *(const f32x4_t*)&stage_out[r * kOutPitch + (lane % LPR) * V + 4 * q];
-      if (m < g.M) finish(e, m, n, g.N, v);
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
+  });
 }
 
 // ---------------------------------------------------------------------- the large-tile kernel (bf16)
@@ -408,28 +445,16 @@ __device__ __forceinline__ void big_product(const GemmArgs<uint16_t>& g, int blo
 #undef ABS_MMA
 #undef ABS_LOAD_B
 #undef ABS_LOAD_A
-  // Register r of a lane: column 4 (lane / 16) + r, row lane % 16 of its block.  32 rows of a wavefront at a time through LDS.
-  __syncthreads();
-  float* const stage_out = (float*)smem + wave * (32 * kOutPitch);
+  // Register r of a lane: column 4 (lane / 16) + r, row lane % 16 of its block.
+  float* const out = (float*)smem + wave * (32 * kOutPitch);
   Epilogue<uint16_t> e = g.e;
   if (e.part) e.part += split * e.part_stride;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  finish_rows<uint16_t, 4>(e, m0 + wm * 128, n0 + wn * 64, g.M, g.N, out, lane, [&](int i) {
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) *(f32x4_t*)&stage_out[(a * 16 + (lane & 15)) * kOutPitch + b * 16 + 4 * (lane >> 4)] = acc[2 * i + a][b];
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int r = lane >> 3; r < 32; r += 8) {
-      const int64_t m = m0 + wm * 128 + i * 32 + r, n = n0 + wn * 64 + (lane & 7) * 8;
-      float v[8];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) *(f32x4_t*)&v[4 * q] = *(const f32x4_t*)&stage_out[r * kOutPitch + (lane & 7) * 8 + 4 * q];
-      if (m < g.M) finish(e, m, n, g.N, v);
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
+      for (int b = 0; b < 4; ++b) *(f32x4_t*)&out[(a * 16 + (lane & 15)) * kOutPitch + b * 16 + 4 * (lane >> 4)] = acc[2 * i + a][b];
+  });
 }
 
 constexpr int kBigLds = 8 * kHalf;
