@@ -19,7 +19,6 @@ namespace abs_impl {
 namespace {
 
 constexpr int kMaxLanes = 1024;            // D: lanes of one sample
-constexpr int kWide = 4;                   // pieces across the channels per lane, for groups of more than kMaxLanes single elements
 
 template <typename T>
 struct NormArgs {
@@ -99,8 +98,9 @@ __device__ __forceinline__ float group_sum(float v, int SP, int TX, int D, float
 }
 
 // Where a thread stands: its sample inside the workgroup, positions p, p + PL, ..., group and piece.
+// A group that is no whole number of pieces (TAIL) ends in one that has nv < V elements of its own.
 struct Place {
-  int sb, p, g, slot;
+  int sb, p, g, slot, nv;
   // how many of the lane's positions p, p + PL, ... lie below `positions`; none for a lane behind the group's pieces (the comparison of a
   // constant with this number is all that a piece costs: PL is a power of two, and positions kept for it would each take a register)
   template <typename A>
@@ -108,7 +108,7 @@ struct Place {
     return p < positions && slot < a.slots ? ((positions - p - 1) >> (31 - __builtin_clz(a.PL))) + 1 : 0;
   }
 };
-template <typename T>
+template <typename T, int V, bool TAIL>
 __device__ __forceinline__ Place place_of(const NormArgs<T>& a) {
   Place q;
   const int t = threadIdx.x, tx = t & (a.TX - 1);
@@ -116,7 +116,69 @@ __device__ __forceinline__ Place place_of(const NormArgs<T>& a) {
   q.p = (t & (a.D - 1)) / a.TX;
   q.g = tx / a.SP;
   q.slot = tx & (a.SP - 1);
+  q.nv = TAIL ? min(V, a.per - q.slot * V) : V;
   return q;
+}
+
+// The last piece of a TAIL group is read V - nv elements early, so that it is one access inside the group, and moved down once it is there,
+// zeros behind it.  (Only where everything is read before anything is written: the elements read twice may be another wavefront's to
+// overwrite.)
+template <typename T, int V>
+__device__ __forceinline__ void move_down(Piece<T, V>& v, int nv) {
+  const int skip = V - nv;
+  if constexpr (sizeof(T) == 2 && V == 4) {
+    const uint64_t x = (((uint64_t)v.w[1] << 32) | v.w[0]) >> (16 * skip);
+    v.w[0] = (uint32_t)x; v.w[1] = (uint32_t)(x >> 32);
+  } else if constexpr (sizeof(T) == 2) {
+    v.w[0] >>= 16 * skip;
+  } else {
+    if (skip & 1) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) v.w[e] = e + 1 < V ? v.w[e + 1] : 0;
+    }
+    if (V > 2 && skip & 2) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) v.w[e] = e + 2 < V ? v.w[e + 2] : 0;
+    }
+  }
+}
+// ... or element by element; and what is written is its own elements alone.
+template <bool TAIL, typename T, int V>
+__device__ __forceinline__ void load_own(Piece<T, V>& v, const void* p, int nv) {
+  if (!TAIL || nv == V) { v.load(p); return; }
+  T e[V];
+#pragma unroll
+  for (int i = 0; i < V - 1; ++i) e[i] = ((const T*)p)[min(i, nv - 1)];       // (no branch, so that all are asked for at once)
+#pragma unroll
+  for (int i = 0; i < V; ++i) e[i] = i < nv ? e[min(i, V - 2)] : T(0);
+  __builtin_memcpy(v.w, e, V * sizeof(T));
+}
+template <bool TAIL, typename T, int V>
+__device__ __forceinline__ void store_own(const Piece<T, V>& v, void* p, int nv) {
+  if (!TAIL || nv == V) { v.store(p); return; }
+  T e[V];
+  __builtin_memcpy(e, v.w, V * sizeof(T));
+#pragma unroll
+  for (int i = 0; i < V - 1; ++i)
+    if (i < nv) ((T*)p)[i] = e[i];
+}
+// gamma and beta of a piece's channels, from c on; 0 behind the group's end
+template <bool TAIL, typename T, int V>
+__device__ __forceinline__ void parameters(const NormArgs<T>& a, int c, int nv, float* gam, float* bet) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) { gam[e] = 1.f; bet[e] = 0.f; }
+  if (a.gamma) {
+    Piece<float, V> pg, pb;
+    if (TAIL) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) { pg.w[e] = __float_as_uint(a.gamma[c + min(e, nv - 1)]); pb.w[e] = __float_as_uint(a.beta[c + min(e, nv - 1)]); }
+    } else {
+      pg.load(a.gamma + c);
+      pb.load(a.beta + c);
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) { gam[e] = e < nv ? pg.at(e) : 0.f; bet[e] = e < nv ? pb.at(e) : 0.f; }
+  }
 }
 
 // Workgroup b of (samples x rest): neighbouring chunks of the same positions on one XCD (workgroups are dealt out over eight), one after
@@ -130,14 +192,14 @@ __device__ __forceinline__ void place_work(uint32_t b, uint32_t per_sample, uint
 }
 
 // Forward.  APPLY: one part holds the sample (parts == 1) and the result is written; else only the part's mean and squared
-// distances are left.  NP positions per lane, CV pieces across the channels of each.  Addresses are a uniform base and a 32-bit
+// distances are left.  NP positions per lane.  Addresses are a uniform base and a 32-bit
 // offset that walks, so that they cost two registers and not two per piece (with 64 registers of values that decides whether
 // anything spills).
-template <typename T, int V, int NP, int CV, bool APPLY>
+template <typename T, int V, int NP, bool APPLY, bool TAIL>
 __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
   __shared__ float red[2][16 * 64];
-  const Place q = place_of(a);
+  const Place q = place_of<T, V, TAIL>(a);
   const uint32_t spb = blockDim.x / (uint32_t)a.D, per_sample = a.chunks * a.parts;
   for (uint32_t b = blockIdx.x; b < a.work; b += gridDim.x) {
     uint32_t si, rest;
@@ -151,15 +213,13 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
     const int64_t col0 = (int64_t)chunk * a.gpc * a.per;
     const char* const src = (const char*)(a.x + (i0 * a.S + pos0) * a.ldx + col0);
     const uint32_t lane_col = (uint32_t)(q.g * a.per + q.slot * V);
-    Vec v[NP * CV];
+    Vec v[NP];
     {
-      uint32_t off = ((uint32_t)(q.sb * (uint32_t)a.S + q.p) * (uint32_t)a.ldx + lane_col) * (uint32_t)sizeof(T);
+      uint32_t off = ((uint32_t)(q.sb * (uint32_t)a.S + q.p) * (uint32_t)a.ldx + lane_col - (uint32_t)(V - q.nv)) * (uint32_t)sizeof(T);
       const uint32_t step = (uint32_t)a.PL * (uint32_t)a.ldx * (uint32_t)sizeof(T);
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
-#pragma unroll
-        for (int j = 0; j < CV; ++j)
-          if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) v[k * CV + j].load(src + (off + (uint32_t)(j * a.SP * V * (int)sizeof(T))));
+        if (k < count) v[k].load(src + off);
         off += step;
         asm volatile("" : "+v"(off));
       }
@@ -168,28 +228,25 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
+      if (k < count) {
+        if (TAIL) move_down(v[k], q.nv);
+        float one = 0.f;
 #pragma unroll
-      for (int j = 0; j < CV; ++j)
-        if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
-          float one = 0.f;
-#pragma unroll
-          for (int e = 0; e < V; ++e) one += v[k * CV + j].at(e);
-          sum += one;
-          v[k * CV + j].hide();
-        }
+        for (int e = 0; e < V; ++e) one += v[k].at(e);
+        sum += one;
+        v[k].hide();
+      }
     const float mean = group_sum(sum, a.SP, a.TX, a.D, red[0]) / elements;
     float dist = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k)
+      if (k < count) {
+        float one = 0.f;
 #pragma unroll
-      for (int j = 0; j < CV; ++j)
-        if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
-          float one = 0.f;
-#pragma unroll
-          for (int e = 0; e < V; ++e) { const float d = v[k * CV + j].at(e) - mean; one += d * d; }
-          dist += one;
-          v[k * CV + j].hide();
-        }
+        for (int e = 0; e < V; ++e) { const float d = v[k].at(e) - mean; one += TAIL && e >= q.nv ? 0.f : d * d; }
+        dist += one;
+        v[k].hide();
+      }
     dist = group_sum(dist, a.SP, a.TX, a.D, red[1]);
     const bool first = live && q.p == 0 && q.slot == 0;
     if (!APPLY) {
@@ -202,31 +259,25 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
       if (first && a.mean) { a.mean[i * a.G + g] = mean; a.rstd[i * a.G + g] = rstd; }
       char* const dst = (char*)(a.y + (i0 * a.S + pos0) * a.ldy + col0);
       const uint32_t step = (uint32_t)a.PL * (uint32_t)a.ldy * (uint32_t)sizeof(T);
+      if (count > 0) {
+        float gam[V], bet[V];
+        parameters<TAIL, T, V>(a, g * a.per + q.slot * V, q.nv, gam, bet);
 #pragma unroll
-      for (int j = 0; j < CV; ++j) {
-        const int s = q.slot + j * a.SP;
-        if (live && s < a.slots) {
-          float gam[V], bet[V];
+        for (int e = 0; e < V; ++e) gam[e] *= rstd;
+        uint32_t off = ((uint32_t)(q.sb * (uint32_t)a.S + q.p) * (uint32_t)a.ldy + lane_col) * (uint32_t)sizeof(T);
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            gam[e] = a.gamma ? a.gamma[g * a.per + s * V + e] * rstd : rstd;
-            bet[e] = a.gamma ? a.beta[g * a.per + s * V + e] : 0.f;
+        for (int k = 0; k < NP; ++k) {
+          if (k < count) {
+            float h[V];
+            Vec o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) h[e] = norm_h(v[k].at(e) - mean, gam[e], bet[e]);
+            op_act_all<V>(h, a.act);
+            o.set(h);
+            store_own<TAIL>(o, dst + off, q.nv);
           }
-          uint32_t off = ((uint32_t)(q.sb * (uint32_t)a.S + q.p) * (uint32_t)a.ldy + lane_col + (uint32_t)(j * a.SP * V)) * (uint32_t)sizeof(T);
-#pragma unroll
-          for (int k = 0; k < NP; ++k) {
-            if (k < count) {
-              float h[V];
-              Vec o;
-#pragma unroll
-              for (int e = 0; e < V; ++e) h[e] = norm_h(v[k * CV + j].at(e) - mean, gam[e], bet[e]);
-              op_act_all<V>(h, a.act);
-              o.set(h);
-              o.store(dst + off);
-            }
-            off += step;
-            asm volatile("" : "+v"(off));
-          }
+          off += step;
+          asm volatile("" : "+v"(off));
         }
       }
     }
@@ -235,10 +286,10 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
 }
 
 // Joins the parts' statistics and writes; a workgroup takes the positions of one part.
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
-  const Place q = place_of(a);
+  const Place q = place_of<T, V, TAIL>(a);
   for (uint32_t b = blockIdx.x; b < a.work; b += gridDim.x) {
     const uint32_t chunk = b % a.chunks, part = b / a.chunks % a.parts;
     const int64_t i = b / a.chunks / a.parts;
@@ -259,11 +310,9 @@ __global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
     const float rstd = rsqrtf(dist * inv + a.eps);
     if (a.mean && part == 0 && q.p == 0 && q.slot == 0) { a.mean[i * a.G + g] = mean; a.rstd[i * a.G + g] = rstd; }
     float gam[V], bet[V];
+    parameters<TAIL, T, V>(a, g * a.per + q.slot * V, q.nv, gam, bet);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      gam[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] * rstd : rstd;
-      bet[e] = a.gamma ? a.beta[g * a.per + q.slot * V + e] : 0.f;
-    }
+    for (int e = 0; e < V; ++e) gam[e] *= rstd;
     const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
     const int64_t col = (int64_t)g * a.per + q.slot * V;
     const T* src = a.x + (i * a.S + pos0 + q.p) * a.ldx + col;
@@ -271,13 +320,13 @@ __global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
 #pragma unroll 4
     for (int pos = q.p; pos < count_pos; pos += a.PL) {
       Vec v, o;
-      v.load(src);
+      load_own<TAIL>(v, src, q.nv);
       float h[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) h[e] = norm_h(v.at(e) - mean, gam[e], bet[e]);
       op_act_all<V>(h, a.act);
       o.set(h);
-      o.store(dst);
+      store_own<TAIL>(o, dst, q.nv);
       src += a.PL * a.ldx;
       dst += a.PL * a.ldy;
     }
@@ -306,39 +355,30 @@ __device__ __forceinline__ void norm_dh(const Piece<T, V>& x, const Piece<T, V>&
 // dh stays in fp32 registers between the sums and dx.  What is added per element are dh and dh d alone, per channel of the lane's piece:
 // with s = gamma rstd the group's two sums are S1 = sum_c s_c sum dh and S2 = sum_c s_c sum (dh d), a channel's share of dgamma is
 // rstd sum (dh d), and dx = s dh - S1 / N - d rstd^2 S2 / N.
-template <typename T, int V, int NP, int CV, bool APPLY>
+template <typename T, int V, int NP, bool APPLY, bool TAIL>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
   constexpr bool kKeep = APPLY && NP * V <= 32;
   constexpr bool kLean = NP * V >= 32;            // no registers for what only the next share needs: sums in LDS, parameters read again
   __shared__ float red[2][16 * 64];
   extern __shared__ float share[];
-  const Place q = place_of(a);
+  const Place q = place_of<T, V, TAIL>(a);
   const uint32_t spb = blockDim.x / (uint32_t)a.D;
   uint32_t chunk, row;
   place_work(blockIdx.x, a.chunks, a.row_count, row, chunk);
   const int g = (int)chunk * a.gpc + q.g;
-  float gam[CV * V], bet[CV * V], sg[CV * V], sb[CV * V];
-  auto parameters = [&]() {
+  float gam[V], bet[V], sg[V], sb[V];
+  auto channels = [&]() {
+    int s = q.slot;
+    asm volatile("" : "+v"(s));
 #pragma unroll
-    for (int j = 0; j < CV; ++j) {
-      int s = q.slot + j * a.SP;
-      asm volatile("" : "+v"(s));
-#pragma unroll
-      for (int e = 0; e < V; ++e) { gam[j * V + e] = 1.f; bet[j * V + e] = 0.f; }
-      if (a.gamma && g < a.G && s < a.slots) {
-        Piece<float, V> pg, pb;
-        pg.load(a.gamma + g * a.per + s * V);
-        pb.load(a.beta + g * a.per + s * V);
-#pragma unroll
-        for (int e = 0; e < V; ++e) { gam[j * V + e] = pg.at(e); bet[j * V + e] = pb.at(e); }
-      }
-    }
+    for (int e = 0; e < V; ++e) { gam[e] = 1.f; bet[e] = 0.f; }
+    if (g < a.G && s < a.slots) parameters<TAIL, T, V>(a, g * a.per + s * V, q.nv, gam, bet);
   };
   if (!kLean) {
-    parameters();
+    channels();
 #pragma unroll
-    for (int e = 0; e < CV * V; ++e) sg[e] = sb[e] = 0.f;
+    for (int e = 0; e < V; ++e) sg[e] = sb[e] = 0.f;
   }
   const uint32_t work = a.work / a.chunks;
   const float inv = 1.0f / ((float)a.S * (float)a.per);
@@ -354,15 +394,14 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     asm volatile("" : "+v"(pos));
     return (pos * (uint32_t)ld + lane_col) * (uint32_t)sizeof(T);
   };
-  const uint32_t wide = (uint32_t)(a.SP * V) * (uint32_t)sizeof(T);                            // to the next of CV pieces
   auto walk = [&](uint32_t& off, int64_t ld) {
     off += (uint32_t)a.PL * (uint32_t)ld * (uint32_t)sizeof(T);
     asm volatile("" : "+v"(off));
   };
   // What a workgroup's next share needs is asked for before this one's is worked on, where that is few registers: with single
   // positions a share is over in the time of a load.
-  constexpr bool kAhead = NP * CV * Vec::kWords <= 4;
-  struct Fetched { Vec x[NP * CV], dy[NP * CV], res[kAhead ? NP * CV : 1]; float mean, rstd; int count; int64_t stat; uint32_t part; };
+  constexpr bool kAhead = NP * Vec::kWords <= 4;
+  struct Fetched { Vec x[NP], dy[NP], res[kAhead ? NP : 1]; float mean, rstd; int count; int64_t stat; uint32_t part; };
   // Uniform places of the share to be fetched: samples a.row_count shares on, or parts of them.
   const int64_t base = col0 * (int64_t)sizeof(T);
   struct Spot { const char *x, *dy, *res; char* y; int64_t i0; };
@@ -382,13 +421,12 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     uint32_t ox = first(ox0, a.ldx), od = first(od0, a.lddy), orr = kAhead ? first(or0, a.lddres) : 0;
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-#pragma unroll
-      for (int j = 0; j < CV; ++j)
-        if (k < f.count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
-          f.x[k * CV + j].load(p.x + (ox + j * wide));
-          f.dy[k * CV + j].load(p.dy + (od + j * wide));
-          if (APPLY && kAhead && a.dres) f.res[kAhead ? k * CV + j : 0].load(p.res + (orr + j * wide));
-        }
+      if (k < f.count) {
+        const uint32_t early = TAIL ? (uint32_t)(V - q.nv) * (uint32_t)sizeof(T) : 0;
+        f.x[k].load(p.x + (ox - early));
+        f.dy[k].load(p.dy + (od - early));
+        if (APPLY && kAhead && a.dres) load_own<TAIL>(f.res[kAhead ? k : 0], p.res + orr, q.nv);
+      }
       if (NP > 1) { walk(ox, a.ldx); walk(od, a.lddy); if (kAhead) walk(orr, a.lddres); }
     }
     f.stat = i * a.G + g;
@@ -410,29 +448,28 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
     Vec* const vd = now.dy;
     const float mean = now.mean, rstd = now.rstd;
     const int count = now.count;
-    if (kLean) parameters();
-    float kept[kKeep ? NP * CV * V : 1], s[CV * V], lb[CV * V], lg[CV * V];
+    if (kLean) channels();
+    float kept[kKeep ? NP * V : 1], s[V], lb[V], lg[V];
 #pragma unroll
-    for (int e = 0; e < CV * V; ++e) { s[e] = gam[e] * rstd; lb[e] = lg[e] = 0.f; }
+    for (int e = 0; e < V; ++e) { s[e] = gam[e] * rstd; lb[e] = lg[e] = 0.f; }
 #pragma unroll
     for (int k = 0; k < NP; ++k)
+      if (k < count) {
+        if (TAIL) { move_down(vx[k], q.nv); move_down(vd[k], q.nv); }
+        float d[V], dh[V];
+        norm_dh<T, V>(vx[k], vd[k], mean, s, bet, a.act, d, dh);
 #pragma unroll
-      for (int j = 0; j < CV; ++j)
-        if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
-          float d[V], dh[V];
-          norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, s + j * V, bet + j * V, a.act, d, dh);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            lb[j * V + e] += dh[e];
-            lg[j * V + e] = fmaf(dh[e], d[e], lg[j * V + e]);
-            if (kKeep) kept[(k * CV + j) * V + e] = dh[e];
-          }
-          vx[k * CV + j].hide();
-          if (!kKeep) vd[k * CV + j].hide();
+        for (int e = 0; e < V; ++e) {
+          lb[e] += dh[e];
+          lg[e] = fmaf(dh[e], d[e], lg[e]);
+          if (kKeep) kept[k * V + e] = dh[e];
         }
+        vx[k].hide();
+        if (!kKeep) vd[k].hide();
+      }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int e = 0; e < CV * V; ++e) {
+    for (int e = 0; e < V; ++e) {
       s1 = fmaf(s[e], lb[e], s1);
       s2 = fmaf(s[e], lg[e], s2);
       if (!kLean) {
@@ -465,29 +502,27 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
       uint32_t oy = first(oy0, a.ldy), orr = a.dres ? first(or0, a.lddres) : 0;
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
-#pragma unroll
-        for (int j = 0; j < CV; ++j)
-          if (k < count && (CV == 1 || q.slot + j * a.SP < a.slots)) {
-            float d[V], w[V];
-            if constexpr (kKeep) {
-#pragma unroll
-              for (int e = 0; e < V; ++e) {
-                d[e] = vx[k * CV + j].at(e) - mean;
-                w[e] = kept[(k * CV + j) * V + e];
-              }
-            } else {
-              norm_dh<T, V>(vx[k * CV + j], vd[k * CV + j], mean, s + j * V, bet + j * V, a.act, d, w);
-            }
-            Vec o, r;
-            if (a.dres) { if constexpr (kAhead) r = now.res[k * CV + j]; else r.load(here.res + (orr + j * wide)); }
+        if (k < count) {
+          float d[V], w[V];
+          if constexpr (kKeep) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-              w[e] = fmaf(s[j * V + e], w[e], fmaf(c2, d[e], c1));
-              if (a.dres) w[e] += r.at(e);
+              d[e] = vx[k].at(e) - mean;
+              w[e] = kept[k * V + e];
             }
-            o.set(w);
-            o.store(here.y + (oy + j * wide));
+          } else {
+            norm_dh<T, V>(vx[k], vd[k], mean, s, bet, a.act, d, w);
           }
+          Vec o, r;
+          if (a.dres) { if constexpr (kAhead) r = now.res[k]; else load_own<TAIL>(r, here.res + orr, q.nv); }
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            w[e] = fmaf(s[e], w[e], fmaf(c2, d[e], c1));
+            if (a.dres) w[e] += r.at(e);
+          }
+          o.set(w);
+          store_own<TAIL>(o, here.y + oy, q.nv);
+        }
         if (NP > 1) { walk(oy, a.ldy); walk(orr, a.lddres); }
       }
     }
@@ -500,50 +535,44 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   }
   // the lanes that share a channel: positions and samples of the workgroup
   const int t = threadIdx.x, lanes = min(a.TX, 64), stack = blockDim.x / (a.TX > 64 ? a.TX : 64);
-  if (CV == 1) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sg[e] = add_lanes<false>(sg[e], 63 & ~(a.TX - 1));
-      sb[e] = add_lanes<false>(sb[e], 63 & ~(a.TX - 1));
-    }
-    if (stack > 1) {                                // [stack][V][TX], dgamma's shares and then dbeta's
-      const int r = t / (a.TX > 64 ? a.TX : 64), tx = t & (a.TX - 1);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h) __syncthreads();
-        if (a.TX >= 64 || (t & 63) < lanes) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) share[(r * V + e) * a.TX + tx] = h ? sb[e] : sg[e];
-        }
-        __syncthreads();
-        if (t < a.TX) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float sum = 0.f;
-            for (int k = 0; k < stack; ++k) sum += share[(k * V + e) * a.TX + t];
-            (h ? sb : sg)[e] = sum;
-          }
-        }
-      }
-    }
-    if (t >= a.TX) return;
+  for (int e = 0; e < V; ++e) {
+    sg[e] = add_lanes<false>(sg[e], 63 & ~(a.TX - 1));
+    sb[e] = add_lanes<false>(sb[e], 63 & ~(a.TX - 1));
   }
-  if (g < a.G) {
-    const int64_t o = (int64_t)row * a.row_step + g * a.per;
+  if (stack > 1) {                                // [stack][V][TX], dgamma's shares and then dbeta's
+    const int r = t / (a.TX > 64 ? a.TX : 64), tx = t & (a.TX - 1);
 #pragma unroll
-    for (int j = 0; j < CV; ++j)
+    for (int h = 0; h < 2; ++h) {
+      if (h) __syncthreads();
+      if (a.TX >= 64 || (t & 63) < lanes) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int s = q.slot + j * a.SP;
-        if (s < a.slots) { a.rows_g[o + s * V + e] = sg[j * V + e]; a.rows_b[o + s * V + e] = sb[j * V + e]; }
+        for (int e = 0; e < V; ++e) share[(r * V + e) * a.TX + tx] = h ? sb[e] : sg[e];
       }
+      __syncthreads();
+      if (t < a.TX) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float sum = 0.f;
+          for (int k = 0; k < stack; ++k) sum += share[(k * V + e) * a.TX + t];
+          (h ? sb : sg)[e] = sum;
+        }
+      }
+    }
+  }
+  if (t >= a.TX) return;
+  if (g < a.G && q.slot < a.slots) {
+    const int64_t o = (int64_t)row * a.row_step + (int64_t)g * a.per + q.slot * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < q.nv) { a.rows_g[o + e] = sg[e]; a.rows_b[o + e] = sb[e]; }
   }
 }
 
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
-  const Place q = place_of(a);
+  const Place q = place_of<T, V, TAIL>(a);
   const float inv = 1.0f / ((float)a.S * (float)a.per);
   for (uint32_t b = blockIdx.x; b < a.work; b += gridDim.x) {
     const uint32_t chunk = b % a.chunks, part = b / a.chunks % a.parts;
@@ -557,11 +586,9 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
     const float mean = a.mean[i * a.G + g], rstd = a.rstd[i * a.G + g];
     const float c1 = -(m1 * inv), c2 = -rstd * (rstd * (m2 * inv));
     float sc[V], bet[V];
+    parameters<TAIL, T, V>(a, g * a.per + q.slot * V, q.nv, sc, bet);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sc[e] = a.gamma ? a.gamma[g * a.per + q.slot * V + e] * rstd : rstd;
-      bet[e] = a.gamma ? a.beta[g * a.per + q.slot * V + e] : 0.f;
-    }
+    for (int e = 0; e < V; ++e) sc[e] *= rstd;
     const int pos0 = (int)part * a.PP, count_pos = (int)min((int64_t)a.PP, a.S - pos0);
     const int64_t at = i * a.S + pos0 + q.p, col = (int64_t)g * a.per + q.slot * V;
     const T* px = a.x + at * a.ldx + col;
@@ -571,8 +598,8 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
 #pragma unroll 2
     for (int pos = q.p; pos < count_pos; pos += a.PL) {
       Vec vx, vd, o, r;
-      vx.load(px); vd.load(pd);
-      if (pr) r.load(pr);
+      load_own<TAIL>(vx, px, q.nv); load_own<TAIL>(vd, pd, q.nv);
+      if (pr) load_own<TAIL>(r, pr, q.nv);
       float d[V], dh[V];
       norm_dh<T, V>(vx, vd, mean, sc, bet, a.act, d, dh);
 #pragma unroll
@@ -581,7 +608,7 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
         if (pr) dh[e] += r.at(e);
       }
       o.set(dh);
-      o.store(dst);
+      store_own<TAIL>(o, dst, q.nv);
       px += a.PL * a.ldx; pd += a.PL * a.lddy; dst += a.PL * a.ldy;
       if (pr) pr += a.PL * a.lddres;
     }
@@ -690,8 +717,8 @@ __global__ __launch_bounds__(256) void norm_plain_share_kernel(NormArgs<T> a) {
 
 // ---- the plan -------------------------------------------------------------------------------------------
 struct NormPlan {
-  int V, NP, CV, threads;
-  bool plain, split;
+  int V, NP, threads;
+  bool tail, plain, split;
   int slots, SP, gpc, TX, PL, D, PP;
   uint32_t chunks, parts, row_count, work, blocks;
   size_t off_rows, bytes;                  // workspace: parts' statistics, then the shares of dgamma / dbeta
@@ -708,17 +735,12 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
   NormPlan q{};
   const int size = op_size(p.dtype), per = p.channels / p.groups;
   const int64_t S = p.spatial;
-  q.V = V; q.CV = 1; q.parts = 1; q.PP = (int)S;
-  q.slots = per / V;
+  q.V = V; q.tail = per % V != 0; q.parts = 1; q.PP = (int)S;
+  q.slots = (per + V - 1) / V;
   q.SP = pow2_up(q.slots);
   const int np_most = backward ? 8 : 16;
   if (q.SP > kMaxLanes) {
-    if (V == 1 && q.SP <= kMaxLanes * kWide && S == 1) {        // single elements of one position: several across the channels
-      q.CV = kWide; q.NP = 1; q.SP = kMaxLanes;
-      q.gpc = 1; q.TX = q.D = kMaxLanes; q.PL = 1; q.chunks = p.groups;
-    } else {
-      q.plain = true;
-    }
+    q.plain = true;
   } else {
     // groups side by side: 128 bytes of a position, more while a sample has less than a wavefront's pieces
     const int g_most = std::min(pow2_up(p.groups), kMaxLanes / q.SP);
@@ -783,7 +805,7 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
       const uint32_t fill = std::max(1u, 256u * (1024u / (uint32_t)q.threads) / q.chunks), all = q.work / q.chunks;
       q.row_count = (int64_t)q.threads / q.D * q.PL * q.NP >= 64 && all <= 4096 ? all : std::min(all, fill);
       // little work is one workgroup's per chunk: its sums are dgamma and dbeta, and the launch that adds shares is spared
-      if (!q.split && all <= 4) q.row_count = 1;
+      if (!q.split && all <= 4 && (all - 1) * q.NP <= 8) q.row_count = 1;
       q.blocks = q.row_count * q.chunks;
     } else {
       q.blocks = std::min(q.work, 1u << 20);
@@ -796,11 +818,11 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
   return q;
 }
 
-// the widest piece that a group is a whole number of (at any pitch and alignment)
+// A piece's elements, at any pitch and alignment: as many as fit, where a group is a whole number of them; other groups end in a
+// piece that is partly theirs, of four elements (two for groups of two and three).  (@@)
 int norm_piece(const abs_group_norm& p, bool backward) {
-  int V = norm_widest(p, backward);
-  while (p.channels / p.groups % V) V /= 2;
-  return V;
+  const int per = p.channels / p.groups, most = norm_widest(p, backward);
+  return per % most == 0 ? most : per >= 4 ? 4 : per >= 2 ? 2 : 1;
 }
 
 const char* norm_problem(const abs_group_norm* p, bool backward) {
@@ -829,51 +851,50 @@ void norm_fill(NormArgs<T>& a, const abs_group_norm& p, const NormPlan& q, char*
   a.part = (float*)ws;
 }
 
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 hipError_t norm_forward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
   const dim3 grid(q.blocks), block((unsigned)q.threads);
-  if constexpr (V == 1) {
-    if (q.CV == kWide) { norm_forward_kernel<T, 1, 1, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
-  }
-#define ABS_NORM_F(NP_)                                                             \
-  if (q.NP == NP_) {                                                                \
-    if (q.split) norm_forward_kernel<T, V, NP_, 1, false><<<grid, block, 0, s>>>(a); \
-    else         norm_forward_kernel<T, V, NP_, 1, true><<<grid, block, 0, s>>>(a);  \
+#define ABS_NORM_F(NP_)                                                               \
+  if (q.NP == NP_) {                                                                  \
+    if (q.split) norm_forward_kernel<T, V, NP_, false, TAIL><<<grid, block, 0, s>>>(a); \
+    else         norm_forward_kernel<T, V, NP_, true, TAIL><<<grid, block, 0, s>>>(a);  \
   }
   ABS_NORM_F(1) ABS_NORM_F(4) ABS_NORM_F(16)
 #undef ABS_NORM_F
   if (q.split) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    norm_apply_kernel<T, V><<<grid, block, 0, s>>>(a);
+    norm_apply_kernel<T, V, TAIL><<<grid, block, 0, s>>>(a);
   }
   return hipGetLastError();
 }
 
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
   const dim3 grid(q.blocks), block((unsigned)q.threads);
   const int stack = q.threads / std::max(q.TX, 64);
-  const size_t lds = q.NP * V >= 32                      ? (size_t)q.threads * V * 8        // (kLean; 32 KB at most either way)
-                     : a.rows_g && q.CV == 1 && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;
-  if constexpr (V == 1) {
-    if (q.CV == kWide) { norm_backward_kernel<T, 1, 1, kWide, true><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
-  }
-#define ABS_NORM_B(NP_)                                                                  \
-  if (q.NP == NP_) {                                                                     \
-    if (q.split) norm_backward_kernel<T, V, NP_, 1, false><<<grid, block, lds, s>>>(a);  \
-    else         norm_backward_kernel<T, V, NP_, 1, true><<<grid, block, lds, s>>>(a);   \
+  const size_t lds = q.NP * V >= 32          ? (size_t)q.threads * V * 8        // (kLean; 32 KB at most either way)
+                     : a.rows_g && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;
+#define ABS_NORM_B(NP_)                                                                    \
+  if (q.NP == NP_) {                                                                       \
+    if (q.split) norm_backward_kernel<T, V, NP_, false, TAIL><<<grid, block, lds, s>>>(a);  \
+    else         norm_backward_kernel<T, V, NP_, true, TAIL><<<grid, block, lds, s>>>(a);   \
   }
   ABS_NORM_B(1)
-  if constexpr (V <= 4) { ABS_NORM_B(4) ABS_NORM_B(8) }
+  if constexpr (V <= 4) { ABS_NORM_B(4) ABS_NORM_B(8) }        // (pieces of 8 are for single positions)
 #undef ABS_NORM_B
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && q.split) {
     const dim3 all(std::min(a.work, 1u << 20));
-    norm_backward_apply_kernel<T, V><<<all, block, 0, s>>>(a);
+    norm_backward_apply_kernel<T, V, TAIL><<<all, block, 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;
+}
+
+template <typename T, int V, bool TAIL>
+hipError_t norm_either(bool backward, const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
+  return backward ? norm_backward_v<T, V, TAIL>(a, q, s) : norm_forward_v<T, V, TAIL>(a, q, s);
 }
 
 template <typename T>
@@ -901,11 +922,11 @@ hipError_t norm_run(const abs_group_norm& p, bool backward, NormArgs<T> a, const
   } else {
     switch (q.V) {
       case 8:
-        if constexpr (sizeof(T) == 2) e = backward ? norm_backward_v<T, 8>(a, q, s) : norm_forward_v<T, 8>(a, q, s);
+        if constexpr (sizeof(T) == 2) e = norm_either<T, 8, false>(backward, a, q, s);
         break;
-      case 4: e = backward ? norm_backward_v<T, 4>(a, q, s) : norm_forward_v<T, 4>(a, q, s); break;
-      case 2: e = backward ? norm_backward_v<T, 2>(a, q, s) : norm_forward_v<T, 2>(a, q, s); break;
-      default: e = backward ? norm_backward_v<T, 1>(a, q, s) : norm_forward_v<T, 1>(a, q, s); break;
+      case 4: e = q.tail ? norm_either<T, 4, true>(backward, a, q, s) : norm_either<T, 4, false>(backward, a, q, s); break;
+      case 2: e = q.tail ? norm_either<T, 2, true>(backward, a, q, s) : norm_either<T, 2, false>(backward, a, q, s); break;
+      default: e = norm_either<T, 1, false>(backward, a, q, s);
     }
   }
   if (e == hipSuccess && a.rows_g && q.row_count > 1) {

@@ -153,6 +153,10 @@ def test_linear_offsets_beyond_32_bits(dtype):
 NORMS = [(1, 1, 1, 1), (3, 1, 8, 8), (5, 1, 48, 4), (2, 7, 6, 2), (4, 9, 24, 6), (3, 196, 24, 6), (2, 49, 33, 11), (130, 1, 256, 32),
          (6, 1, 2048, 32), (7, 1, 2048, 1), (3, 1, 1143, 3), (2, 1, 1500, 1), (2, 3, 1500, 1), (1, 1, 40000, 2), (2, 64, 512, 8),
          (1, 1024, 64, 32), (2, 1000, 320, 32), (1, 5000, 8, 1), (3, 300, 130, 1), (1, 40000, 16, 4), (70, 33, 12, 3)]
+# groups that are no whole number of pieces: partial pieces of one to three, one that is alone in a wavefront, samples cut into parts
+PARTIAL = [(3, 50, 10, 2), (2, 300, 69, 1), (2, 40, 771, 3), (1, 3000, 85, 5), (2, 9000, 7, 1), (5, 1, 4099, 1), (9, 1, 129, 3),
+           (2, 20000, 14, 2), (40, 1, 9, 3), (1, 700, 1030, 2)]
+NORMS += PARTIAL
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -180,10 +184,10 @@ def test_group_norm_backward(n, S, C, G, dtype):
         got = lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=a, residual=r)
         for g, v, s, name in zip(got, *ou.norm_gradient(x, gamma, beta, mean, rstd, dy, r, a), ("dx", "dgamma", "dbeta")):
             ou.close(g, v, s, f"{name}, act {a}")
-    # relu: the side of the corner is that of h in fp32, rounded after every operation
+    # relu: the side of the corner is that of fma(x - mean, gamma rstd, beta), both factors rounded to fp32 (a product of two is exact in fp64)
     got = lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=RELU)
     wide = lambda t: t.repeat_interleave(C // G, 1)[:, None, :]
-    h = ((x.float() - wide(mean)) * wide(rstd)) * gamma + beta
+    h = (x.float() - wide(mean)).double() * (wide(rstd) * gamma).double() + beta.double()
     masked = dy * (h > 0)
     for g, v, s, name in zip(got, *ou.norm_gradient(x, gamma, beta, mean, rstd, masked, None, NONE), ("dx", "dgamma", "dbeta")):
         ou.close(g, v, s, f"{name}, relu")
@@ -220,6 +224,40 @@ def test_group_norm_in_place_and_images():
     got, _, _ = lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=SILU, residual=res, out=res)
     assert torch.equal(got, dx) and got is res
     assert torch.equal(lib.group_norm_forward(x, gamma, beta, 4, act=RELU, out=x)[0], y) and torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,S,C,G", PARTIAL)
+def test_group_norm_in_place_partial_pieces(n, S, C, G, dtype):
+    x, dy, res = (torch.randn(n, S, C, device="cuda").to(dtype) for _ in range(3))
+    gamma, beta = torch.randn(C, device="cuda"), torch.randn(C, device="cuda")
+    y, mean, rstd = lib.group_norm_forward(x, gamma, beta, G, act=SILU)
+    dx, dgamma, dbeta = lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=SILU, residual=res)
+    got = lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=SILU, residual=res, out=res)
+    assert torch.equal(got[0], dx) and got[0] is res and torch.equal(got[1], dgamma) and torch.equal(got[2], dbeta)
+    lib.group_norm_forward(x, gamma, beta, G, act=SILU, out=x)
+    assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("C,G", [(10, 2), (69, 1), (771, 3), (9, 3)])
+def test_group_norm_partial_pieces_stay_inside(C, G, dtype):
+    """Rows in longer rows whose other columns are NaN, the first one at the start of its memory, the last one at its end."""
+    n, S = 2, 37
+    flat = [torch.full((n * S * (C + 5) - 5,), float("nan"), dtype=dtype, device="cuda") for _ in range(4)]
+    x, dy, res, out = (f.as_strided((n, S, C), (S * (C + 5), C + 5, 1)) for f in flat)
+    for v in (x, dy, res):
+        v.copy_(torch.randn(n, S, C, device="cuda"))
+    gamma, beta = 1 + 0.3 * torch.randn(C, device="cuda"), 0.3 * torch.randn(C, device="cuda")
+    got = lib.group_norm_forward(x, gamma, beta, G, act=SILU, out=out)
+    for g, v, s in zip(got, *ou.norm(x, gamma, beta, G, 1e-5, SILU)):
+        ou.close(g, v, s)
+    grads = lib.group_norm_backward(x, gamma, beta, got[1], got[2], dy, act=SILU, residual=res, out=out)
+    for g, v, s in zip(grads, *ou.norm_gradient(x, gamma, beta, got[1], got[2], dy, res, SILU)):
+        ou.close(g, v, s)
+    rest = torch.ones_like(flat[3], dtype=torch.bool)
+    rest.as_strided((n, S, C), (S * (C + 5), C + 5, 1)).fill_(False)
+    assert torch.isnan(flat[3][rest]).all()
 
 
 def test_group_norm_far_from_zero():
