@@ -595,11 +595,13 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
     const T* pd = a.dy + at * a.lddy + col;
     const T* pr = a.dres ? a.dres + at * a.lddres + col : nullptr;
     T* dst = a.y + at * a.ldy + col;
-#pragma unroll 2
+    const int early = TAIL ? V - q.nv : 0;                    // (dx may be dres, never x or dy)
+#pragma unroll 4
     for (int pos = q.p; pos < count_pos; pos += a.PL) {
       Vec vx, vd, o, r;
-      load_own<TAIL>(vx, px, q.nv); load_own<TAIL>(vd, pd, q.nv);
+      vx.load(px - early); vd.load(pd - early);
       if (pr) load_own<TAIL>(r, pr, q.nv);
+      if (TAIL) { move_down(vx, q.nv); move_down(vd, q.nv); }
       float d[V], dh[V];
       norm_dh<T, V>(vx, vd, mean, sc, bet, a.act, d, dh);
 #pragma unroll
@@ -622,6 +624,7 @@ __global__ __launch_bounds__(1024) void norm_share_sum_kernel(const float* rows,
   const float* p = rows + (blockIdx.y ? C : 0) + c;
   float v = 0.f;
   if (c < C)
+#pragma unroll 8
     for (uint32_t k = r; k < row_count; k += 32) v += p[(int64_t)k * 2 * C];
   s[r][threadIdx.x & 31] = v;
   __syncthreads();
@@ -819,7 +822,9 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
 }
 
 // A piece's elements, at any pitch and alignment: as many as fit, where a group is a whole number of them; other groups end in a
-// piece that is partly theirs, of four elements (two for groups of two and three).  (@@)
+// piece that is partly theirs, of four elements (two for groups of two and three).  Backward eight only for single positions: the sums and
+// parameters of a piece's channels fill the registers that more positions need.  (bf16 gradients, four and a part against single elements:
+// 47 x 2116 x 69 in one group 53 and 103 us, 1622 x 289 x 10 in two 46 and 79; eight against four: 8192 x 2048 in 32 groups 44 and 47.)
 int norm_piece(const abs_group_norm& p, bool backward) {
   const int per = p.channels / p.groups, most = norm_widest(p, backward);
   return per % most == 0 ? most : per >= 4 ? 4 : per >= 2 ? 2 : 1;
@@ -875,21 +880,25 @@ hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t 
   const int stack = q.threads / std::max(q.TX, 64);
   const size_t lds = q.NP * V >= 32          ? (size_t)q.threads * V * 8        // (kLean; 32 KB at most either way)
                      : a.rows_g && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;
+  if constexpr (V == 8) {                                      // (single positions, never split)
+    norm_backward_kernel<T, V, 1, true, TAIL><<<grid, block, lds, s>>>(a);
+    return hipGetLastError();
+  } else {
 #define ABS_NORM_B(NP_)                                                                    \
   if (q.NP == NP_) {                                                                       \
     if (q.split) norm_backward_kernel<T, V, NP_, false, TAIL><<<grid, block, lds, s>>>(a);  \
     else         norm_backward_kernel<T, V, NP_, true, TAIL><<<grid, block, lds, s>>>(a);   \
   }
-  ABS_NORM_B(1)
-  if constexpr (V <= 4) { ABS_NORM_B(4) ABS_NORM_B(8) }        // (pieces of 8 are for single positions)
+    ABS_NORM_B(1) ABS_NORM_B(4) ABS_NORM_B(8)
 #undef ABS_NORM_B
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && q.split) {
-    const dim3 all(std::min(a.work, 1u << 20));
-    norm_backward_apply_kernel<T, V, TAIL><<<all, block, 0, s>>>(a);
-    e = hipGetLastError();
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && q.split) {
+      const dim3 all(std::min(a.work, 1u << 20));
+      norm_backward_apply_kernel<T, V, TAIL><<<all, block, 0, s>>>(a);
+      e = hipGetLastError();
+    }
+    return e;
   }
-  return e;
 }
 
 template <typename T, int V, bool TAIL>
