@@ -362,9 +362,9 @@ int abs_calibrate_mfma(int32_t data_mode, int32_t iters, int32_t workgroups, flo
                        void* hip_stream, double* h_ms, double* h_tflops);
 
 /*
- * Operators of a network's hidden layers (abs_create_blocks' networks are made of them): the product of a layer with bias, activation and residual in one
- * pass, group normalisation with an activation behind it, and dropout whose mask is a function of a counter;
- * each with its gradient.  They need no handle: sizes travel in a small struct, matrices are row-major DEVICE
+ * Operators of a network's hidden layers (abs_create_blocks' networks are made of them): the product of a layer with
+ * bias, activation and residual in one pass, group normalisation with an activation behind it, and dropout whose mask
+ * is a function of a counter; each with its gradient.  They need no handle: sizes travel in a small struct, matrices are row-major DEVICE
  * arrays owned by the caller with a row pitch in elements (ld*, at least the row's length), in the dtype the
  * struct names (ABS_X_FP32 or ABS_X_BF16; biases, gamma, beta, saved statistics and their gradients are always
  * fp32).  Any size, pitch and alignment that the elements allow is taken (a large product of matrices whose rows'
@@ -384,11 +384,12 @@ enum { ABS_ACT_NONE = 0, ABS_ACT_RELU = 1, ABS_ACT_SILU = 2, ABS_ACT_GELU = 3 };
 /*
  * z = x W + b,  y = act(z) + r, with x [rows, d_in], W [d_in, d_out], b [d_out] (may be NULL), r [rows, d_out]
  * (may be NULL), y and z [rows, d_out] (z may be NULL; a backward pass of a layer with an activation needs it).
- * rows >= 0, 1 <= d_in, d_out <= 2^20, rows < 2^31.
+ * rows >= 0, 1 <= d_in, d_out <= 2^20, rows < 2^31, pitches below 2^32, at most 2^22 tiles of 128 x 128 in y, dx or dW.
  * The backward pass, for a gradient dy [rows, d_out] of y:  dz = dy act'(z) (relu: 0 where z is not positive;
  * d_z may be NULL for ABS_ACT_NONE),  dx = dz W^T, dW = x^T dz, db = sum of dz over the rows; the residual's
  * gradient is dy itself.  d_dx, d_dw, d_db: any of them may be NULL, then it is not computed.  With bf16
- * operands dz is rounded to bf16 once, for the matrix cores; db is summed from the unrounded values.  d_y may be d_r (each element is read before it is written).
+ * operands dz is rounded to bf16 once, for the matrix cores; db is summed from the unrounded values.  d_y may be d_r
+ * with the same pitch (each element is read before it is written).
  */
 typedef struct abs_linear {
   int32_t dtype;
@@ -413,7 +414,7 @@ int abs_linear_backward(const abs_linear* p, const void* d_x, const void* d_w, c
  *   h = (x - mean) rstd gamma + beta,  y = act(h).
  * d_gamma, d_beta fp32 [channels] (both may be NULL: 1 and 0); d_mean, d_rstd fp32 [n, groups] are outputs (both may
  * be NULL).  groups = 1 with spatial = 1 is layer normalisation.  n >= 0, spatial >= 1, n spatial < 2^31,
- * 1 <= channels <= 2^20; d_y may be d_x with the same pitch.
+ * 1 <= channels <= 2^20, pitches below 2^40; d_y may be d_x with the same pitch.
  * The backward pass, for a gradient dy of y, with mean and rstd of the forward pass:  dh = dy act'(h),
  *   dx = rstd (dh gamma - mean_m(dh gamma) - xhat mean_m(dh gamma xhat)) + dres,
  *   dgamma = sum over samples and positions of dh xhat, dbeta = the same of dh,

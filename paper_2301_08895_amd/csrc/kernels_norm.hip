@@ -806,7 +806,8 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
       // as many workgroups as the CUs hold at once (1024 lanes each by their registers); a workgroup per share where a share has
       // so many positions that its two numbers per channel do not count
       const uint32_t fill = std::max(1u, 256u * (1024u / (uint32_t)q.threads) / q.chunks), all = q.work / q.chunks;
-      q.row_count = (int64_t)q.threads / q.D * q.PL * q.NP >= 64 && all <= 4096 ? all : std::min(all, fill);
+      const bool fits = (int64_t)all * q.chunks * q.threads < 1ll << 32;                              // (a launch's threads)
+      q.row_count = (int64_t)q.threads / q.D * q.PL * q.NP >= 64 && all <= 4096 && fits ? all : std::min(all, fill);
       // little work is one workgroup's per chunk: its sums are dgamma and dbeta, and the launch that adds shares is spared
       if (!q.split && all <= 4 && (all - 1) * q.NP <= 8) q.row_count = 1;
       q.blocks = q.row_count * q.chunks;

@@ -1,5 +1,7 @@
 """The operators of a network's hidden layers on the GPU against their plain forms in 64 bits (operator_util.py, with the
 tolerances' derivation), at the sizes, pitches and values where they can go wrong."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -97,6 +99,33 @@ def test_linear_of_many_tiles(rows, d_in, d_out, act):
     got = lib.linear_backward(x, w, dy, act=act, z=z)
     for g, v, s, name in zip(got, *ou.linear_gradient(x, w, z, dy, act), ("dx", "dw", "db")):
         ou.close(g, v, s, name)
+
+
+# tiles of 128 x 128: one run, contractions in shares, dx and dW side by side
+TILED = [(BF, 2048, 2048, 2048), (BF, 4096, 1024, 1024), (BF, 8192, 1024, 512), (BF, 256, 4096, 4096), (BF, 3000, 1100, 1064),
+         (F32, 4096, 512, 1000), (F32, 300, 2048, 2052), (F32, 1300, 1100, 1060)]
+
+
+@pytest.mark.parametrize("dtype,rows,d_in,d_out", TILED)
+def test_linear_tiled(dtype, rows, d_in, d_out):
+    x, w = rows_of(rows, d_in, dtype), rows_of(d_in, d_out, dtype, scale=d_in ** -0.5)
+    b, r = torch.randn(d_out, device="cuda"), rows_of(rows, d_out, dtype)
+    want, wz, sy, sz = ou.linear(x, w, b, SILU, r)
+    y, z = lib.linear_forward(x, w, b, act=SILU, residual=r, keep_z=True, out=r)
+    assert y is r
+    ou.close(z, wz, sz, "z")
+    ou.close(y, want, sy, "y over the residual")
+    dy = rows_of(rows, d_out, dtype)
+    want, slack = ou.linear_gradient(x, w, z, dy, SILU)
+    got = lib.linear_backward(x, w, dy, act=SILU, z=z)
+    for g, v, s, name in zip(got, want, slack, ("dx", "dw", "db")):
+        ou.close(g, v, s, name)
+    for needs in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (0, 0, 0)):
+        some = lib.linear_backward(x, w, dy, act=SILU, z=z, need_dx=bool(needs[0]), need_dw=bool(needs[1]), need_db=bool(needs[2]))
+        for g, v, s, need in zip(some, want, slack, needs):
+            assert (g is not None) == bool(need)
+            if need:
+                ou.close(g, v, s, f"of {needs}")
 
 
 def test_linear_of_no_rows():
@@ -451,9 +480,37 @@ def test_two_runs_give_the_same_bits_on_any_stream(rows, d, groups, dtype):
         assert torch.equal(p, q)
 
 
-def test_captured_and_replayed():
+def test_two_threads_on_two_streams():
+    """Calls of both at once, each with workspaces of its own: the bits of calls one after the other."""
+    blocks = [Block(1500, 1032, 24, BF), Block(700, 516, 12, F32)]
+    want = [blk.run() for blk in blocks]
+    torch.cuda.synchronize()
+    got, wrong = [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(5):
+                    got[i] = blocks[i].run()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:                                     # (reported in the test's own thread)
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not wrong, wrong
+    for a, b in zip(got, want):
+        for p, q in zip(a, b):
+            assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("rows,d,groups,dtype", [(260, 128, 16, BF), (2100, 1024, 16, BF), (1200, 1028, 4, F32)])
+def test_captured_and_replayed(rows, d, groups, dtype):
     """Forward and backward of a block in a graph: every replay on new inputs gives the eager call's bits, with eager work between."""
-    blk = Block(260, 128, 16, BF)
+    blk = Block(rows, d, groups, dtype)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
@@ -463,8 +520,8 @@ def test_captured_and_replayed():
     with torch.cuda.graph(graph):
         got = blk.run()
     for i in range(4):
-        blk.a.copy_(torch.randn(260, 128, device="cuda"))
-        blk.dy.copy_(torch.randn(260, 128, device="cuda"))
+        blk.a.copy_(torch.randn(rows, d, device="cuda"))
+        blk.dy.copy_(torch.randn(rows, d, device="cuda"))
         want = blk.run()
         torch.cuda.synchronize()
         graph.replay()
