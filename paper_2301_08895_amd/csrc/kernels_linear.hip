@@ -695,9 +695,10 @@ struct ColumnPart<float> {
 template <typename T>
 struct DzSource { const T* dy; const T* z; int64_t lddy, ldz; int act; };
 
-// Tiles of one of the products; its contraction in `splits` shares of `steps` blocks each, which leave in fp32 to be joined.
+// Tiles of one of the products, 8 / team in a workgroup (one above the other, `team` wavefronts each); its contraction in `splits`
+// shares of `steps` blocks each, which leave in fp32 to be joined.  tiles: workgroups' worth.
 template <typename T>
-struct SmallPart { Epilogue<T> e; int nt, tiles, splits, steps; };
+struct SmallPart { Epilogue<T> e; int nt, tiles, splits, steps, team; };
 template <typename T>
 struct SmallArgs {
   const T* x; const T* w;
@@ -709,13 +710,14 @@ struct SmallArgs {
   bool dw;
 };
 
-// 32 rows of the partial results of all wavefronts, added in their order, and what follows
+// 32 rows of the partial results of every team's wavefronts, added in their order, and what follows.  Tile `i` of the workgroup has rows
+// m0 + i m_tile, ... + m_step each.
 template <typename T>
-__device__ __forceinline__ void small_finish(const Epilogue<T>& e, const f32x16_t& a0, const f32x16_t& a1, float* red, int waves, int64_t m0,
-                                             int m_step, int64_t M, int64_t n0, int64_t N) {
+__device__ __forceinline__ void small_finish(const Epilogue<T>& e, const f32x16_t& a0, const f32x16_t& a1, float* red, int team, int waves,
+                                             int64_t m0, int m_tile, int m_step, int64_t M, int64_t n0, int64_t N) {
   constexpr int kPitch = 64 + 4, V = kPiece<T>, LPR = 64 / V;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  if (wave < waves) {
+  if ((wave & (team - 1)) < waves) {
     float* q = red + (wave * 32 + (lane & 31)) * kPitch + 8 * (lane >> 5);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {       // registers 4 b .. of a0 / a1: even / odd columns 2 (8 b + 4 (lane / 32) + r)
@@ -724,42 +726,44 @@ __device__ __forceinline__ void small_finish(const Epilogue<T>& e, const f32x16_
     }
   }
   __syncthreads();
-  for (int r = t / LPR; r < 32; r += 512 / LPR) {
+  for (int j = t / LPR; j < 32 * (kSmallWaves / team); j += 512 / LPR) {
+    const int i = j >> 5, r = j & 31;
     float v[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = 0.f;
-    const float* q = red + r * kPitch + (t % LPR) * V;
+    for (int k = 0; k < V; ++k) v[k] = 0.f;
+    const float* q = red + (i * team * 32 + r) * kPitch + (t % LPR) * V;
     for (int w = 0; w < waves; ++w)
 #pragma unroll
       for (int h = 0; h < V / 4; ++h) {
         const f32x4_t s = *(const f32x4_t*)(q + w * 32 * kPitch + 4 * h);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[4 * h + i] += s[i];
+        for (int k = 0; k < 4; ++k) v[4 * h + k] += s[k];
       }
-    const int64_t m = m0 + (int64_t)r * m_step;
+    const int64_t m = m0 + (int64_t)i * m_tile + (int64_t)r * m_step;
     if (m < M) finish(e, m, n0 + (t % LPR) * V, N, v);
   }
 }
 
-// A wavefront's blocks first, first + 8, ... of the contraction, U at a time: all their loads stand before the first use.
+// A wavefront's blocks first, first + team, ... of the contraction, U at a time: all their loads stand before the first use.
 template <int U, typename Step, typename Load, typename Use>
-__device__ __forceinline__ void in_steps(int first, int blocks, Load load, Use use) {
+__device__ __forceinline__ void in_steps(int first, int team, int blocks, Load load, Use use) {
   int kb = first;
-  for (; kb + (U - 1) * kSmallWaves < blocks; kb += U * kSmallWaves) {
+  for (; kb + (U - 1) * team < blocks; kb += U * team) {
     Step s[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(kb + u * kSmallWaves, s[u]);
+    for (int u = 0; u < U; ++u) load(kb + u * team, s[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) use(s[u]);
   }
-  for (; kb < blocks; kb += kSmallWaves) {
+  for (; kb < blocks; kb += team) {
     Step s;
     load(kb, s);
     use(s);
   }
 }
 
-template <typename T, bool BACKWARD>
+// TEAM: 8, which spares address arithmetic (1 x 2048 x 2048 7.4 us against 8.5), or 0, whatever the parts say.
+template <typename T, bool BACKWARD, int TEAM>
 __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
   constexpr int R = kPiece<T>;
   __shared__ __attribute__((aligned(16))) float red[kSmallWaves * 32 * 68];
@@ -772,7 +776,7 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   // this workgroup's tile, share of the contraction and blocks of it
-  int n0, tm, first, blocks, waves, split;
+  int n0, tm, first, blocks, waves, split, team = TEAM, at, mate;             // at: this wavefront's tile of the workgroup's, mate: its number there
   auto place = [&](const SmallPart<T>& part, int id, int K) {
     split = part.splits > 1 ? id / part.tiles : 0;
     const int tile = id - split * part.tiles;
@@ -780,7 +784,10 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
     n0 = (tile - tm * part.nt) * 64;
     first = split * part.steps;
     blocks = min((K + kBlockK<T> - 1) / kBlockK<T>, first + part.steps);
-    waves = min(kSmallWaves, blocks - first);
+    if (TEAM == 0) team = part.team;
+    waves = min(team, blocks - first);
+    at = wave / team;
+    mate = wave & (team - 1);
   };
   auto epilogue = [&](const SmallPart<T>& part) {
     Epilogue<T> e = part.e;
@@ -790,11 +797,11 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
   if constexpr (!BACKWARD) {
     const int K = g.d_in;
     place(g.a, blockIdx.x, K);
-    const int m0 = tm * 32;
-    const T* const xr = g.x + (int64_t)min(m0 + l32, g.rows - 1) * g.ldx;
+    const int m0 = tm * (32 * kSmallWaves / team);
+    const T* const xr = g.x + (int64_t)min(m0 + at * 32 + l32, g.rows - 1) * g.ldx;
     struct Step { RowPart<T> a; ColumnPart<T> b; };
     const ColumnPlace c = column_place(n0 + 2 * l32, g.d_out);
-    in_steps<4, Step>(first + wave, blocks,
+    in_steps<4, Step>(first + mate, team, blocks,
         [&](int kb, Step& s) {
           const int k = kb * kBlockK<T> + lk * R;
           s.a.load(xr, k, K);
@@ -804,21 +811,21 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
           acc[0][0] = multiply(s.b.frag(0), s.a.frag(), acc[0][0]);
           acc[0][1] = multiply(s.b.frag(1), s.a.frag(), acc[0][1]);
         });
-    small_finish<T>(epilogue(g.a), acc[0][0], acc[0][1], red, waves, m0, 1, g.rows, n0, g.d_out);
+    small_finish<T>(epilogue(g.a), acc[0][0], acc[0][1], red, team, waves, m0, 32, 1, g.rows, n0, g.d_out);
     return;
   }
   const int dx_blocks = g.a.tiles * g.a.splits;
   if ((int)blockIdx.x < dx_blocks) {                        // dx = dz W^T
     const int K = g.d_out;
     place(g.a, blockIdx.x, K);
-    const int m0 = tm * 32;
-    const int64_t row = min(m0 + l32, g.rows - 1);
+    const int m0 = tm * (32 * kSmallWaves / team);
+    const int64_t row = min(m0 + at * 32 + l32, g.rows - 1);
     const T* const dr = g.dz.dy + row * g.dz.lddy;
     const T* const zr = g.dz.z + row * g.dz.ldz;
     const T* const w0 = g.w + (int64_t)min(n0 + 2 * l32, g.d_in - 1) * g.ldw;
     const T* const w1 = g.w + (int64_t)min(n0 + 2 * l32 + 1, g.d_in - 1) * g.ldw;
     struct Step { RowPart<T> a, z, b0, b1; };
-    in_steps<4, Step>(first + wave, blocks,
+    in_steps<4, Step>(first + mate, team, blocks,
         [&](int kb, Step& s) {
           const int k = kb * kBlockK<T> + lk * R;
           s.a.load(dr, k, K);
@@ -831,17 +838,17 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
           acc[0][0] = multiply(s.b0.frag(), s.a.frag(), acc[0][0]);
           acc[0][1] = multiply(s.b1.frag(), s.a.frag(), acc[0][1]);
         });
-    small_finish<T>(epilogue(g.a), acc[0][0], acc[0][1], red, waves, m0, 1, g.rows, n0, g.d_in);
+    small_finish<T>(epilogue(g.a), acc[0][0], acc[0][1], red, team, waves, m0, 32, 1, g.rows, n0, g.d_in);
     return;
   }
   // dW = x^T dz, and db in the first row of tiles
   const int K = g.rows;
   place(g.b, (int)blockIdx.x - dx_blocks, K);
-  const int m0 = tm * 64;
+  const int m0 = tm * (64 * kSmallWaves / team);
   float s0 = 0.f, s1 = 0.f;
   struct Step { ColumnPart<T> a, b, z; };
-  const ColumnPlace ca = column_place(m0 + 2 * l32, g.d_in), cb = column_place(n0 + 2 * l32, g.d_out);
-  in_steps<2, Step>(first + wave, blocks,
+  const ColumnPlace ca = column_place(m0 + at * 64 + 2 * l32, g.d_in), cb = column_place(n0 + 2 * l32, g.d_out);
+  in_steps<2, Step>(first + mate, team, blocks,
       [&](int kb, Step& s) {
         const int k = kb * kBlockK<T> + lk * R;
         s.a.load(g.x, g.ldx, k, K, ca, g.d_in);
@@ -874,7 +881,7 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {                             // rows m0 + i, m0 + i + 2, ...
     if (i) __syncthreads();
-    small_finish<T>(e, acc[i][0], acc[i][1], red, waves, m0 + i, 2, g.d_in, n0, g.d_out);
+    small_finish<T>(e, acc[i][0], acc[i][1], red, team, waves, m0 + i, 64, 2, g.d_in, n0, g.d_out);
   }
 }
 
@@ -975,7 +982,8 @@ Product cut_product(int64_t M, int64_t N, int64_t K, int dtype, bool big, int64_
   if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
   return q;
 }
-constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16};
+constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+bool cut_counts(const Product& q, int split) { return q.nsplit == split && (split == 1 || (q.steps_per_split >= 4 && (int64_t)q.mt * q.nt * split <= 2048)); }
 
 Product plan_product(int64_t M, int64_t N, int64_t K, int dtype, double* cost_out) {
   const TileCost c = tile_cost(dtype);
@@ -984,7 +992,7 @@ Product plan_product(int64_t M, int64_t N, int64_t K, int dtype, double* cost_ou
   for (int big = dtype == ABS_X_BF16 ? 1 : 0; big >= 0; --big)
     for (int split : kCuts) {
       const Product q = cut_product(M, N, K, dtype, big != 0, split);
-      if (q.nsplit != split || (split > 1 && q.steps_per_split < 4)) continue;
+      if (!cut_counts(q, split)) continue;
       const double units = (double)q.mt * q.nt * q.nsplit, steps = q.steps_per_split;
       const double us = (big ? std::ceil(units / 256) * (c.big_start + c.big_step * steps)
                              : units <= 256 ? c.start + c.step * steps : std::ceil(units / 512) * (c.start2 + c.step2 * steps)) +
@@ -1016,31 +1024,39 @@ bool plan_pair(const abs_linear& p, double apart, Product& dx, Product& dw) {
   double least = apart + 3;                                       // (their two launches' gap)
   bool found = false;
   for (int big = p.dtype == ABS_X_BF16 ? 1 : 0; big >= 0; --big)
-    for (int sa : kCuts)
+    for (int sa : kCuts) {
+      const Product a = cut_product(p.rows, p.d_in, p.d_out, p.dtype, big != 0, sa);
+      if (!cut_counts(a, sa)) continue;
       for (int sb : kCuts) {
-        const Product a = cut_product(p.rows, p.d_in, p.d_out, p.dtype, big != 0, sa), b = cut_product(p.d_in, p.d_out, p.rows, p.dtype, big != 0, sb);
-        if (a.nsplit != sa || b.nsplit != sb || (sa > 1 && a.steps_per_split < 4) || (sb > 1 && b.steps_per_split < 4)) continue;
-        const double start = big ? c.big_start : c.start2, step = big ? 1.15 * c.big_step : c.step2;
-        const double us = last_end((int64_t)b.mt * b.nt * sb, start + step * b.steps_per_split, (int64_t)a.mt * a.nt * sa,
-                                   start + step * a.steps_per_split, big ? 256 : 512) +
-                          std::max(join_cost(sa, p.rows, p.d_in), join_cost(sb, p.d_in, p.d_out));
+        const Product b = cut_product(p.d_in, p.d_out, p.rows, p.dtype, big != 0, sb);
+        if (!cut_counts(b, sb)) continue;
+        const double start = big ? c.big_start : c.start2, step = big ? 1.15 * c.big_step : c.step2, join = std::max(join_cost(sa, p.rows, p.d_in), join_cost(sb, p.d_in, p.d_out));
+        const double ta = start + step * a.steps_per_split, tb = start + step * b.steps_per_split;
+        const int64_t na = (int64_t)a.mt * a.nt * sa, nb = (int64_t)b.mt * b.nt * sb, slots = big ? 256 : 512;
+        if (join + std::max(std::max(ta, tb), (na * ta + nb * tb) / slots) >= least) continue;
+        const double us = join + last_end(nb, tb, na, ta, slots);
         if (us < least) { least = us; dx = a; dw = b; found = true; }
       }
+    }
   return found;
 }
 
 // Which products linear_small_kernel takes (us, it / the tile kernels with their copies, dz and joins; bf16 unless said).  Forward
-// 810 x 520 x 300 6.4 / 14.9, 1024^3 10.3 / 20.9, 2048 x 2048 x 512 20 / 24, 4096 x 1024 x 1024 32 / 20; fp32 2048 x 512 x 512
-// 22 / 27, 1024^3 38 / 35.  Backward 200 x 256 x 256 8.3 / 20, 1000^3 41 / 50, 4096 x 512 x 512 55 / 51, 2048 x 2048 x 512 91 / 38; fp32
-// 2048 x 512 x 512 52 / 59, 1000^3 83 / 75.  A dW of many tiles with few rows each is not for it: 8 x 4096 x 4096 80 / 35.
+// 810 x 520 x 300 6.4 / 24, 1024^3 10 / 21, 2048 x 2048 x 512 20 / 23, 4096 x 256 x 1024 12.5 / 10.9; fp32 2048 x 512 x 512 22 / 28,
+// 410 x 1736 x 1088 37 / 36, 1024^3 39 / 36.  Backward 512^3 11 / 17, 13556 x 176 x 94 35 / 36, 1024 x 512 x 512 24 / 19, 64 x 2048 x
+// 2048 21 / 20, 4096 x 512 x 512 52 / 30; fp32 1024 x 512 x 512 30 / 34, 2048 x 512 x 512 53 / 42.  Layers so narrow that dW is a tile
+// or two stay longer: 100000 x 64 x 64 53 / 65, fp32 73 / 175, 20000 x 64 x 512 71 / 111 (8192 x 256 x 256 55 / 45).  A dW of many tiles with
+// few rows each is not for it: 8 x 4096 x 4096 80 / 35.
 bool small_product(const abs_linear& p, bool backward) {
   const bool half = p.dtype == ABS_X_BF16;
   const double macs = (double)p.rows * p.d_in * p.d_out;
   if (p.d_in < 2 || p.d_out < 2) return false;                       // (columns are read in pairs)
-  return backward ? macs <= (half ? 1.1e9 : 8e8) && (double)p.d_in * p.d_out <= 4.3e6 : macs <= (half ? 2.2e9 : 9e8);
+  if (!backward) return macs <= (half ? 2.2e9 : 7.5e8);
+  const double width = (double)p.d_in * p.d_out;
+  return width <= 4.3e6 && macs <= (width <= (half ? 8192 : 40000) ? (half ? 8e8 : 1e9) : 3e8);
 }
 
-struct SmallProduct { int nt, tiles, splits, steps; size_t part_bytes; };
+struct SmallProduct { int nt, tiles, splits, steps, team; size_t part_bytes; };
 
 struct LinearPlan {
   bool small, pair, pack_x, pack_w, dz;
@@ -1073,6 +1089,12 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
       const int64_t shares = blocks <= (p.dtype == ABS_X_BF16 && rows_of_tile == 32 ? 4 : 2) * each ? 1 : std::max<int64_t>(1, std::min<int64_t>((blocks + each - 1) / each, 640 / s.tiles));
       s.steps = (int)((blocks + shares - 1) / shares);
       s.splits = (int)((blocks + s.steps - 1) / s.steps);
+      // several tiles in a workgroup: with blocks too few for eight wavefronts as long as every CU has a workgroup, else two
+      // (30000 x 300 x 20, gradients 81 -> 50 us; 2 x 645 x 23, whose few workgroups would do eight tiles' epilogues each, 8 -> 21)
+      const int64_t mt = (M + rows_of_tile - 1) / rows_of_tile, mine = std::min<int64_t>(blocks, s.steps);
+      s.team = kSmallWaves;
+      while (s.team > 1 && mt * s.nt * s.splits * (s.team / 2) >= (s.team / 2 >= mine ? 256 : 512) * kSmallWaves) s.team /= 2;
+      s.tiles = (int)((mt * s.team + kSmallWaves - 1) / kSmallWaves) * s.nt;
       s.part_bytes = s.splits > 1 ? op_round_up((size_t)s.splits * M * op_round_up(N, 4) * 4, 256) : 0;
       return s;
     };
@@ -1190,7 +1212,7 @@ SmallArgs<T> small_args(const abs_linear& p, const void* x, const void* w) {
 // one product of linear_small_kernel, and what joins its shares (join.shares stays 0 where there is one)
 template <typename T>
 SmallPart<T> small_part(const SmallProduct& q, const Epilogue<T>& e, float* part, int64_t M, int64_t N, Join<T>& join) {
-  SmallPart<T> s{e, q.nt, q.tiles, q.splits, q.steps};
+  SmallPart<T> s{e, q.nt, q.tiles, q.splits, q.steps, q.team};
   if (q.splits > 1) {
     s.e.part = part;
     s.e.ldpart = (int64_t)op_round_up(N, 4);
@@ -1210,7 +1232,9 @@ hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, 
     SmallArgs<T> g = small_args<T>(p, x, w);
     Join<T> join{};
     g.a = small_part(q.sa, e, (float*)(ws + q.off_part), p.rows, p.d_out, join);
-    linear_small_kernel<T, false><<<dim3((unsigned)(q.sa.tiles * q.sa.splits)), 512, 0, s>>>(g);
+    const dim3 grid((unsigned)(q.sa.tiles * q.sa.splits));
+    if (q.sa.team == kSmallWaves) linear_small_kernel<T, false, kSmallWaves><<<grid, 512, 0, s>>>(g);
+    else                          linear_small_kernel<T, false, 0><<<grid, 512, 0, s>>>(g);
     const hipError_t err = hipGetLastError();
     return err == hipSuccess ? launch_join(join, Join<T>{}, DbShares{}, s) : err;
   }
@@ -1249,7 +1273,9 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     }
     const int blocks = g.a.tiles * g.a.splits + g.b.tiles * g.b.splits;
     if (blocks == 0) return hipSuccess;
-    linear_small_kernel<T, true><<<dim3((unsigned)blocks), 512, 0, s>>>(g);
+    const dim3 grid((unsigned)blocks);
+    if (q.sa.team == kSmallWaves && q.sb.team == kSmallWaves) linear_small_kernel<T, true, kSmallWaves><<<grid, 512, 0, s>>>(g);
+    else                                                       linear_small_kernel<T, true, 0><<<grid, 512, 0, s>>>(g);
     err = hipGetLastError();
     return err == hipSuccess ? launch_join(ja, jb, d, s) : err;
   }
