@@ -886,11 +886,23 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
 }
 
 // ---------------------------------------------------------------------- dz = dy act'(z), and its column sums
-// 256 threads: 32 pieces of columns, 8 rows at a time; a workgroup's shares of the column sums leave in `sums` [gridDim.y][N].  Bound by
-// memory: 8192 x 2048 bf16 19 us, 5.3 TB/s, a large copy's rate.
-template <typename T, int V>
+// 256 threads: 32 pieces of columns, 8 rows at a time; a workgroup's shares of the column sums leave in `sums` [gridDim.y][N].  Rows of dz
+// are whole pieces (lddz), zeros from N on.  Bound by memory: 8192 x 2048 bf16 19 us, 5.3 TB/s, a large copy's rate.
+template <typename T>
+__device__ __forceinline__ void load_columns(Piece<T, kPiece<T>>& v, const T* p, int count) {
+  constexpr int V = kPiece<T>;
+  if (count >= V) { v.load(p); return; }
+  T e[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) e[i] = p[min(i, count - 1)];
+#pragma unroll
+  for (int i = 0; i < V; ++i) e[i] = i < count ? e[i] : T(0);
+  __builtin_memcpy(v.w, e, 16);
+}
+template <typename T>
 __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t lddy, const T* z, int64_t ldz, T* dz, int64_t lddz, int64_t rows,
                                                         int N, int act, float* sums) {
+  constexpr int V = kPiece<T>;
   __shared__ float red[8][32 * V + 1];
   const int t = threadIdx.x, c = t & 31, rl = t >> 5;
   const int n = ((int)blockIdx.x * 32 + c) * V;
@@ -901,8 +913,8 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t ldd
 #pragma unroll 2
     for (int64_t m = (int64_t)blockIdx.y * 8 + rl; m < rows; m += (int64_t)gridDim.y * 8) {
       Piece<T, V> d, h, o;
-      d.load(dy + m * lddy + n);
-      if (act != ABS_ACT_NONE) h.load(z + m * ldz + n);
+      load_columns(d, dy + m * lddy + n, N - n);
+      if (act != ABS_ACT_NONE) load_columns(h, z + m * ldz + n, N - n);
       float f[V], g[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) { f[e] = d.at(e); g[e] = act != ABS_ACT_NONE ? h.at(e) : 0.f; }
@@ -933,18 +945,21 @@ __global__ __launch_bounds__(256) void linear_db_kernel(DbShares d) { add_db(d);
 // ---------------------------------------------------------------------- an operand whose rows are not whole 16-byte pieces: a copy that is
 // (columns beyond the end are zero: they meet zeros or leave through columns that are not stored)
 template <typename T>
-__global__ __launch_bounds__(256) void linear_pack_kernel(const T* src, int64_t ld, int64_t rows, int64_t cols, T* dst, int64_t ldd) {
+struct Pack { const T* src; int64_t ld, rows, cols; T* dst; int64_t ldd; };
+template <typename T>
+__global__ __launch_bounds__(256) void linear_pack_kernel(Pack<T> first, Pack<T> second) {
   constexpr int V = kPiece<T>;
-  const int64_t pieces = ldd / V, total = rows * pieces;
+  const Pack<T>& p = blockIdx.y ? second : first;
+  const int64_t pieces = p.ldd / V, total = p.rows * pieces;
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
-    const int64_t m = q / pieces, c = (q - m * pieces) * V;
+    const int64_t m = total < 1ll << 32 ? (int64_t)((uint32_t)q / (uint32_t)pieces) : q / pieces, c = (q - m * pieces) * V;
     Loose<T, V> o;
-    if (c + V <= cols) o = *(const Loose<T, V>*)(src + m * ld + c);
+    if (c + V <= p.cols) o = *(const Loose<T, V>*)(p.src + m * p.ld + c);
     else {
 #pragma unroll
-      for (int e = 0; e < V; ++e) o.e[e] = c + e < cols ? src[m * ld + c + e] : T(0);
+      for (int e = 0; e < V; ++e) o.e[e] = c + e < p.cols ? p.src[m * p.ld + c + e] : T(0);
     }
-    *(Loose<T, V>*)(dst + m * ldd + c) = o;
+    *(Loose<T, V>*)(p.dst + m * p.ldd + c) = o;
   }
 }
 
@@ -1121,7 +1136,7 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     q.dz = p.act != ABS_ACT_NONE || !(dy_ok && p.d_out % piece == 0 && p.lddy % piece == 0);
     if (q.dz) q.off_dz = take((size_t)p.rows * q.out8 * size);
     // eight workgroups on every CU, 16 rows each at least
-    const int cols = p.d_out % piece == 0 ? (p.d_out / piece + 31) / 32 : (p.d_out + 31) / 32;
+    const int cols = (int)((q.out8 / piece + 31) / 32);
     q.sum_rows = (int)std::max<int64_t>(1, std::min<int64_t>((p.rows + 15) / 16, std::max(1, 2048 / cols)));
     q.off_sums = take((size_t)q.sum_rows * p.d_out * 4);
     double ca, cb;
@@ -1156,9 +1171,16 @@ const char* linear_problem(const abs_linear* p, bool backward) {
 }
 bool bad_pitch(int64_t ld, int64_t cols) { return ld < cols || ld >= 1ll << 32; }
 
+// The copies that a pass's operands need, side by side.
 template <typename T>
-hipError_t pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd, hipStream_t s) {
-  linear_pack_kernel<T><<<few_blocks(rows * (ldd / kPiece<T>)), 256, 0, s>>>((const T*)src, ld, rows, cols, (T*)dst, ldd);
+hipError_t pack_operands(const abs_linear& p, const LinearPlan& q, const void* x, const void* w, bool want_x, bool want_w, char* ws, hipStream_t s) {
+  const Pack<T> px{(const T*)x, p.ldx, p.rows, p.d_in, (T*)(ws + q.off_x), q.in8}, pw{(const T*)w, p.ldw, p.d_in, p.d_out, (T*)(ws + q.off_w), q.out8};
+  want_x = want_x && q.pack_x;
+  want_w = want_w && q.pack_w;
+  if (!want_x && !want_w) return hipSuccess;
+  auto threads = [](const Pack<T>& c) { return c.rows * (c.ldd / kPiece<T>); };
+  const int64_t most = std::max(want_x ? threads(px) : 0, want_w ? threads(pw) : 0);
+  linear_pack_kernel<T><<<dim3(few_blocks(most), want_x && want_w ? 2 : 1), 256, 0, s>>>(want_x ? px : pw, pw);
   return hipGetLastError();
 }
 
@@ -1242,8 +1264,9 @@ hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, 
   GemmArgs<T> g{};
   g.A = (const T*)x; g.lda = p.ldx; g.B = (const T*)w; g.ldb = p.ldw;
   hipError_t err = hipSuccess;
-  if (q.pack_x) { g.A = (const T*)(ws + q.off_x); g.lda = q.in8; err = pack<T>(x, p.ldx, p.rows, p.d_in, ws + q.off_x, q.in8, s); }
-  if (err == hipSuccess && q.pack_w) { g.B = (const T*)(ws + q.off_w); g.ldb = q.out8; err = pack<T>(w, p.ldw, p.d_in, p.d_out, ws + q.off_w, q.out8, s); }
+  if (q.pack_x) { g.A = (const T*)(ws + q.off_x); g.lda = q.in8; }
+  if (q.pack_w) { g.B = (const T*)(ws + q.off_w); g.ldb = q.out8; }
+  err = pack_operands<T>(p, q, x, w, true, true, ws, s);
   if (err != hipSuccess) return err;
   g.M = p.rows; g.N = p.d_out; g.K = p.d_in; g.nc = q.out8; g.mc = 0;
   g.e = e;
@@ -1286,33 +1309,27 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
   float* sums = db ? (float*)(ws + q.off_sums) : nullptr;
   if ((q.dz && products) || db) {
     T* out = q.dz && products ? (T*)(ws + q.off_dz) : nullptr;
-    const bool whole = p.d_out % V == 0;
-    const int per = whole ? 32 * V : 32;
-    const dim3 grid((unsigned)((p.d_out + per - 1) / per), (unsigned)q.sum_rows);
-    if (whole) linear_dz_kernel<T, V><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
-    else       linear_dz_kernel<T, 1><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
+    const dim3 grid((unsigned)((p.d_out + 32 * V - 1) / (32 * V)), (unsigned)q.sum_rows);
+    linear_dz_kernel<T><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
     err = hipGetLastError();
     if (db) d = DbShares{sums, q.sum_rows, p.d_out, db};
-    if (err == hipSuccess && out && q.out8 != p.d_out) {       // the pieces' ends meet zeros in dx
-      linear_zero_kernel<T><<<few_blocks(p.rows * (q.out8 - p.d_out)), 256, 0, s>>>(out + p.d_out, q.out8, p.rows, q.out8 - p.d_out);
-      err = hipGetLastError();
-    }
     if (out) { dz = out; lddz = q.out8; }
   }
   float* part = (float*)(ws + q.off_part);
   GemmArgs<T> ga{}, gb{};
   if (err == hipSuccess && dx) {
     ga.A = dz; ga.lda = lddz; ga.B = (const T*)w; ga.ldb = p.ldw;
-    if (q.pack_w) { ga.B = (const T*)(ws + q.off_w); ga.ldb = q.out8; err = pack<T>(w, p.ldw, p.d_in, p.d_out, ws + q.off_w, q.out8, s); }
+    if (q.pack_w) { ga.B = (const T*)(ws + q.off_w); ga.ldb = q.out8; }
     ga.M = p.rows; ga.N = p.d_in; ga.K = p.d_out;
     ga.e.y = (T*)dx; ga.e.ldy = p.lddx;
   }
   if (err == hipSuccess && dw) {
     gb.A = (const T*)x; gb.lda = p.ldx; gb.B = dz; gb.ldb = lddz;
-    if (q.pack_x) { gb.A = (const T*)(ws + q.off_x); gb.lda = q.in8; err = pack<T>(x, p.ldx, p.rows, p.d_in, ws + q.off_x, q.in8, s); }
+    if (q.pack_x) { gb.A = (const T*)(ws + q.off_x); gb.lda = q.in8; }
     gb.M = p.d_in; gb.N = p.d_out; gb.K = p.rows; gb.mc = q.in8; gb.nc = q.out8;
     gb.e.y = (T*)dw; gb.e.ldy = p.lddw;
   }
+  if (err == hipSuccess) err = pack_operands<T>(p, q, x, w, dw != nullptr, dx != nullptr, ws, s);
   if (err != hipSuccess) return err;
   if (q.pair && dx && dw) {
     const Join<T> jb = set_product(q.pair_dw, gb, part), ja = set_product(q.pair_dx, ga, (float*)(ws + q.off_part2));
