@@ -19,6 +19,7 @@ namespace abs_impl {
 namespace {
 
 constexpr int kMaxLanes = 1024;            // D: lanes of one sample
+constexpr int64_t kPlenty = 65536;         // lanes that fill the chip: 256 on a CU
 
 template <typename T>
 struct NormArgs {
@@ -781,9 +782,16 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
       q.parts = (uint32_t)((S + q.PP - 1) / q.PP);
       q.D = q.TX * q.PL;
     } else {
+      // As few positions a lane as half a workgroup takes while the lanes are few, more where more positions leave lanes enough: what a
+      // lane does once - its place, the sums across lanes - takes the time of several pieces (bf16 6140 x 9 x 224 in 32 groups 85 -> 21 us,
+      // gradient 88 -> 41; 500 x 9 x 224 10.7 -> 6.4, 16.8 -> 13; 4000 x 49 x 64 in 8 34 -> 15; 100000 x 4 x 64 35 -> 24, but its
+      // gradient 58 -> 62).
       q.NP = np_most;
-      for (int np : {1, 4, np_most})
-        if ((int64_t)q.TX * pow2_up((S + np - 1) / np) <= 512) { q.NP = np; break; }
+      auto lanes_at = [&](int np) { return (int64_t)q.TX * pow2_up((S + np - 1) / np); };
+      for (int np : {1, 4, np_most}) {
+        const int more = np == 1 ? 4 : backward && size == 4 ? 0 : np_most;       // (eight positions of fp32 spill in the backward pass)
+        if (lanes_at(np) <= 512 && (np == np_most || S <= np || !more || p.n * q.chunks * lanes_at(more) < kPlenty)) { q.NP = np; break; }
+      }
       q.PL = pow2_up((S + q.NP - 1) / q.NP);
       q.D = q.TX * q.PL;
     }
