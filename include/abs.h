@@ -388,8 +388,9 @@ enum { ABS_ACT_NONE = 0, ABS_ACT_RELU = 1, ABS_ACT_SILU = 2, ABS_ACT_GELU = 3 };
  * The backward pass, for a gradient dy [rows, d_out] of y:  dz = dy act'(z) (relu: 0 where z is not positive;
  * d_z may be NULL for ABS_ACT_NONE),  dx = dz W^T, dW = x^T dz, db = sum of dz over the rows; the residual's
  * gradient is dy itself.  d_dx, d_dw, d_db: any of them may be NULL, then it is not computed.  With bf16
- * operands dz is rounded to bf16 once, for the matrix cores; db is summed from the unrounded values.  d_y may be d_r
- * with the same pitch (each element is read before it is written).
+ * operands the matrix cores get dz in bf16: small products as the sum of two bf16 values, large ones rounded once
+ * (dx and dW then differ from the exact ones by two roundings, not one); db is summed from the unrounded values.
+ * d_y may be d_r with the same pitch (each element is read before it is written).
  */
 typedef struct abs_linear {
   int32_t dtype;

@@ -556,6 +556,11 @@ template <> struct FragOf<uint16_t> { typedef bf16x8_t type; };
 template <> struct FragOf<float> { typedef f32x4_t type; };
 template <typename T> using Frag = typename FragOf<T>::type;
 
+// dz is rounded for the matrix instruction; what that leaves out of f goes through it as well (a second operand, 16 bits of dz in all: a
+// gradient's rounding is then its output's alone, for instructions that a product waiting for memory has to spare).  Nothing of what is
+// not finite.
+__device__ __forceinline__ float left_out(float f, float rounded) { const float l = f - rounded; return fabsf(l) < 3e38f ? l : 0.f; }
+
 // [row][k]: elements k .. k + 7 (fp32: 3) of a row, zeros from K on
 template <typename T>
 struct RowPart {
@@ -576,8 +581,8 @@ struct RowPart {
     }
   }
   __device__ __forceinline__ Frag<T> frag() const { Frag<T> f; __builtin_memcpy(&f, w, 16); return f; }
-  // this = dz, from dy (this) and z
-  __device__ __forceinline__ void slope(const RowPart& z, int act) {
+  // this = dz, from dy (this) and z, which becomes the part of dz that bf16 leaves out (fp32: nothing is)
+  __device__ __forceinline__ void slope(RowPart& z, int act) {
     Piece<T, kPiece<T>> d, h;
     float f[kPiece<T>], g[kPiece<T>];
 #pragma unroll
@@ -588,6 +593,13 @@ struct RowPart {
     d.set(f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = d.w[i];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < kPiece<T>; ++e) f[e] = left_out(f[e], d.at(e));
+      h.set(f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z.w[i] = h.w[i];
+    }
   }
 };
 
@@ -632,7 +644,7 @@ struct ColumnPart<uint16_t> {
     __builtin_memcpy(&v, f, 16);
     return v;
   }
-  __device__ __forceinline__ void slope(const ColumnPart& z, int act, float& s0, float& s1) {
+  __device__ __forceinline__ void slope(ColumnPart& z, int act, float& s0, float& s1) {
 #pragma unroll
     for (int r = 0; r < 8; r += 4) {
       float f[8], h[8];
@@ -646,6 +658,11 @@ struct ColumnPart<uint16_t> {
       o.set(f);
 #pragma unroll
       for (int i = 0; i < 4; ++i) { s0 += f[2 * i]; s1 += f[2 * i + 1]; w[r + i] = o.w[i]; }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = left_out(f[i], o.at(i));
+      o.set(f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z.w[r + i] = o.w[i];
     }
   }
   __device__ __forceinline__ void sum(float& s0, float& s1) const {
@@ -682,7 +699,7 @@ struct ColumnPart<float> {
     }
   }
   __device__ __forceinline__ f32x4_t frag(int odd) const { return f32x4_t{w[odd][0], w[odd][1], w[odd][2], w[odd][3]}; }
-  __device__ __forceinline__ void slope(const ColumnPart& z, int act, float& s0, float& s1) {
+  __device__ __forceinline__ void slope(ColumnPart& z, int act, float& s0, float& s1) {
     op_slope_all<8>(&w[0][0], &z.w[0][0], act);
     sum(s0, s1);
   }
@@ -837,6 +854,10 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
           if (g.dz.act != ABS_ACT_NONE) s.a.slope(s.z, g.dz.act);
           acc[0][0] = multiply(s.b0.frag(), s.a.frag(), acc[0][0]);
           acc[0][1] = multiply(s.b1.frag(), s.a.frag(), acc[0][1]);
+          if (sizeof(T) == 2 && g.dz.act > ABS_ACT_RELU) {          // (relu's dz is dy or 0)
+            acc[0][0] = multiply(s.b0.frag(), s.z.frag(), acc[0][0]);
+            acc[0][1] = multiply(s.b1.frag(), s.z.frag(), acc[0][1]);
+          }
         });
     small_finish<T>(epilogue(g.a), acc[0][0], acc[0][1], red, team, waves, m0, 32, 1, g.rows, n0, g.d_in);
     return;
@@ -863,6 +884,13 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
         acc[0][1] = multiply(fb1, fa0, acc[0][1]);
         acc[1][0] = multiply(fb0, fa1, acc[1][0]);
         acc[1][1] = multiply(fb1, fa1, acc[1][1]);
+        if (sizeof(T) == 2 && g.dz.act > ABS_ACT_RELU) {          // (relu's dz is dy or 0)
+          const Frag<T> fz0 = s.z.frag(0), fz1 = s.z.frag(1);
+          acc[0][0] = multiply(fz0, fa0, acc[0][0]);
+          acc[0][1] = multiply(fz1, fa0, acc[0][1]);
+          acc[1][0] = multiply(fz0, fa1, acc[1][0]);
+          acc[1][1] = multiply(fz1, fa1, acc[1][1]);
+        }
       });
   if (g.db && m0 == 0) {
     s0 += __shfl_xor(s0, 32);
