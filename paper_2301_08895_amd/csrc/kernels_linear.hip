@@ -915,11 +915,12 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
 
 // ---------------------------------------------------------------------- dz = dy act'(z), and its column sums
 // 256 threads: 32 pieces of columns, 8 rows at a time; a workgroup's shares of the column sums leave in `sums` [gridDim.y][N].  Rows of dz
-// are whole pieces (lddz), zeros from N on.  Bound by memory: 8192 x 2048 bf16 19 us, 5.3 TB/s, a large copy's rate.
-template <typename T>
+// are whole pieces (lddz), zeros from N on.  Bound by memory: 8192 x 2048 bf16 19 us, 5.3 TB/s, a large copy's rate (WHOLE: N is whole
+// pieces; with the ends' branch 23).
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void load_columns(Piece<T, kPiece<T>>& v, const T* p, int count) {
   constexpr int V = kPiece<T>;
-  if (count >= V) { v.load(p); return; }
+  if (WHOLE || count >= V) { v.load(p); return; }
   T e[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) e[i] = p[min(i, count - 1)];
@@ -927,7 +928,7 @@ __device__ __forceinline__ void load_columns(Piece<T, kPiece<T>>& v, const T* p,
   for (int i = 0; i < V; ++i) e[i] = i < count ? e[i] : T(0);
   __builtin_memcpy(v.w, e, 16);
 }
-template <typename T>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t lddy, const T* z, int64_t ldz, T* dz, int64_t lddz, int64_t rows,
                                                         int N, int act, float* sums) {
   constexpr int V = kPiece<T>;
@@ -941,8 +942,8 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t ldd
 #pragma unroll 2
     for (int64_t m = (int64_t)blockIdx.y * 8 + rl; m < rows; m += (int64_t)gridDim.y * 8) {
       Piece<T, V> d, h, o;
-      load_columns(d, dy + m * lddy + n, N - n);
-      if (act != ABS_ACT_NONE) load_columns(h, z + m * ldz + n, N - n);
+      load_columns<WHOLE>(d, dy + m * lddy + n, N - n);
+      if (act != ABS_ACT_NONE) load_columns<WHOLE>(h, z + m * ldz + n, N - n);
       float f[V], g[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) { f[e] = d.at(e); g[e] = act != ABS_ACT_NONE ? h.at(e) : 0.f; }
@@ -1338,7 +1339,8 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
   if ((q.dz && products) || db) {
     T* out = q.dz && products ? (T*)(ws + q.off_dz) : nullptr;
     const dim3 grid((unsigned)((p.d_out + 32 * V - 1) / (32 * V)), (unsigned)q.sum_rows);
-    linear_dz_kernel<T><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
+    if (p.d_out % V == 0) linear_dz_kernel<T, true><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
+    else                  linear_dz_kernel<T, false><<<grid, 256, 0, s>>>((const T*)dy, p.lddy, (const T*)z, p.ldz, out, q.out8, p.rows, p.d_out, p.act, sums);
     err = hipGetLastError();
     if (db) d = DbShares{sums, q.sum_rows, p.d_out, db};
     if (out) { dz = out; lddz = q.out8; }
