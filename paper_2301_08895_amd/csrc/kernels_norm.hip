@@ -693,6 +693,93 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
   }
 }
 
+// Backward, single positions of wide groups, like norm_row_kernel: a workgroup takes every row_count-th sample of one group, so that its
+// channels' sums add up in registers.  gamma and beta are read again for every sample (they are in the caches).  Groups of whole pieces
+// alone: the registers do not hold a partial piece's handling too (4096 x 4099 fp32 125 -> 139 us).  4096 x 8192 bf16 in one group 61 us
+// (79 in norm_backward_kernel, floor 39), x 16384 127 (366 in the plain kernel, floor 78), fp32 4096 x 4096 57 (130); 4096 x 2048
+// bf16 34 against 30 there, hence the rule.
+template <typename T, int V>
+__global__ __launch_bounds__(1024) void norm_row_backward_kernel(NormArgs<T> a) {
+  typedef Piece<T, V> Vec;
+  __shared__ float red[2][16];
+  const float inv = 1.0f / (float)a.per;
+  const uint32_t row = blockIdx.x / (uint32_t)a.G, g = blockIdx.x - row * (uint32_t)a.G;
+  const int c0 = (int)g * a.per;
+  auto slot_of = [&](int k) { return (int)threadIdx.x + k * (int)blockDim.x; };
+  float sg[kRow][V], sb[kRow][V];
+#pragma unroll
+  for (int k = 0; k < kRow; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) sg[k][e] = sb[k][e] = 0.f;
+  for (int64_t i = row; i < a.n; i += a.row_count) {
+    const T* const px = a.x + i * a.ldx + c0;
+    const T* const pd = a.dy + i * a.lddy + c0;
+    Vec x[kRow], dy[kRow];
+#pragma unroll
+    for (int k = 0; k < kRow; ++k) {
+      const int slot = slot_of(k);
+      if (slot < a.slots) {
+        x[k].load(px + slot * V);
+        dy[k].load(pd + slot * V);
+      }
+    }
+    const float mean = a.mean[i * a.G + g], rstd = a.rstd[i * a.G + g];
+    float kept[kRow][V], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < kRow; ++k) {
+      const int slot = slot_of(k);
+      if (slot < a.slots) {
+        float s[V], bet[V], d[V], dh[V];
+        parameters<false, T, V>(a, c0 + slot * V, V, s, bet);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] *= rstd;
+        norm_dh<T, V>(x[k], dy[k], mean, s, bet, a.act, d, dh);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          sb[k][e] += dh[e];
+          sg[k][e] = fmaf(rstd, dh[e] * d[e], sg[k][e]);
+          kept[k][e] = s[e] * dh[e];
+          s1 += kept[k][e];
+          s2 = fmaf(kept[k][e], d[e], s2);
+        }
+        x[k].hide();
+      }
+    }
+    s1 = row_sum(s1, red[0]);
+    s2 = row_sum(s2, red[1]);
+    const float c1 = -(s1 * inv), c2 = -rstd * (rstd * (s2 * inv));
+    T* const py = a.y + i * a.ldy + c0;
+    const T* const pr = a.dres ? a.dres + i * a.lddres + c0 : nullptr;
+#pragma unroll
+    for (int k = 0; k < kRow; ++k) {
+      const int slot = slot_of(k);
+      if (slot < a.slots) {
+        Vec o, res;
+        if (pr) res.load(pr + slot * V);
+        float w[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          w[e] = kept[k][e] + fmaf(c2, x[k].at(e) - mean, c1);
+          if (pr) w[e] += res.at(e);
+        }
+        o.set(w);
+        o.store(py + slot * V);
+      }
+    }
+    // (red[0] is written again only behind the second sum's barrier, red[1] only behind the first one's)
+  }
+  if (!a.rows_g) return;
+#pragma unroll
+  for (int k = 0; k < kRow; ++k) {
+    const int slot = slot_of(k);
+    if (slot < a.slots) {
+      const int64_t o = (int64_t)row * a.row_step + c0 + slot * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) { a.rows_g[o + e] = sg[k][e]; a.rows_b[o + e] = sb[k][e]; }
+    }
+  }
+}
+
 // dgamma, dbeta: the workgroups' shares added in their order, 32 channels x 32 rows of shares at a time, eight rows of a lane in
 // flight (423 shares of 69 channels 16 -> 6 us)
 __global__ __launch_bounds__(1024) void norm_share_sum_kernel(const float* rows, uint32_t row_count, int C, float* dgamma, float* dbeta) {
@@ -804,10 +891,16 @@ struct NormPlan {
   size_t off_rows, bytes;                  // workspace: parts' statistics, then the shares of dgamma / dbeta
 };
 
-// The widest piece: 16 bytes; backward four elements, but for single positions (norm_piece).
-int norm_widest(const abs_group_norm& p, bool backward) { return p.dtype == ABS_X_BF16 && (!backward || p.spatial == 1) ? 8 : 4; }
-
 int pow2_up(int64_t x) { int p = 1; while (p < x) p <<= 1; return p; }
+
+// Single positions of groups so wide that several pieces a lane pay: norm_row_kernel, norm_row_backward_kernel.
+bool norm_rows(const abs_group_norm& p, bool backward, int V) {
+  const int per = p.channels / p.groups, slots = (per + V - 1) / V;
+  return p.spatial == 1 && slots <= kRow * 1024 && p.n * p.groups < 1ll << 31 && (backward ? V == 4 && per % 4 == 0 && per >= 4096 : slots > 32);
+}
+
+// The widest piece: 16 bytes; backward four elements, but for single positions (norm_piece).
+int norm_widest(const abs_group_norm& p, bool backward) { return p.dtype == ABS_X_BF16 && (!backward || (p.spatial == 1 && !norm_rows(p, true, 4))) ? 8 : 4; }
 
 // V: elements of a piece.
 NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
@@ -818,11 +911,16 @@ NormPlan norm_plan(const abs_group_norm& p, bool backward, int V) {
   q.slots = (per + V - 1) / V;
   q.SP = pow2_up(q.slots);
   const int np_most = backward ? 8 : 16;
-  if (!backward && S == 1 && q.slots > 32 && q.slots <= kRow * 1024 && p.n * p.groups < 1ll << 31) {
+  if (norm_rows(p, backward, V)) {
     q.row = true;
     q.threads = std::max(64, pow2_up((q.slots + kRow - 1) / kRow));
     q.work = (uint32_t)(p.n * p.groups);
     q.blocks = std::min(q.work, 1u << 20);
+    if (backward) {
+      q.row_count = (uint32_t)std::min<int64_t>(p.n, std::max(1, 256 * (1024 / q.threads) / p.groups));
+      q.blocks = q.row_count * (uint32_t)p.groups;
+      if (q.row_count > 1) q.bytes = op_round_up((size_t)q.row_count * 2 * p.channels * 4, 256);
+    }
     return q;
   }
   if (q.SP > kMaxLanes) {
@@ -969,6 +1067,9 @@ hipError_t norm_forward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s
 template <typename T, int V, bool TAIL>
 hipError_t norm_backward_v(const NormArgs<T>& a, const NormPlan& q, hipStream_t s) {
   const dim3 grid(q.blocks), block((unsigned)q.threads);
+  if constexpr (V == 4 && !TAIL) {
+    if (q.row) { norm_row_backward_kernel<T, V><<<grid, block, 0, s>>>(a); return hipGetLastError(); }
+  }
   const int stack = q.threads / std::max(q.TX, 64);
   const size_t lds = q.NP * V >= 32          ? (size_t)q.threads * V * 8        // (kLean; 32 KB at most either way)
                      : a.rows_g && stack > 1 ? (size_t)stack * V * q.TX * 4 : 0;

@@ -180,7 +180,7 @@ def test_linear_offsets_beyond_32_bits(dtype):
 # n, positions, channels, groups: one value a group, odd groups, groups wider than a wavefront or a workgroup's lanes,
 # one position and many, samples that fit a workgroup and that are cut into parts
 NORMS = [(1, 1, 1, 1), (3, 1, 8, 8), (5, 1, 48, 4), (2, 7, 6, 2), (4, 9, 24, 6), (3, 196, 24, 6), (2, 49, 33, 11), (130, 1, 256, 32),
-         (6, 1, 2048, 32), (7, 1, 2048, 1), (300, 1, 264, 1), (9, 1, 2 * 4096, 2), (2, 1, 32768, 1), (2, 1, 32776, 1), (3, 1, 1143, 3), (2, 1, 1500, 1), (2, 3, 1500, 1), (1, 1, 40000, 2), (2, 64, 512, 8),
+         (6, 1, 2048, 32), (7, 1, 2048, 1), (300, 1, 264, 1), (9, 1, 2 * 4096, 2), (2, 1, 32768, 1), (700, 1, 4096, 1), (3, 1, 2 * 5004, 2), (5, 1, 16384, 1), (2, 1, 32776, 1), (3, 1, 1143, 3), (2, 1, 1500, 1), (2, 3, 1500, 1), (1, 1, 40000, 2), (2, 64, 512, 8),
          (1, 1024, 64, 32), (2, 1000, 320, 32), (1, 5000, 8, 1), (3, 300, 130, 1), (1, 40000, 16, 4), (70, 33, 12, 3)]
 # groups that are no whole number of pieces: partial pieces of one to three, one that is alone in a wavefront, samples cut into parts
 PARTIAL = [(3, 50, 10, 2), (2, 300, 69, 1), (2, 40, 771, 3), (1, 3000, 85, 5), (2, 9000, 7, 1), (5, 1, 4099, 1), (9, 1, 129, 3),
