@@ -9,8 +9,8 @@
 //  * a group's sum is then shuffles over powers of two, and, where D is more than a wavefront, one exchange through LDS.
 //  * the variance is the mean of the squared distances from the mean, two passes over registers: nothing cancels.
 // Samples that do not fit (and few large ones, which would leave most CUs idle) are cut into parts along the positions:
-// one launch leaves each part's statistics, the next one joins them and writes.  Groups of more than 1024 pieces take a
-// plain kernel.
+// one launch leaves each part's statistics, the next one joins them and writes.  Wide groups of single positions have kernels of their
+// own (norm_row_kernel), and groups of more than 1024 pieces at several positions, or more than 4096 at one, a plain one.
 #include "operators.h"
 
 #include <algorithm>
@@ -799,7 +799,8 @@ __global__ __launch_bounds__(1024) void norm_share_sum_kernel(const float* rows,
   }
 }
 
-// ---- groups of any width: a workgroup per sample and group, every pass over memory ---------------------
+// ---- groups of any width: a workgroup per sample and group, every pass over memory (bf16 64 x 65536 in one group 50 us, gradient 89,
+// the bytes alone 3 and 5) ---------------------
 __device__ __forceinline__ float block_sum(float v, float* red) {
   for (int off = 1; off < 64; off <<= 1) v += __shfl_xor(v, off);
   __syncthreads();
