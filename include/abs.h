@@ -387,7 +387,8 @@ enum { ABS_ACT_NONE = 0, ABS_ACT_RELU = 1, ABS_ACT_SILU = 2, ABS_ACT_GELU = 3 };
  * rows >= 0, 1 <= d_in, d_out <= 2^20, rows < 2^31, pitches below 2^32, at most 2^22 tiles of 128 x 128 in y, dx or dW.
  * The backward pass, for a gradient dy [rows, d_out] of y:  dz = dy act'(z) (relu: 0 where z is not positive;
  * d_z may be NULL for ABS_ACT_NONE),  dx = dz W^T, dW = x^T dz, db = sum of dz over the rows; the residual's
- * gradient is dy itself.  d_dx, d_dw, d_db: any of them may be NULL, then it is not computed.  With bf16
+ * gradient is dy itself.  d_dx, d_dw, d_db: any of them may be NULL, then it is not computed; without d_dw d_x is
+ * not read and may be NULL, without d_dx d_w.  With bf16
  * operands the matrix cores get dz in bf16: small products as the sum of two bf16 values, large ones rounded once
  * (dx and dW then differ from the exact ones by two roundings, not one); db is summed from the unrounded values.
  * d_y may be d_r with the same pitch (each element is read before it is written).

@@ -869,31 +869,46 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
   place(g.b, (int)blockIdx.x - dx_blocks, K);
   const int m0 = tm * (64 * kSmallWaves / team);
   float s0 = 0.f, s1 = 0.f;
-  struct Step { ColumnPart<T> a, b, z; };
-  const ColumnPlace ca = column_place(m0 + at * 64 + 2 * l32, g.d_in), cb = column_place(n0 + 2 * l32, g.d_out);
-  in_steps<2, Step>(first + mate, team, blocks,
-      [&](int kb, Step& s) {
-        const int k = kb * kBlockK<T> + lk * R;
-        s.a.load(g.x, g.ldx, k, K, ca, g.d_in);
-        s.b.load(g.dz.dy, g.dz.lddy, k, K, cb, g.d_out);
-        if (g.dz.act != ABS_ACT_NONE) s.z.load(g.dz.z, g.dz.ldz, k, K, cb, g.d_out);
-      },
-      [&](Step& s) {
-        if (g.dz.act != ABS_ACT_NONE) s.b.slope(s.z, g.dz.act, s0, s1);
-        else if (g.db && m0 == 0) s.b.sum(s0, s1);
-        const Frag<T> fa0 = s.a.frag(0), fa1 = s.a.frag(1), fb0 = s.b.frag(0), fb1 = s.b.frag(1);
-        acc[0][0] = multiply(fb0, fa0, acc[0][0]);
-        acc[0][1] = multiply(fb1, fa0, acc[0][1]);
-        acc[1][0] = multiply(fb0, fa1, acc[1][0]);
-        acc[1][1] = multiply(fb1, fa1, acc[1][1]);
-        if (sizeof(T) == 2 && g.dz.act > ABS_ACT_RELU) {          // (relu's dz is dy or 0)
-          const Frag<T> fz0 = s.z.frag(0), fz1 = s.z.frag(1);
-          acc[0][0] = multiply(fz0, fa0, acc[0][0]);
-          acc[0][1] = multiply(fz1, fa0, acc[0][1]);
-          acc[1][0] = multiply(fz0, fa1, acc[1][0]);
-          acc[1][1] = multiply(fz1, fa1, acc[1][1]);
-        }
-      });
+  const ColumnPlace cb = column_place(n0 + 2 * l32, g.d_out);
+  if (g.dw) {
+    struct Step { ColumnPart<T> a, b, z; };
+    const ColumnPlace ca = column_place(m0 + at * 64 + 2 * l32, g.d_in);
+    in_steps<2, Step>(first + mate, team, blocks,
+        [&](int kb, Step& s) {
+          const int k = kb * kBlockK<T> + lk * R;
+          s.a.load(g.x, g.ldx, k, K, ca, g.d_in);
+          s.b.load(g.dz.dy, g.dz.lddy, k, K, cb, g.d_out);
+          if (g.dz.act != ABS_ACT_NONE) s.z.load(g.dz.z, g.dz.ldz, k, K, cb, g.d_out);
+        },
+        [&](Step& s) {
+          if (g.dz.act != ABS_ACT_NONE) s.b.slope(s.z, g.dz.act, s0, s1);
+          else if (g.db && m0 == 0) s.b.sum(s0, s1);
+          const Frag<T> fa0 = s.a.frag(0), fa1 = s.a.frag(1), fb0 = s.b.frag(0), fb1 = s.b.frag(1);
+          acc[0][0] = multiply(fb0, fa0, acc[0][0]);
+          acc[0][1] = multiply(fb1, fa0, acc[0][1]);
+          acc[1][0] = multiply(fb0, fa1, acc[1][0]);
+          acc[1][1] = multiply(fb1, fa1, acc[1][1]);
+          if (sizeof(T) == 2 && g.dz.act > ABS_ACT_RELU) {          // (relu's dz is dy or 0)
+            const Frag<T> fz0 = s.z.frag(0), fz1 = s.z.frag(1);
+            acc[0][0] = multiply(fz0, fa0, acc[0][0]);
+            acc[0][1] = multiply(fz1, fa0, acc[0][1]);
+            acc[1][0] = multiply(fz0, fa1, acc[1][0]);
+            acc[1][1] = multiply(fz1, fa1, acc[1][1]);
+          }
+        });
+  } else {                                                          // db alone: x, which may be missing, is not read
+    struct Step { ColumnPart<T> b, z; };
+    in_steps<2, Step>(first + mate, team, blocks,
+        [&](int kb, Step& s) {
+          const int k = kb * kBlockK<T> + lk * R;
+          s.b.load(g.dz.dy, g.dz.lddy, k, K, cb, g.d_out);
+          if (g.dz.act != ABS_ACT_NONE) s.z.load(g.dz.z, g.dz.ldz, k, K, cb, g.d_out);
+        },
+        [&](Step& s) {
+          if (g.dz.act != ABS_ACT_NONE) s.b.slope(s.z, g.dz.act, s0, s1);
+          else s.b.sum(s0, s1);
+        });
+  }
   if (g.db && m0 == 0) {
     s0 += __shfl_xor(s0, 32);
     s1 += __shfl_xor(s1, 32);

@@ -1,0 +1,65 @@
+"""Calls of the hidden layers' operators on the GPU that the documentation allows beside those of test_gpu_operators.py: missing
+operands, values at the edges of a type, ranges of plans, different pitches of one call's matrices."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2301_08895_amd as lib
+import operator_util as ou
+from operator_util import NONE, RELU, SILU, GELU
+from paper_2301_08895_amd.binding import AbsLinear, _lib
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _seed():
+    torch.manual_seed(23)
+
+
+def normal(rows, cols, dtype, scale=1.0):
+    return (torch.randn(rows, cols, device="cuda") * scale).to(dtype)
+
+
+def gradient_call(x, w, z, dy, act, dx, dw, db):
+    """abs_linear_backward itself, any operand or output missing."""
+    rows, d_out = dy.shape
+    d_in = next(t for t in (x, dx) if t is not None).shape[1] if x is not None or dx is not None else 24
+    p = AbsLinear(0 if dy.dtype == F32 else 1, act, rows, d_in, d_out, d_in, d_out, d_out, d_out, d_out, d_out, d_in, d_out)
+    n = _lib.abs_linear_workspace_size(C.byref(p), 1, 0)
+    ws = torch.empty(n + 256, dtype=torch.uint8, device="cuda")
+    at = (ws.data_ptr() + 255) // 256 * 256
+    ptr = lambda t: None if t is None else t.data_ptr()
+    rc = _lib.abs_linear_backward(C.byref(p), ptr(x), ptr(w), ptr(z), ptr(dy), ptr(dx), ptr(dw), ptr(db), at, n,
+                                  torch.cuda.current_stream().cuda_stream)
+    assert rc == 0, lib.abs_last_error(None)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,d_out", [(40, 33), (5000, 40), (30000, 2100)])
+@pytest.mark.parametrize("act", [NONE, GELU])
+def test_bias_gradient_needs_neither_x_nor_w(rows, d_out, act, dtype):
+    """One workgroup's layer, one whose rows are cut into shares, and one beyond the single launch."""
+    z, dy = normal(rows, d_out, dtype), normal(rows, d_out, dtype)
+    db = torch.empty(d_out, device="cuda")
+    gradient_call(None, None, z, dy, act, None, None, db)
+    x, w = torch.zeros(rows, 24, dtype=dtype, device="cuda"), torch.zeros(24, d_out, dtype=dtype, device="cuda")
+    want, slack = ou.linear_gradient(x, w, z, dy, act)
+    ou.close(db, want[2], slack[2], "db")
+    assert torch.equal(lib.linear_backward(x, w, dy, act=act, z=z, need_dx=False, need_dw=False)[2], db)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,d_in,d_out", [(40, 50, 33), (3000, 640, 900)])
+def test_input_gradient_needs_no_x_and_weight_gradient_no_w(rows, d_in, d_out, dtype):
+    x, w = normal(rows, d_in, dtype), normal(d_in, d_out, dtype, d_in ** -0.5)
+    z, dy = normal(rows, d_out, dtype), normal(rows, d_out, dtype)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    gradient_call(None, w, z, dy, SILU, dx, None, None)
+    gradient_call(x, None, z, dy, SILU, None, dw, None)
+    want, slack = ou.linear_gradient(x, w, z, dy, SILU)
+    ou.close(dx, want[0], slack[0], "dx")
+    ou.close(dw, want[1], slack[1], "dw")
