@@ -342,6 +342,21 @@ def abs_draw_batch_rows(cfg: AbsConfig, n: int, j: int) -> np.ndarray:
     return out
 
 
+def _model_size(p: dict) -> int:
+    """Parameters of a workload's model, in the order of abs_get_model: what abs_create copies from d_w0."""
+    d = p["dims"]
+    if p["model"] == 0:
+        return d[0]
+    if p["model"] == 3:
+        d0, C1, C2, F1, F2, C, C0, k = d
+        side = ((round((d0 // C0) ** 0.5) - k + 1) // 2 - k + 1) // 2
+        shapes = [(C0 * k * k, C1), (C1 * k * k, C2), (C2 * side * side, F1), (F1, F2), (F2, C)]
+    else:
+        shapes = list(zip(d[:-1], d[1:]))
+    norms = 2 * sum(d[1:-1]) if p.get("blocks") else 0                  # gamma and beta of the hidden layers
+    return sum(rows * cols + cols for rows, cols in shapes) + norms
+
+
 class Simulation:
     """Harness convenience: owns the device buffers (PyTorch is used for nothing but
     device memory and the stream) and a libabs handle."""
@@ -360,6 +375,10 @@ class Simulation:
                 self.handle = abs_create(self.cfg, None, None, None, None, 0, None)
             self.P = None
             return
+        self.ws_bytes = abs_workspace_size(self.cfg) if blocks is None else abs_blocks_workspace_size(self.cfg, blocks)
+        self.P = int(inputs["w0"].size)
+        if self.P != _model_size(p):                   # (abs_create copies as many floats as the model has)
+            raise AbsError(-1, f"w0 has {self.P} elements, the model {_model_size(p)} parameters")
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU: libabs has no CPU path (use device_mode=0 for schedule-only runs)")
         self.torch = torch
@@ -374,8 +393,6 @@ class Simulation:
             hit = (X, y, w0, xt.to(dev), torch.from_numpy(y).to(dev), torch.from_numpy(w0).to(dev))
             shared[device] = hit
         self.d_X, self.d_y, self.d_w0 = hit[3:]
-        self.P = int(inputs["w0"].size)
-        self.ws_bytes = abs_workspace_size(self.cfg) if blocks is None else abs_blocks_workspace_size(self.cfg, blocks)
         self.d_ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=dev)
         base = self.d_ws.data_ptr()
         self.ws_ptr = (base + 255) // 256 * 256

@@ -178,3 +178,21 @@ def test_workspace_of_the_convolutional_model_by_the_row():
         grow = (C0 * k * k + 1) * C1 + (C1 * k * k + 1) * C2
         words = 3 + n1 + F0 + 2 * (F1 + F2) + C + F0 + grow + 2 + (n1 if apart else 0)
         assert abs((b - a) / 10_000 - (4 * words + n1 + F0)) < 1, (S, (b - a) / 10_000, 4 * words + n1 + F0)
+
+
+@pytest.mark.parametrize("i", [1, 2, 3, 6])
+def test_initial_weights_of_another_size_are_refused(i):
+    """abs_create copies the model's parameters from w0: an array of another length is refused before anything touches a device."""
+    small = dict(M=400) if i != 3 else dict(M=400, dims=[16, 24, 24, 4], n_classes=4, N=4, B=8, n_slow=1)
+    p = workloads.scaled_preset(i, **small)
+    d = workloads.make_inputs(p)
+    assert lib.binding._model_size(p) == d["w0"].size == workloads.param_count(p)
+    cases = [(p, dict(d, w0=d["w0"][:-1])), (p, dict(d, w0=np.concatenate([d["w0"], d["w0"][:1]])))]
+    if i == 3:                                           # inputs made before the blocks were asked for
+        q = workloads.with_blocks(p, groups=8)
+        assert lib.binding._model_size(q) == workloads.make_inputs(q)["w0"].size == d["w0"].size + 2 * (24 + 24)
+        cases += [(q, d), (p, workloads.make_inputs(q))]
+    for q, wrong in cases:
+        with pytest.raises(lib.AbsError) as e:
+            lib.Simulation(q, wrong)
+        assert e.value.code == -1 and "parameters" in str(e.value)
