@@ -31,6 +31,7 @@ import numpy as np
 import workloads
 from . import binding as lib
 
+METHODS = "abs,adasync,sa_adasync,k_async,local_sgd"
 TICKS_PER_UNIT = float(1 << 20)       # the simulated clock counts 2^-20 time units
 
 
@@ -111,7 +112,7 @@ def sweep_a(p: dict, values, seeds: int, rounds: int, every: int, eval_rows: int
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     ap.add_argument("--config", type=int, default=2, help="workload 1..5; 6: the convolutional model of Section V-A")
-    ap.add_argument("--methods", default="abs,adasync,sa_adasync,k_async,local_sgd")
+    ap.add_argument("--methods", default=None, help=f"default: {METHODS}, with --blocks those of one local step")
     ap.add_argument("--rounds", type=int, default=600)
     ap.add_argument("--every", type=int, default=100, help="rounds between read-outs")
     ap.add_argument("--eval-rows", type=int, default=4096)
@@ -139,14 +140,22 @@ def main(argv=None):
     if a.sweep_a is not None:
         sweep_a(p, [int(v) for v in a.sweep_a.split(",")], max(1, a.seeds), a.rounds, every, a.eval_rows, a.target)
         return 0
-    out = []
-    for name in a.methods.split(","):
-        over = {}
-        if a.U and name != "sync_sgd":
-            over["U"] = a.U
+
+    def over(name):
+        o = {"U": a.U} if a.U and name != "sync_sgd" else {}
         if a.a is not None and name.startswith(("abs", "sa_abs")):
-            over["a"] = a.a
-        out += run_method(p, name, a.rounds, every, a.eval_rows, over)
+            o["a"] = a.a
+        return o
+
+    names = (a.methods or METHODS).split(",")
+    if a.blocks is not None:                    # said here, not behind the last round of the methods before
+        single = [n for n in names if workloads.method_preset(p, n, **over(n)).get("U", 1) <= 1]
+        if not single or a.methods and single != names:
+            ap.error("--blocks: workers take one local step a round (no local_sgd, no --U above 1)")
+        names = single
+    out = []
+    for name in names:
+        out += run_method(p, name, a.rounds, every, a.eval_rows, over(name))
     if a.json:
         for r in out:
             print(json.dumps(r))
@@ -158,7 +167,7 @@ def main(argv=None):
               f"{r['train_loss']:11.5f} {r['eval_loss']:10.5f} {r['eval_acc']:8.4f}")
     if a.target is not None:
         print(f"\nfirst read-out with held-out loss <= {a.target}:")
-        for name in a.methods.split(","):
+        for name in names:
             hit = next((r for r in out if r["method"] == name and r["eval_loss"] <= a.target), None)
             print(f"  {name:14s} " + (f"time {hit['time']:.2f}, comm {hit['comm']}, round {hit['round']}" if hit
                                       else "not reached"))
