@@ -100,12 +100,13 @@ __device__ __forceinline__ float op_act(float z) {
   if (ACT == ABS_ACT_GELU) { float e; return z * op_phi(z, e); }
   return z;
 }
+// d act'(z).  relu: a choice, not a product - nothing of d passes where z is not positive, and it may be infinite there
 template <int ACT>
-__device__ __forceinline__ float op_act_slope(float z) {
-  if (ACT == ABS_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (ACT == ABS_ACT_SILU) { const float p = op_sigmoid(z); return fmaf(z * p, 1.0f - p, p); }
-  if (ACT == ABS_ACT_GELU) { float e; const float c = op_phi(z, e); return fmaf(z * 0.39894228040143268f, e, c); }
-  return 1.f;
+__device__ __forceinline__ float op_slope(float d, float z) {
+  if (ACT == ABS_ACT_RELU) return z > 0.f ? d : 0.f;
+  if (ACT == ABS_ACT_SILU) { const float p = op_sigmoid(z); return d * fmaf(z * p, 1.0f - p, p); }
+  if (ACT == ABS_ACT_GELU) { float e; const float c = op_phi(z, e); return d * fmaf(z * 0.39894228040143268f, e, c); }
+  return d;
 }
 // N values at once, the activation a uniform run-time value: one branch
 template <int N>
@@ -122,19 +123,19 @@ __device__ __forceinline__ void op_act_all(float* h, int act) {
     for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_GELU>(h[i]);
   }
 }
-// d[i] *= act'(h[i])
+// d[i] = d[i] act'(h[i])
 template <int N>
 __device__ __forceinline__ void op_slope_all(float* d, const float* h, int act) {
   asm volatile("" : "+s"(act));
   if (act == ABS_ACT_RELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] *= op_act_slope<ABS_ACT_RELU>(h[i]);
+    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_RELU>(d[i], h[i]);
   } else if (act == ABS_ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] *= op_act_slope<ABS_ACT_SILU>(h[i]);
+    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_SILU>(d[i], h[i]);
   } else if (act == ABS_ACT_GELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] *= op_act_slope<ABS_ACT_GELU>(h[i]);
+    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_GELU>(d[i], h[i]);
   }
 }
 // the same with the activation as a uniform run-time value
@@ -146,12 +147,12 @@ __device__ __forceinline__ float op_act(float z, int act) {
     default: return z;
   }
 }
-__device__ __forceinline__ float op_act_slope(float z, int act) {
+__device__ __forceinline__ float op_slope(float d, float z, int act) {
   switch (act) {
-    case ABS_ACT_RELU: return op_act_slope<ABS_ACT_RELU>(z);
-    case ABS_ACT_SILU: return op_act_slope<ABS_ACT_SILU>(z);
-    case ABS_ACT_GELU: return op_act_slope<ABS_ACT_GELU>(z);
-    default: return 1.f;
+    case ABS_ACT_RELU: return op_slope<ABS_ACT_RELU>(d, z);
+    case ABS_ACT_SILU: return op_slope<ABS_ACT_SILU>(d, z);
+    case ABS_ACT_GELU: return op_slope<ABS_ACT_GELU>(d, z);
+    default: return d;
   }
 }
 #endif

@@ -63,3 +63,35 @@ def test_input_gradient_needs_no_x_and_weight_gradient_no_w(rows, d_in, d_out, d
     want, slack = ou.linear_gradient(x, w, z, dy, SILU)
     ou.close(dx, want[0], slack[0], "dx")
     ou.close(dw, want[1], slack[1], "dw")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,d_in,d_out", [(60, 40, 33), (900, 700, 904)])
+def test_relu_lets_nothing_of_masked_gradients_through(rows, d_in, d_out, dtype):
+    """dz is 0 where z is not positive, whatever dy holds there (one launch, and tiles behind a pass for dz)."""
+    x, w = normal(rows, d_in, dtype), normal(d_in, d_out, dtype, d_in ** -0.5)
+    z, dy = normal(rows, d_out, dtype), normal(rows, d_out, dtype)
+    off = z <= 0
+    off[0, 0], z[0, 0] = True, 0.0
+    wild = dy.clone()
+    wild[off] = torch.tensor([float("inf"), -float("inf"), float("nan"), 3e38], device="cuda").to(dtype).repeat(off.sum() // 4 + 1)[:off.sum()]
+    got = lib.linear_backward(x, w, wild, act=RELU, z=z)
+    for g, v, s, name in zip(got, *ou.linear_gradient(x, w, z, torch.where(off, 0, dy), RELU), ("dx", "dw", "db")):
+        ou.close(g, v, s, name)
+
+
+# one workgroup per sample, samples in parts, single positions, wide groups of those, groups of the plain kernel
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,S,C,G", [(5, 49, 32, 4), (1, 5000, 16, 2), (40, 1, 256, 8), (9, 1, 4096, 1), (2, 3, 16400, 2)])
+def test_relu_behind_a_norm_lets_nothing_of_masked_gradients_through(n, S, C, G, dtype):
+    x, dy = normal(n * S, C, dtype).view(n, S, C), normal(n * S, C, dtype).view(n, S, C)
+    gamma, beta = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    _, mean, rstd = lib.group_norm_forward(x, gamma, beta, G)
+    wide = lambda t: t.repeat_interleave(C // G, 1)[:, None, :]
+    # on the border the sign is the distance's (gamma and rstd are positive, beta is 0)
+    off = (x.float() - wide(mean)) <= 0
+    wild = torch.where(off, float("inf"), dy.float()).to(dtype)
+    got = lib.group_norm_backward(x, gamma, beta, mean, rstd, wild, act=RELU)
+    want, slack = ou.norm_gradient(x, gamma, beta, mean, rstd, torch.where(off, 0, dy), None, NONE)
+    for g, v, s, name in zip(got, want, slack, ("dx", "dgamma", "dbeta")):
+        ou.close(g, v, s, name)
