@@ -558,10 +558,24 @@ template <> struct FragOf<uint16_t> { typedef bf16x8_t type; };
 template <> struct FragOf<float> { typedef f32x4_t type; };
 template <typename T> using Frag = typename FragOf<T>::type;
 
-// dz is rounded for the matrix instruction; what that leaves out of f goes through it as well (a second operand, 16 bits of dz in all: a
-// gradient's rounding is then its output's alone, for instructions that a product waiting for memory has to spare).  Nothing of what is
-// not finite.
-__device__ __forceinline__ float left_out(float f, float rounded) { const float l = f - rounded; return fabsf(l) < 3e38f ? l : 0.f; }
+// dz goes through the matrix instruction as the sum of two bf16 values (15 bits of it and more: a gradient's rounding is then its output's
+// alone, for instructions that a product waiting for memory has to spare).  Both have dz's sign, and neither is 0 unless dz is: the first
+// is the largest bf16 value below dz in size, the second the rest.  An infinite x or W thus meets no other factors than it meets in dz; of
+// an infinite dz both are infinite.  shrink: 1 - 2^-23, or, for relu, whose dz is a bf16 value already, 1 (there is no second part).
+template <int N>
+__device__ __forceinline__ void two_parts(const float* f, float shrink, Piece<uint16_t, N>& first, Piece<uint16_t, N>& rest) {
+  float r[N];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i)
+    first.w[i] = __builtin_amdgcn_perm(__float_as_uint(f[2 * i + 1] * shrink), __float_as_uint(f[2 * i] * shrink), 0x07060302u);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float l = f[i] - first.at(i);
+    r[i] = fabsf(l) < 3e38f ? l : f[i];
+  }
+  rest.set(r);
+}
+__device__ __forceinline__ float parts_shrink(int act) { return act > ABS_ACT_RELU ? 0.99999988f : 1.0f; }
 
 // [row][k]: elements k .. k + 7 (fp32: 3) of a row, zeros from K on
 template <typename T>
@@ -583,7 +597,7 @@ struct RowPart {
     }
   }
   __device__ __forceinline__ Frag<T> frag() const { Frag<T> f; __builtin_memcpy(&f, w, 16); return f; }
-  // this = dz, from dy (this) and z, which becomes the part of dz that bf16 leaves out (fp32: nothing is)
+  // this = dz, from dy (this) and z, which becomes the second part of a bf16 dz
   __device__ __forceinline__ void slope(RowPart& z, int act) {
     Piece<T, kPiece<T>> d, h;
     float f[kPiece<T>], g[kPiece<T>];
@@ -592,16 +606,10 @@ struct RowPart {
 #pragma unroll
     for (int e = 0; e < kPiece<T>; ++e) { f[e] = d.at(e); g[e] = h.at(e); }
     op_slope_all<kPiece<T>>(f, g, act);
-    d.set(f);
+    if constexpr (sizeof(T) == 2) two_parts<kPiece<T>>(f, parts_shrink(act), d, h);
+    else d.set(f);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = d.w[i];
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int e = 0; e < kPiece<T>; ++e) f[e] = left_out(f[e], d.at(e));
-      h.set(f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z.w[i] = h.w[i];
-    }
+    for (int i = 0; i < 4; ++i) { w[i] = d.w[i]; if (sizeof(T) == 2) z.w[i] = h.w[i]; }
   }
 };
 
@@ -656,15 +664,10 @@ struct ColumnPart<uint16_t> {
         h[2 * i] = __uint_as_float(z.w[r + i] << 16); h[2 * i + 1] = __uint_as_float(z.w[r + i] & 0xFFFF0000u);
       }
       op_slope_all<8>(f, h, act);
-      Piece<uint16_t, 8> o;
-      o.set(f);
+      Piece<uint16_t, 8> o, rest;
+      two_parts<8>(f, parts_shrink(act), o, rest);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { s0 += f[2 * i]; s1 += f[2 * i + 1]; w[r + i] = o.w[i]; }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = left_out(f[i], o.at(i));
-      o.set(f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z.w[r + i] = o.w[i];
+      for (int i = 0; i < 4; ++i) { s0 += f[2 * i]; s1 += f[2 * i + 1]; w[r + i] = o.w[i]; z.w[r + i] = rest.w[i]; }
     }
   }
   __device__ __forceinline__ void sum(float& s0, float& s1) const {

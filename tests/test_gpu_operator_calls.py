@@ -95,3 +95,19 @@ def test_relu_behind_a_norm_lets_nothing_of_masked_gradients_through(n, S, C, G,
     want, slack = ou.norm_gradient(x, gamma, beta, mean, rstd, torch.where(off, 0, dy), None, NONE)
     for g, v, s, name in zip(got, want, slack, ("dx", "dgamma", "dbeta")):
         ou.close(g, v, s, name)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("act", [NONE, SILU, GELU])
+@pytest.mark.parametrize("rows,d_in,d_out", [(40, 50, 33), (5000, 40, 24), (900, 700, 904)])
+def test_infinite_operands_of_a_gradient(rows, d_in, d_out, act, dtype):
+    """A single infinite factor gives an infinity of its sign, where dz has one; NaN where dz is 0."""
+    x, w = normal(rows, d_in, dtype), normal(d_in, d_out, dtype, d_in ** -0.5)
+    z, dy = normal(rows, d_out, dtype), normal(rows, d_out, dtype)
+    x[rows // 2, 3], x[1, 20], w[7, 5], w[d_in - 1, d_out - 1] = float("inf"), -float("inf"), -float("inf"), float("inf")
+    dy[1, 4] = dy[rows - 1, 5] = 0.0
+    got = lib.linear_backward(x, w, dy, act=act, z=z)
+    want, slack = ou.linear_gradient(x, w, z, dy, act)
+    assert torch.isinf(want[0]).any() and torch.isinf(want[1]).any() and torch.isnan(want[0]).any() and torch.isnan(want[1]).any()
+    for g, v, s, name in zip(got, want, slack, ("dx", "dw", "db")):
+        ou.close(g, v, s, name)
