@@ -68,7 +68,7 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t 
       for (int i = 0; i < V; ++i) v[i] += bias.at(i);
     }
     if (e.z) { o.set(v); o.store(e.z + m * e.ldz + n); }
-    op_act_all<V>(v, e.act);
+    op_act_all<V, kFine<T>>(v, e.act);
     if (e.r) {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] += res.at(i);
@@ -82,7 +82,7 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, int64_t m, int64_t 
         float h = v[i];
         if (e.bias) h += e.bias[n + i];
         if (e.z) op_narrow(h, e.z[m * e.ldz + n + i]);
-        h = op_act(h, e.act);
+        h = op_act<kFine<T>>(h, e.act);
         if (e.r) h += op_widen(e.r[m * e.ldr + n + i]);
         op_narrow(h, e.y[m * e.ldy + n + i]);
       }
@@ -605,7 +605,7 @@ struct RowPart {
     for (int i = 0; i < 4; ++i) { d.w[i] = w[i]; h.w[i] = z.w[i]; }
 #pragma unroll
     for (int e = 0; e < kPiece<T>; ++e) { f[e] = d.at(e); g[e] = h.at(e); }
-    op_slope_all<kPiece<T>>(f, g, act);
+    op_slope_all<kPiece<T>, kFine<T>>(f, g, act);
     if constexpr (sizeof(T) == 2) two_parts<kPiece<T>>(f, parts_shrink(act), d, h);
     else d.set(f);
 #pragma unroll
@@ -663,7 +663,7 @@ struct ColumnPart<uint16_t> {
         f[2 * i] = __uint_as_float(w[r + i] << 16); f[2 * i + 1] = __uint_as_float(w[r + i] & 0xFFFF0000u);
         h[2 * i] = __uint_as_float(z.w[r + i] << 16); h[2 * i + 1] = __uint_as_float(z.w[r + i] & 0xFFFF0000u);
       }
-      op_slope_all<8>(f, h, act);
+      op_slope_all<8, false>(f, h, act);
       Piece<uint16_t, 8> o, rest;
       two_parts<8>(f, parts_shrink(act), o, rest);
 #pragma unroll
@@ -705,7 +705,7 @@ struct ColumnPart<float> {
   }
   __device__ __forceinline__ f32x4_t frag(int odd) const { return f32x4_t{w[odd][0], w[odd][1], w[odd][2], w[odd][3]}; }
   __device__ __forceinline__ void slope(ColumnPart& z, int act, float& s0, float& s1) {
-    op_slope_all<8>(&w[0][0], &z.w[0][0], act);
+    op_slope_all<8, true>(&w[0][0], &z.w[0][0], act);
     sum(s0, s1);
   }
   __device__ __forceinline__ void sum(float& s0, float& s1) const {
@@ -967,7 +967,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* dy, int64_t ldd
       float f[V], g[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) { f[e] = d.at(e); g[e] = act != ABS_ACT_NONE ? h.at(e) : 0.f; }
-      op_slope_all<V>(f, g, act);
+      op_slope_all<V, kFine<T>>(f, g, act);
 #pragma unroll
       for (int e = 0; e < V; ++e) s[e] += f[e];
       o.set(f);

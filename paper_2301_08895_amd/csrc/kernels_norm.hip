@@ -275,7 +275,7 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
             Vec o;
 #pragma unroll
             for (int e = 0; e < V; ++e) h[e] = norm_h(v[k].at(e) - mean, gam[e], bet[e]);
-            op_act_all<V>(h, a.act);
+            op_act_all<V, kFine<T>>(h, a.act);
             o.set(h);
             store_own<TAIL>(o, dst + off, q.nv);
           }
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(1024) void norm_row_kernel(NormArgs<T> a) {
         parameters<TAIL, T, V>(a, (int)c0 + slot * V, own(slot), gam, bet);
 #pragma unroll
         for (int e = 0; e < V; ++e) h[e] = norm_h(v[k].at(e) - mean, gam[e] * rstd, bet[e]);
-        op_act_all<V>(h, a.act);
+        op_act_all<V, kFine<T>>(h, a.act);
         Vec o;
         o.set(h);
         store_own<TAIL>(o, dst + slot * V, own(slot));
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(1024) void norm_apply_kernel(NormArgs<T> a) {
       float h[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) h[e] = norm_h(v.at(e) - mean, gam[e], bet[e]);
-      op_act_all<V>(h, a.act);
+      op_act_all<V, kFine<T>>(h, a.act);
       o.set(h);
       store_own<TAIL>(o, dst, q.nv);
       src += a.PL * a.ldx;
@@ -420,7 +420,7 @@ __device__ __forceinline__ void norm_dh(const Piece<T, V>& x, const Piece<T, V>&
   if (act != ABS_ACT_NONE) {
 #pragma unroll
     for (int e = 0; e < V; ++e) h[e] = norm_h(d[e], s[e], bet[e]);
-    op_slope_all<V>(dh, h, act);
+    op_slope_all<V, kFine<T>>(dh, h, act);
   }
 }
 
@@ -839,7 +839,7 @@ __global__ __launch_bounds__(1024) void norm_plain_kernel(NormArgs<T> a) {
         for (int c = threadIdx.x; c < a.per; c += blockDim.x) {
           const float gam = a.gamma ? a.gamma[c0 + c] : 1.f, bet = a.gamma ? a.beta[c0 + c] : 0.f;
           const float d = op_widen(a.x[(i * a.S + pos) * a.ldx + c0 + c]) - mean, s = gam * rstd;
-          const float w = op_slope(op_widen(a.dy[(i * a.S + pos) * a.lddy + c0 + c]), norm_h(d, s, bet), a.act) * s;
+          const float w = op_slope<kFine<T>>(op_widen(a.dy[(i * a.S + pos) * a.lddy + c0 + c]), norm_h(d, s, bet), a.act) * s;
           s1 += w; s2 += w * d;
         }
       m1 = block_sum(s1, red) * inv;
@@ -851,9 +851,9 @@ __global__ __launch_bounds__(1024) void norm_plain_kernel(NormArgs<T> a) {
         const float gam = a.gamma ? a.gamma[c0 + c] : 1.f, bet = a.gamma ? a.beta[c0 + c] : 0.f;
         const float d = op_widen(a.x[at * a.ldx + c0 + c]) - mean, s = gam * rstd, h = norm_h(d, s, bet);
         float v;
-        if (!BACKWARD) v = op_act(h, a.act);
+        if (!BACKWARD) v = op_act<kFine<T>>(h, a.act);
         else {
-          v = op_slope(op_widen(a.dy[at * a.lddy + c0 + c]), h, a.act) * s - m1 - d * m2;
+          v = op_slope<kFine<T>>(op_widen(a.dy[at * a.lddy + c0 + c]), h, a.act) * s - m1 - d * m2;
           if (a.dres) v += op_widen(a.dres[at * a.lddres + c0 + c]);
         }
         op_narrow(v, a.y[at * a.ldy + c0 + c]);
@@ -875,7 +875,7 @@ __global__ __launch_bounds__(256) void norm_plain_share_kernel(NormArgs<T> a) {
     for (int64_t at = r; at < total; at += a.row_count) {
       const int64_t i = at / a.S;
       const float d = op_widen(a.x[at * a.ldx + c]) - a.mean[i * a.G + g], rstd = a.rstd[i * a.G + g];
-      const float dh = op_slope(op_widen(a.dy[at * a.lddy + c]), norm_h(d, gam * rstd, bet), a.act);
+      const float dh = op_slope<kFine<T>>(op_widen(a.dy[at * a.lddy + c]), norm_h(d, gam * rstd, bet), a.act);
       sg += dh * (d * rstd); sb += dh;
     }
     a.rows_g[(int64_t)r * a.row_step + c] = sg;

@@ -80,78 +80,124 @@ struct Piece {
   }
 };
 
-// ---- activations.  act(z) and act'(z) in fp32; a NaN stays one ----------------------------------------
-__device__ __forceinline__ float op_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }   // 2 ulp
-// The normal distribution function Phi(z) = (1 + erf(z / sqrt 2)) / 2, and e = exp(-z^2 / 2): erfc by the rational form in
-// t = 1 / (1 + p |z| / sqrt 2) of Abramowitz and Stegun, 7.1.26 (|error| of erf <= 1.5e-7), which shares the exponential with the
-// density that the slope needs: 13 operations and two transcendental ones where erff and a further exponential take about 60.
+// ---- activations.  act(z) and act'(z) in fp32; a NaN stays one.  u = 2^-24 is half a step of fp32 ---------------
+// Two evaluations of each: behind fp32 elements (kFine) one that is off by a few steps of the result at every z, behind bf16 ones, whose
+// half step is 2^-8, one of half as many operations.
+template <typename T> constexpr bool kFine = sizeof(T) == 4;
+
+// exp(-s) (1 - c), s in [0, 400], c small: the product s log2(e) in two parts, so that its rounding does not grow with s.
+__device__ __forceinline__ float op_exp_minus(float s, float c) {
+  constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f, kLn2 = 0.693147182f;
+  const float y = s * kLog2e, low = fmaf(s, kRest, fmaf(s, kLog2e, -y));
+  const float e = __builtin_amdgcn_exp2f(-y);
+  return fmaf(-fmaf(low, kLn2, c), e, e);
+}
+// The logistic function p = 1 / (1 + exp(-z)) and q = 1 - p.  Fine: 6 u of either at every z.  Else p's error is a few u of p for z >= 0 and
+// grows to about |z| u of p below (the rounding of z log2(e)): a few u of 1, and 2^-18 of p where z = -80.
+template <bool FINE>
+__device__ __forceinline__ float op_sigmoid(float z, float& q) {
+  if (FINE) {
+    const float e = op_exp_minus(fminf(fabsf(z), 200.f), 0.f), r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
+    q = z < 0.f ? r : er;
+    return z < 0.f ? er : r;
+  }
+  const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+  q = 1.0f - p;
+  return p;
+}
+// The normal distribution function Phi(z) = (1 + erf(z / sqrt 2)) / 2, and e = exp(-z^2 / 2), which the slope's density needs too.
+// Fine: Phi(-x) = e f(x), x = |z|, where f(x) (x + 5/2) is smooth and between 1/2 and 5/4: a polynomial of degree 9 in (x - 5/2) / (x + 5/2) (fitted to
+// [0, 13.6] for the least largest relative error, 0.25 u), e with x^2 in two parts.  10 u of Phi at every z, in 34 operations.
+// Else erfc by the rational form in t = 1 / (1 + p |z| / sqrt 2) of Abramowitz and Stegun, 7.1.26: erf's error is 1.5e-7 at most (a
+// relative error of Phi of 2^-14 at z = -3), in 13 operations; two more in either are transcendental.
+template <bool FINE>
 __device__ __forceinline__ float op_phi(float z, float& e) {
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-  e = __expf(-x * x);
-  const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-  const float tail = 0.5f * q * e;                       // Phi(-|z|)
+  float tail;                                            // Phi(-|z|)
+  if (FINE) {
+    const float x = fminf(fabsf(z), 20.f), h = 0.5f * x, s = h * x;
+    e = op_exp_minus(s, fmaf(h, x, -s));
+    const float t = __builtin_amdgcn_rcpf(x + 2.5f), v = fmaf(-5.0f, t, 1.0f);
+    float f = -0.000156221766f;
+    f = fmaf(f, v, -0.000309014693f);
+    f = fmaf(f, v, 0.000684247119f);
+    f = fmaf(f, v, 0.00252179429f);
+    f = fmaf(f, v, -0.00160130544f);
+    f = fmaf(f, v, -0.0163856447f);
+    f = fmaf(f, v, 0.00923601165f);
+    f = fmaf(f, v, 0.131986931f);
+    f = fmaf(f, v, -0.433692008f);
+    f = fmaf(f, v, 0.706656635f);
+    tail = f * t * e;
+  } else {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    e = __expf(-x * x);
+    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    tail = 0.5f * q * e;
+  }
   return z < 0.f ? tail : 1.0f - tail;
 }
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float op_act(float z) {
   if (ACT == ABS_ACT_RELU) return z < 0.f ? 0.f : z;
-  if (ACT == ABS_ACT_SILU) return z * op_sigmoid(z);
-  if (ACT == ABS_ACT_GELU) { float e; return z * op_phi(z, e); }
+  if (ACT == ABS_ACT_SILU) { float q; return z * op_sigmoid<FINE>(z, q); }
+  if (ACT == ABS_ACT_GELU) { float e; return z * op_phi<FINE>(z, e); }
   return z;
 }
 // d act'(z).  relu: a choice, not a product - nothing of d passes where z is not positive, and it may be infinite there
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float op_slope(float d, float z) {
   if (ACT == ABS_ACT_RELU) return z > 0.f ? d : 0.f;
-  if (ACT == ABS_ACT_SILU) { const float p = op_sigmoid(z); return d * fmaf(z * p, 1.0f - p, p); }
-  if (ACT == ABS_ACT_GELU) { float e; const float c = op_phi(z, e); return d * fmaf(z * 0.39894228040143268f, e, c); }
+  if (ACT == ABS_ACT_SILU) { float q; const float p = op_sigmoid<FINE>(z, q); return d * fmaf(z * p, q, p); }
+  if (ACT == ABS_ACT_GELU) { float e; const float c = op_phi<FINE>(z, e); return d * fmaf(z * 0.39894228040143268f, e, c); }
   return d;
 }
 // N values at once, the activation a uniform run-time value: one branch
-template <int N>
+template <int N, bool FINE>
 __device__ __forceinline__ void op_act_all(float* h, int act) {
   asm volatile("" : "+s"(act));           // (compared here: not once, with the result kept in scalar registers)
   if (act == ABS_ACT_RELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_RELU>(h[i]);
+    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_RELU, FINE>(h[i]);
   } else if (act == ABS_ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_SILU>(h[i]);
+    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_SILU, FINE>(h[i]);
   } else if (act == ABS_ACT_GELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_GELU>(h[i]);
+    for (int i = 0; i < N; ++i) h[i] = op_act<ABS_ACT_GELU, FINE>(h[i]);
   }
 }
 // d[i] = d[i] act'(h[i])
-template <int N>
+template <int N, bool FINE>
 __device__ __forceinline__ void op_slope_all(float* d, const float* h, int act) {
   asm volatile("" : "+s"(act));
   if (act == ABS_ACT_RELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_RELU>(d[i], h[i]);
+    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_RELU, FINE>(d[i], h[i]);
   } else if (act == ABS_ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_SILU>(d[i], h[i]);
+    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_SILU, FINE>(d[i], h[i]);
   } else if (act == ABS_ACT_GELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_GELU>(d[i], h[i]);
+    for (int i = 0; i < N; ++i) d[i] = op_slope<ABS_ACT_GELU, FINE>(d[i], h[i]);
   }
 }
 // the same with the activation as a uniform run-time value
+template <bool FINE>
 __device__ __forceinline__ float op_act(float z, int act) {
   switch (act) {
-    case ABS_ACT_RELU: return op_act<ABS_ACT_RELU>(z);
-    case ABS_ACT_SILU: return op_act<ABS_ACT_SILU>(z);
-    case ABS_ACT_GELU: return op_act<ABS_ACT_GELU>(z);
+    case ABS_ACT_RELU: return op_act<ABS_ACT_RELU, FINE>(z);
+    case ABS_ACT_SILU: return op_act<ABS_ACT_SILU, FINE>(z);
+    case ABS_ACT_GELU: return op_act<ABS_ACT_GELU, FINE>(z);
     default: return z;
   }
 }
+template <bool FINE>
 __device__ __forceinline__ float op_slope(float d, float z, int act) {
   switch (act) {
-    case ABS_ACT_RELU: return op_slope<ABS_ACT_RELU>(d, z);
-    case ABS_ACT_SILU: return op_slope<ABS_ACT_SILU>(d, z);
-    case ABS_ACT_GELU: return op_slope<ABS_ACT_GELU>(d, z);
+    case ABS_ACT_RELU: return op_slope<ABS_ACT_RELU, FINE>(d, z);
+    case ABS_ACT_SILU: return op_slope<ABS_ACT_SILU, FINE>(d, z);
+    case ABS_ACT_GELU: return op_slope<ABS_ACT_GELU, FINE>(d, z);
     default: return d;
   }
 }

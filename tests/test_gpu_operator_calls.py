@@ -111,3 +111,71 @@ def test_infinite_operands_of_a_gradient(rows, d_in, d_out, act, dtype):
     assert torch.isinf(want[0]).any() and torch.isinf(want[1]).any() and torch.isnan(want[0]).any() and torch.isnan(want[1]).any()
     for g, v, s, name in zip(got, want, slack, ("dx", "dw", "db")):
         ou.close(g, v, s, name)
+
+
+def _act64(z, act):
+    """act(z), act'(z), and Phi or the logistic function at z and |z| times its derivative; no cancellation for z < 0."""
+    if act == SILU:
+        p, q = torch.sigmoid(z), torch.sigmoid(-z)
+        return z * p, p * (1 + z * q), p, z.abs() * p * q
+    p = 0.5 * torch.special.erfc(-z / 2 ** 0.5)
+    density = torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+    return z * p, p + z * density, p, z.abs() * density
+
+
+def _points(dtype):
+    z = torch.cat([torch.linspace(-100, 100, 4001), torch.linspace(-6, 6, 4001), torch.randn(4000),
+                   torch.tensor([0.0, -0.0, 2.0 ** -100, -2.0 ** -100, 88.7, -88.7, 1e30, -1e30])])
+    return torch.cat([z, torch.zeros(-len(z) % 64)]).cuda().to(dtype).view(-1, 64)
+
+
+@pytest.mark.parametrize("act", [SILU, GELU])
+@pytest.mark.parametrize("wide", [64, 2048])
+def test_fp32_activations_are_fp32_at_every_z(act, wide):
+    """z = x I exactly, so what is seen is the activation's own error: 10 half steps in the polynomial's and exponential's roundings, two
+    more for each of the two instructions that are one step off, and the product's.  Below 2^-126 (times |z|) the exponential is 0."""
+    z = _points(F32).repeat(1, wide // 64)
+    value, slope, p, part = _act64(z.double(), act)
+    eye = torch.eye(wide, device="cuda")
+    tiny = 2.0 ** -126 * (1 + z.double().abs())
+    y, kept = lib.linear_forward(z, eye, act=act, keep_z=True)
+    assert torch.equal(kept, z)
+    assert ((y.double() - value).abs() <= 16 * ou.U * value.abs() + tiny).all()
+    dx, _, _ = lib.linear_backward(z, eye, torch.ones_like(z), act=act, z=z)
+    assert ((dx.double() - slope).abs() <= 20 * ou.U * (p + part) + tiny).all()
+
+
+@pytest.mark.parametrize("act", [SILU, GELU])
+def test_fp32_activations_behind_a_norm(act):
+    """gamma = 0: the activation's argument is beta."""
+    beta = _points(F32).flatten()
+    value, slope, p, part = _act64(beta.double(), act)
+    tiny = 2.0 ** -126 * (1 + beta.double().abs())
+    x = torch.randn(1, 1, beta.numel(), device="cuda")
+    gamma = torch.zeros_like(beta)
+    for groups in (beta.numel() // 64, 1):
+        y, mean, rstd = lib.group_norm_forward(x, gamma, beta, groups, act=act)
+        assert ((y.flatten().double() - value).abs() <= 16 * ou.U * value.abs() + tiny).all()
+        dbeta = lib.group_norm_backward(x, gamma, beta, mean, rstd, torch.ones_like(x), act=act)[2]
+        assert ((dbeta.double() - slope).abs() <= 20 * ou.U * (p + part) + tiny).all()
+
+
+@pytest.mark.parametrize("act", [SILU, GELU])
+def test_bf16_activations_over_their_range(act):
+    """What is evaluated behind bf16 elements is off by 2^-8 of the result for its rounding, and by 2 (|z| + 8) half steps of fp32 of it
+    (silu) or by erf's 1.5e-7 and four half steps of 1 times |z| / 2 (gelu); the same of the slope's terms.  Where exp(-z) passes fp32, from
+    z = -87 down, silu is 0."""
+    z = _points(BF)
+    value, slope, p, part = _act64(z.double(), act)
+    size = z.double().abs()
+    tiny = 2.0 ** -125 * (1 + size)
+    if act == SILU:
+        off, off_slope = 2 * (size + 8) * ou.U * value.abs(), 2 * (size + 8) * ou.U * (p + part) + 4 * ou.U * (1 + size) * p
+    else:
+        off = size * (0.75e-7 + 4 * ou.U)
+        off_slope = 0.75e-7 + 4 * ou.U + (2 * size * size + 8) * ou.U * part
+    eye = torch.eye(64, device="cuda").to(BF)
+    y = lib.linear_forward(z, eye, act=act)
+    ou.close(y, value, off + tiny, "value")
+    dx, _, _ = lib.linear_backward(z, eye, torch.ones_like(z), act=act, z=z)
+    ou.close(dx, slope, off_slope + tiny + 2.0 ** -15 * slope.abs(), "slope")
