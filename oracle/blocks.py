@@ -2,8 +2,9 @@
 
   a_1 = x W_0 + b_0,  u_l = dropout(act(group norm(a_l))),  a_{l+1} = u_l W_l + b_l (+ a_l where the widths agree),
 softmax cross-entropy on a_L.  Parameter vector: W_0, b_0, then per layer l >= 1 gamma_l, beta_l, W_l, b_l.
-Rounding points of the bf16 path: matrices; a_l; the normalised and activated value; after dropout; the logits' gradient; every
-gradient that is handed on (of u_l, after dropout, of a_l); and each version's matrix gradient.  Sums are wide.
+Rounding points of the bf16 path: matrices; a_l of the hidden layers; the normalised and activated value; after dropout; the logits'
+gradient; every gradient that is handed on (of u_l, after dropout, of a_l); and each version's matrix gradient.  The logits and
+sums are wide.
 """
 from __future__ import annotations
 
@@ -75,7 +76,7 @@ def forward(dims, opt, w, X, masks=None, rnd=round_bf16):
         rec["u"], rec["W"] = u, rnd(W)
         z = u @ rec["W"] + b
         rec["adds"] = bool(opt["residual"] and 1 <= l < L - 1 and dims[l] == dims[l + 1])
-        a = rnd(z + rec["a"]) if rec["adds"] else rnd(z)
+        a = z if l == L - 1 else rnd(z + rec["a"]) if rec["adds"] else rnd(z)
         st.append(rec)
     return a, st
 

@@ -237,7 +237,7 @@ struct BlocksPlan {
   size_t shadow_stride, shadow_off[8];       // bf16 copies of a version's matrices (elements)
   // byte offsets into the workspace
   size_t off_ring, off_shadow, off_label;
-  size_t off_a[8], off_u[8];          // a_l (l = 0: the gathered rows), u_l: bf16 [N B][d_l]
+  size_t off_a[8], off_u[8];          // a_l (l = 0: the gathered rows; the logits a_L have none), u_l: bf16 [N B][d_l]
   size_t off_mean[8], off_rstd[8];
   size_t off_da[2], off_du;           // gradients of a_{l+1} / a_l in turn, of u_l
   size_t off_dw, off_dv;              // one version's gradient of a matrix (bf16), of vectors (fp32)

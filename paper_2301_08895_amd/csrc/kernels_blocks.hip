@@ -3,7 +3,7 @@
 //   a_{l+1} = u_l W_l + b_l (+ a_l where the widths agree),   logits = a_L,   softmax cross-entropy.
 // A round is a chain of the library's own operators over the stacked minibatches, layer by layer; within a layer one
 // call per model version that the round's uploads computed at (their rows are contiguous: the descriptor lists them grouped by
-// version).  Activations and gradients are bf16; the models of the ring, the sums and the update are fp32, each
+// version).  Activations and gradients are bf16; the models of the ring, the logits, the sums and the update are fp32, each
 // version's matrices are narrowed to bf16 once.  The bf16 gradient of a version's matrix (coefficients of Eq. 3 in it) is subtracted
 // from the fp32 model, oldest version first.
 #include <hip/hip_runtime.h>
@@ -31,9 +31,9 @@ __global__ __launch_bounds__(128) void blocks_gather_kernel(const uint16_t* X, c
   if (threadIdx.x == 0) label[m] = y[row];
 }
 
-// A wavefront per row of logits [rows][C], C <= 256: loss, and either the gradient c_k (p - 1_y) or whether the first largest
-// logit is the label.
-__global__ __launch_bounds__(256) void blocks_loss_kernel(const uint16_t* z, int C, int rows, const int32_t* label, int B, RoundDesc rd,
+// A wavefront per row of logits, C <= 256, which arrive in fp32 as the shares of the output layer's product: loss, and either the gradient
+// c_k (p - 1_y) or whether the first largest logit is the label.  Rows m of one model version; row0: the stack's rows before them.
+__global__ __launch_bounds__(256) void blocks_loss_kernel(OpShares z, const float* bias, int C, int rows, const int32_t* label, int row0, int B, RoundDesc rd,
                                                           float* rowloss, uint16_t* dz, float* correct) {
   const int lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (m >= rows) return;
@@ -43,7 +43,14 @@ __global__ __launch_bounds__(256) void blocks_loss_kernel(const uint16_t* z, int
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int c = lane + 64 * q;
-    v[q] = c < C ? op_widen(z[(size_t)m * C + c]) : -INFINITY;
+    v[q] = -INFINITY;
+    if (c < C) {
+      const float* const p = z.part + m * z.ld + c;
+      float s = p[0];
+#pragma unroll 4
+      for (int k = 1; k < z.shares; ++k) s += p[k * z.stride];
+      v[q] = s + bias[c];
+    }
     if (v[q] > top || v[q] != v[q]) { top = v[q]; best = c; }       // (a NaN stays on top: the loss is NaN)
   }
 #pragma unroll
@@ -67,7 +74,7 @@ __global__ __launch_bounds__(256) void blocks_loss_kernel(const uint16_t* z, int
     if (correct) correct[m] = best == lab ? 1.f : 0.f;
   }
   if (!dz) return;
-  const float coef = rd.w[m / B].c, inv = 1.0f / sum;
+  const float coef = rd.w[(row0 + m) / B].c, inv = 1.0f / sum;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int c = lane + 64 * q;
@@ -124,6 +131,9 @@ bool adds(const BlocksPlan& p, int l) { return p.opt.residual && l >= 1 && l < p
 // Uploads of one model version: rows [row, row + rows) of the stack.
 struct Group { uint32_t slot; int64_t row, rows; };
 
+// What the output layer's rows become: losses, and gradients (dz, with the descriptor's coefficients) or hits (correct).
+struct LossOut { const int32_t* label; const RoundDesc& rd; float* rowloss; uint16_t* dz; float* correct; int kind; };
+
 struct Chain {
   const BlocksArgs& a;
   const BlocksPlan& p;
@@ -142,8 +152,8 @@ struct Chain {
   void did(int r) { if (rc == ABS_OK) rc = r; }
   void launched() { if (rc == ABS_OK) rc = op_hip("blocks", hipGetLastError()); }
 
-  // a_1 .. a_L of `rows` stacked rows; drop_base < 0: no dropout (evaluation)
-  void forward(const Group* g, int groups, int64_t rows, int64_t drop_base) {
+  // a_1 .. a_{L-1} of `rows` stacked rows and what `out` wants of the logits; drop_base < 0: no dropout (evaluation)
+  void forward(const Group* g, int groups, int64_t rows, int64_t drop_base, const LossOut& out) {
     for (int l = 0; l < p.L && rc == ABS_OK; ++l) {
       if (l) {
         hook->begin(KK_BLOCKS_NORM, 10.0 * rows * p.d[l], 4.0 * rows * p.d[l]);
@@ -162,6 +172,10 @@ struct Chain {
           hook->end(KK_BLOCKS_DROPOUT);
         }
       }
+      if (l == p.L - 1) {
+        for (int i = 0; i < groups; ++i) output(g[i], out);
+        continue;
+      }
       hook->begin(KK_BLOCKS_LINEAR, 2.0 * rows * p.d[l] * p.d[l + 1], 2.0 * (rows * (double)(p.d[l] + p.d[l + 1]) + (double)p.d[l] * p.d[l + 1]));
       for (int i = 0; i < groups; ++i) {
         const abs_linear q = linear_of(p, l, g[i].rows);
@@ -171,6 +185,24 @@ struct Chain {
       }
       hook->end(KK_BLOCKS_LINEAR);
     }
+  }
+
+  // the logits of one version's rows stay in the product's fp32 shares until the loss has read them: rounded to bf16, two of them closer
+  // than half a step would be equal, and the first one the largest
+  void output(const Group& g, const LossOut& out) {
+    const int l = p.L - 1, C = p.d[p.L];
+    const abs_linear q = linear_of(p, l, g.rows);
+    OpShares z{};
+    hook->begin(KK_BLOCKS_LINEAR, 2.0 * g.rows * p.d[l] * C, 2.0 * (g.rows * (double)p.d[l] + 2.0 * g.rows * C + (double)p.d[l] * C));
+    did(op_linear_forward_shares(&q, in(l) + (size_t)g.row * p.d[l], narrow(g.slot, l), at<void>(p.off_ops), p.ops_bytes, s, &z));
+    hook->end(KK_BLOCKS_LINEAR);
+    if (rc != ABS_OK) return;
+    hook->begin(out.kind, 8.0 * g.rows * C, 4.0 * g.rows * C + (out.dz ? 2.0 * g.rows * C : 0));
+    blocks_loss_kernel<<<dim3((unsigned)((g.rows + 3) / 4)), 256, 0, s>>>(z, model(g.slot) + p.b_off[l], C, (int)g.rows, out.label + g.row, (int)g.row, p.B, out.rd,
+                                                                         out.rowloss + g.row, out.dz ? out.dz + (size_t)g.row * C : nullptr,
+                                                                         out.correct ? out.correct + g.row : nullptr);
+    launched();
+    hook->end(out.kind);
   }
 
   // next -= the change of n parameters at `off`; `fresh`: the first one, from the current model
@@ -267,7 +299,7 @@ bool blocks_plan(const abs_config& c, const abs_blocks& b, BlocksPlan& p, const 
   p.off_ring = take((size_t)p.R * p.slot_stride * 4);
   p.off_shadow = take((size_t)p.R * p.shadow_stride * 2);
   p.off_label = take(rows * 4);
-  for (int l = 0; l <= L; ++l) p.off_a[l] = take(rows * p.d[l] * 2);
+  for (int l = 0; l < L; ++l) p.off_a[l] = take(rows * p.d[l] * 2);
   for (int l = 1; l < L; ++l) {
     p.off_u[l] = take(rows * p.d[l] * 2);
     p.off_mean[l] = take(rows * b.groups * 4);
@@ -284,7 +316,7 @@ bool blocks_plan(const abs_config& c, const abs_blocks& b, BlocksPlan& p, const 
     for (int back = 0; back < passes; ++back)
       for (int l = 0; l < L; ++l) {
         const abs_linear q = linear_of(p, l, n);
-        p.ops_bytes = std::max(p.ops_bytes, abs_linear_workspace_size(&q, back, 0));
+        p.ops_bytes = std::max(p.ops_bytes, !back && l == L - 1 ? op_linear_shares_size(&q) : abs_linear_workspace_size(&q, back, 0));
         if (!l) continue;
         const abs_group_norm g = norm_of(p, l, n);
         p.ops_bytes = std::max(p.ops_bytes, abs_group_norm_workspace_size(&g, back));
@@ -322,12 +354,8 @@ hipError_t launch_blocks_round(const BlocksArgs& a, const RoundDesc& rd, hipStre
   blocks_gather_kernel<<<dim3((unsigned)rows), 128, 0, s>>>(a.X, a.y, p.d[0], a.shard_rows, a.batch_key, p.B, rd, c.act(0), c.at<int32_t>(p.off_label));
   c.launched();
   hook->end(KK_BLOCKS_LOSS);
-  c.forward(g, groups, rows, drop_base);
-  const int C = p.d[p.L];
-  hook->begin(KK_BLOCKS_LOSS, 8.0 * rows * C, 4.0 * rows * C);
-  blocks_loss_kernel<<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(c.act(p.L), C, (int)rows, c.at<int32_t>(p.off_label), p.B, rd,
-                                                                     c.at<float>(p.off_rowloss), c.at<uint16_t>(p.off_da[p.L & 1]), nullptr);
-  c.launched();
+  c.forward(g, groups, rows, drop_base, LossOut{c.at<int32_t>(p.off_label), rd, c.at<float>(p.off_rowloss), c.at<uint16_t>(p.off_da[p.L & 1]), nullptr, KK_BLOCKS_LOSS});
+  hook->begin(KK_BLOCKS_LOSS, (double)rows, 4.0 * rows);
   blocks_publish_kernel<<<dim3(1), 128, 0, s>>>(c.at<float>(p.off_rowloss), p.B, K, a.mailbox, rd.stamp);
   c.launched();
   hook->end(KK_BLOCKS_LOSS);
@@ -351,13 +379,8 @@ hipError_t launch_blocks_eval(const BlocksArgs& a, uint32_t slot, const EvalArgs
     n = (int)(left >= cap ? cap : left >= p.B ? left / p.B * p.B : left);
     const Group g{slot, 0, n};
     c.x0 = (const uint16_t*)e.X + (size_t)row0 * p.d[0];
-    c.forward(&g, 1, n, -1);
-    hook->begin(KK_EVAL, 8.0 * n * p.d[p.L], 2.0 * n * p.d[p.L]);
     const RoundDesc none{};
-    blocks_loss_kernel<<<dim3((unsigned)((n + 3) / 4)), 256, 0, s>>>(c.act(p.L), p.d[p.L], n, (const int32_t*)e.y + row0, p.B, none, e.rowloss,
-                                                                   nullptr, e.correct);
-    c.launched();
-    hook->end(KK_EVAL);
+    c.forward(&g, 1, n, -1, LossOut{(const int32_t*)e.y + row0, none, e.rowloss, nullptr, e.correct, KK_EVAL});
     err = c.result();
     if (err == hipSuccess) err = launch_eval_reduce(e, n, s, hook);
   }

@@ -1034,6 +1034,7 @@ struct TileCost { double start, step, start2, step2, big_start, big_step; };
 TileCost tile_cost(int dtype) { return dtype == ABS_X_BF16 ? TileCost{5, 0.78, 7, 1.04, 12, 1.4} : TileCost{8, 2.2, 8, 4.1, 0, 0}; }
 double join_cost(int64_t split, int64_t M, int64_t N) { return split > 1 ? 3 + (double)split * M * N * 8 / 6e6 : 0; }
 
+size_t shares_bytes(int shares, int64_t M, int64_t N) { return (size_t)shares * M * op_round_up(N, 4) * 4; }
 Product cut_product(int64_t M, int64_t N, int64_t K, int dtype, bool big, int64_t split) {
   Product q{};
   const int tile = big ? kBig : kTile, step = dtype == ABS_X_BF16 ? 64 : 32;
@@ -1043,7 +1044,7 @@ Product cut_product(int64_t M, int64_t N, int64_t K, int dtype, bool big, int64_
   const int64_t steps = (K + step - 1) / step;
   q.steps_per_split = (int)((steps + split - 1) / split);
   q.nsplit = (int)((steps + q.steps_per_split - 1) / q.steps_per_split);
-  if (q.nsplit > 1) q.part_bytes = (size_t)q.nsplit * M * op_round_up(N, 4) * 4;
+  if (q.nsplit > 1) q.part_bytes = shares_bytes(q.nsplit, M, N);
   return q;
 }
 constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
@@ -1131,8 +1132,8 @@ struct LinearPlan {
   size_t off_x, off_w, off_dz, off_sums, off_part, off_part2, bytes;
 };
 
-// aligned: the pointers are; need_copy of x / w and, for the backward pass, of dy into dz
-LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok, bool dy_ok) {
+// x_ok, w_ok, dy_ok: the pointers are aligned to pieces.  shares: the forward product stays in shares, also where there is one.
+LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok, bool dy_ok, bool shares = false) {
   LinearPlan q{};
   const int size = op_size(p.dtype), piece = 16 / size;
   q.in8 = (int64_t)op_round_up(p.d_in, piece);
@@ -1144,14 +1145,14 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
   q.small = small_product(p, backward);
   if (q.small) {
     const int block = p.dtype == ABS_X_BF16 ? 16 : 8;
-    auto split = [&](int64_t M, int64_t N, int64_t K, int rows_of_tile) {
+    auto split = [&](int64_t M, int64_t N, int64_t K, int rows_of_tile, bool keep) {
       SmallProduct s{};
       s.nt = (int)((N + 63) / 64);
       s.tiles = (int)((M + rows_of_tile - 1) / rows_of_tile) * s.nt;
       // a long contraction of few tiles in shares, four blocks a wavefront at least
       const int64_t blocks = (K + block - 1) / block, each = 4 * kSmallWaves;
-      const int64_t shares = blocks <= (p.dtype == ABS_X_BF16 && rows_of_tile == 32 ? 4 : 2) * each ? 1 : std::max<int64_t>(1, std::min<int64_t>((blocks + each - 1) / each, 640 / s.tiles));
-      s.steps = (int)((blocks + shares - 1) / shares);
+      const int64_t cuts = blocks <= (p.dtype == ABS_X_BF16 && rows_of_tile == 32 ? 4 : 2) * each ? 1 : std::max<int64_t>(1, std::min<int64_t>((blocks + each - 1) / each, 640 / s.tiles));
+      s.steps = (int)((blocks + cuts - 1) / cuts);
       s.splits = (int)((blocks + s.steps - 1) / s.steps);
       // several tiles in a workgroup: with blocks too few for eight wavefronts as long as every CU has a workgroup, else two
       // (30000 x 300 x 20, gradients 81 -> 50 us; 2 x 645 x 23, whose few workgroups would do eight tiles' epilogues each, 8 -> 21)
@@ -1159,11 +1160,11 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
       s.team = kSmallWaves;
       while (s.team > 1 && mt * s.nt * s.splits * (s.team / 2) >= (s.team / 2 >= mine ? 256 : 512) * kSmallWaves) s.team /= 2;
       s.tiles = (int)((mt * s.team + kSmallWaves - 1) / kSmallWaves) * s.nt;
-      s.part_bytes = s.splits > 1 ? op_round_up((size_t)s.splits * M * op_round_up(N, 4) * 4, 256) : 0;
+      s.part_bytes = s.splits > 1 || keep ? op_round_up(shares_bytes(s.splits, M, N), 256) : 0;
       return s;
     };
-    q.sa = backward ? split(p.rows, p.d_in, p.d_out, 32) : split(p.rows, p.d_out, p.d_in, 32);
-    if (backward) q.sb = split(p.d_in, p.d_out, p.rows, 64);
+    q.sa = backward ? split(p.rows, p.d_in, p.d_out, 32, false) : split(p.rows, p.d_out, p.d_in, 32, shares);
+    if (backward) q.sb = split(p.d_in, p.d_out, p.rows, 64, false);
     q.off_part = take(q.sa.part_bytes);
     q.off_dz = take(q.sb.part_bytes);
     q.off_sums = take(q.sb.splits > 1 ? (size_t)q.sb.splits * p.d_out * 4 : 0);
@@ -1176,6 +1177,7 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     if (q.pack_x) q.off_x = take((size_t)p.rows * q.in8 * size);
     if (q.pack_w) q.off_w = take((size_t)p.d_in * q.out8 * size);
     q.fwd = plan_product(p.rows, p.d_out, p.d_in, p.dtype, nullptr);
+    if (shares) q.fwd.part_bytes = shares_bytes(q.fwd.nsplit, p.rows, p.d_out);
     q.off_part = take(q.fwd.part_bytes);
   } else {
     q.pack_x = !x_whole;
@@ -1249,21 +1251,30 @@ hipError_t launch_join(const Join<T>& a, const Join<T>& b, const DbShares& d, hi
   return hipGetLastError();
 }
 
-// g with the plan's tiles and, where its contraction is cut, shares that go to `part` and join into what g wanted
+// shares of a product that its caller adds: nothing is joined
 template <typename T>
-Join<T> set_product(const Product& q, GemmArgs<T>& g, float* part) {
+void hand_over(Join<T>& j, OpShares* out) {
+  *out = OpShares{j.e.part, j.e.ldpart, j.e.part_stride, j.shares};
+  j = Join<T>{};
+}
+
+// g with the plan's tiles and, where its contraction is cut (or `keep` wants its shares), shares that go to `part` and join into what g wanted
+template <typename T>
+Join<T> set_product(const Product& q, GemmArgs<T>& g, float* part, OpShares* keep = nullptr) {
   g.mt = q.mt; g.nt = q.nt; g.nsplit = q.nsplit; g.steps_per_split = q.steps_per_split;
-  if (q.nsplit == 1) return Join<T>{};
+  if (q.nsplit == 1 && !keep) return Join<T>{};
   g.e.ldpart = (int64_t)op_round_up(g.N, 4);
   g.e.part_stride = g.M * g.e.ldpart;
   g.e.part = part;
-  return Join<T>{g.e, g.M, g.N, q.nsplit};
+  Join<T> join{g.e, g.M, g.N, q.nsplit};
+  if (keep) hand_over(join, keep);
+  return join;
 }
 int product_blocks(const Product& q) { return (q.mt * q.nt * q.nsplit + 7) / 8 * 8; }
 
 template <typename T, bool ATR, bool BTR>
-hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, const DbShares& d, hipStream_t s) {
-  const Join<T> join = set_product(q, g, part);
+hipError_t run_product(const Product& q, GemmArgs<T> g, float* part, const DbShares& d, OpShares* keep, hipStream_t s) {
+  const Join<T> join = set_product(q, g, part, keep);
   const dim3 grid((unsigned)product_blocks(q));
   if (q.big) {
     if constexpr (sizeof(T) == 2) linear_big_kernel<ATR, BTR><<<grid, 512, 0, s>>>(g);
@@ -1282,27 +1293,28 @@ SmallArgs<T> small_args(const abs_linear& p, const void* x, const void* w) {
 }
 // one product of linear_small_kernel, and what joins its shares (join.shares stays 0 where there is one)
 template <typename T>
-SmallPart<T> small_part(const SmallProduct& q, const Epilogue<T>& e, float* part, int64_t M, int64_t N, Join<T>& join) {
+SmallPart<T> small_part(const SmallProduct& q, const Epilogue<T>& e, float* part, int64_t M, int64_t N, Join<T>& join, OpShares* keep = nullptr) {
   SmallPart<T> s{e, q.nt, q.tiles, q.splits, q.steps, q.team};
-  if (q.splits > 1) {
+  if (q.splits > 1 || keep) {
     s.e.part = part;
     s.e.ldpart = (int64_t)op_round_up(N, 4);
     s.e.part_stride = M * s.e.ldpart;
     join = Join<T>{s.e, M, N, q.splits};
+    if (keep) hand_over(join, keep);
   }
   return s;
 }
 
 template <typename T>
 hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, const void* w, const float* b, const void* r, void* y, void* z,
-                       char* ws, hipStream_t s) {
+                       OpShares* keep, char* ws, hipStream_t s) {
   Epilogue<T> e{};
   e.bias = b; e.r = (const T*)r; e.y = (T*)y; e.z = (T*)z;
   e.ldr = p.ldr; e.ldy = p.ldy; e.ldz = p.ldz; e.act = p.act;
   if (q.small) {
     SmallArgs<T> g = small_args<T>(p, x, w);
     Join<T> join{};
-    g.a = small_part(q.sa, e, (float*)(ws + q.off_part), p.rows, p.d_out, join);
+    g.a = small_part(q.sa, e, (float*)(ws + q.off_part), p.rows, p.d_out, join, keep);
     const dim3 grid((unsigned)(q.sa.tiles * q.sa.splits));
     if (q.sa.team == kSmallWaves) linear_small_kernel<T, false, kSmallWaves><<<grid, 512, 0, s>>>(g);
     else                          linear_small_kernel<T, false, 0><<<grid, 512, 0, s>>>(g);
@@ -1319,7 +1331,7 @@ hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, 
   if (err != hipSuccess) return err;
   g.M = p.rows; g.N = p.d_out; g.K = p.d_in; g.nc = q.out8; g.mc = 0;
   g.e = e;
-  return run_product<T, false, true>(q.fwd, g, part, DbShares{}, s);
+  return run_product<T, false, true>(q.fwd, g, part, DbShares{}, keep, s);
 }
 
 template <typename T>
@@ -1390,12 +1402,45 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     err = hipGetLastError();
     return err == hipSuccess ? launch_join(ja, jb, d, s) : err;
   }
-  if (dx) { err = run_product<T, false, false>(q.dx, ga, part, d, s); d = DbShares{}; }
-  if (err == hipSuccess && dw) { err = run_product<T, true, true>(q.dw, gb, part, d, s); d = DbShares{}; }
+  if (dx) { err = run_product<T, false, false>(q.dx, ga, part, d, nullptr, s); d = DbShares{}; }
+  if (err == hipSuccess && dw) { err = run_product<T, true, true>(q.dw, gb, part, d, nullptr, s); d = DbShares{}; }
   return err == hipSuccess ? launch_join(Join<T>{}, Join<T>{}, d, s) : err;
 }
 
+// Both passes behind their checks of what they write: keep: shares (OpShares) in place of y.
+int forward_call(const abs_linear* p, const void* x, const void* w, const float* b, const void* r, void* y, void* z, OpShares* keep, void* ws,
+                 size_t bytes, hipStream_t s) {
+  if (!x || !w || !(y || keep)) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
+  const uintptr_t all = (uintptr_t)x | (uintptr_t)w | (uintptr_t)r | (uintptr_t)y | (uintptr_t)z;
+  if (all & (uintptr_t)(op_size(p->dtype) - 1) || (uintptr_t)b & 3) return op_fail(ABS_E_ARG, "linear: a pointer is not aligned to its elements");
+  const LinearPlan q = linear_plan(*p, false, op_aligned(x, 16), op_aligned(w, 16), true, keep != nullptr);
+  if (q.bytes && (!ws || (uintptr_t)ws & 255)) return op_fail(ABS_E_ARG, "linear: d_workspace must be 256-byte aligned");
+  if (bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "linear: workspace too small");
+  const hipError_t e = p->dtype == ABS_X_BF16 ? forward_run<uint16_t>(*p, q, x, w, b, r, y, z, keep, (char*)ws, s)
+                                              : forward_run<float>(*p, q, x, w, b, r, y, z, keep, (char*)ws, s);
+  return op_hip("abs_linear_forward", e);
+}
+
+int backward_call(const abs_linear* p, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, float* db, void* ws,
+                  size_t bytes, hipStream_t s) {
+  if (!dy || (dw && !x) || (dx && !w) || (p->act != ABS_ACT_NONE && !z)) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
+  const LinearPlan q = linear_plan(*p, true, op_aligned(x, 16), op_aligned(w, 16), op_aligned(dy, 16));
+  if (q.bytes && (!ws || (uintptr_t)ws & 255)) return op_fail(ABS_E_ARG, "linear: d_workspace must be 256-byte aligned");
+  if (bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "linear: workspace too small");
+  const hipError_t e = p->dtype == ABS_X_BF16 ? backward_run<uint16_t>(*p, q, x, w, z, dy, dx, dw, db, (char*)ws, s)
+                                              : backward_run<float>(*p, q, x, w, z, dy, dx, dw, db, (char*)ws, s);
+  return op_hip("abs_linear_backward", e);
+}
+
 }  // namespace
+
+// (the library's own calls: operands aligned, pitches checked where the arrays are laid out)
+size_t op_linear_shares_size(const abs_linear* p) noexcept { return linear_plan(*p, false, false, false, false, true).bytes; }
+int op_linear_forward_shares(const abs_linear* p, const void* d_x, const void* d_w, void* d_workspace, size_t workspace_bytes, void* hip_stream,
+                             OpShares* product) noexcept {
+  if (const char* why = linear_problem(p, false)) return op_fail(ABS_E_ARG, why);
+  return forward_call(p, d_x, d_w, nullptr, nullptr, nullptr, nullptr, product, d_workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
 }  // namespace abs_impl
 
 using namespace abs_impl;
@@ -1413,16 +1458,7 @@ int abs_linear_forward(const abs_linear* p, const void* d_x, const void* d_w, co
   if (bad_pitch(p->ldy, p->d_out) || (d_z && bad_pitch(p->ldz, p->d_out)) || (d_r && bad_pitch(p->ldr, p->d_out)))
     return op_fail(ABS_E_ARG, "linear: a pitch is below the row's length, or 2^32 or more");
   if (p->rows == 0) return ABS_OK;
-  if (!d_x || !d_w || !d_y) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
-  const uintptr_t all = (uintptr_t)d_x | (uintptr_t)d_w | (uintptr_t)d_r | (uintptr_t)d_y | (uintptr_t)d_z;
-  if (all & (uintptr_t)(op_size(p->dtype) - 1) || (uintptr_t)d_b & 3) return op_fail(ABS_E_ARG, "linear: a pointer is not aligned to its elements");
-  const LinearPlan q = linear_plan(*p, false, op_aligned(d_x, 16), op_aligned(d_w, 16), true);
-  if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "linear: d_workspace must be 256-byte aligned");
-  if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "linear: workspace too small");
-  const hipError_t e = p->dtype == ABS_X_BF16
-      ? forward_run<uint16_t>(*p, q, d_x, d_w, d_b, d_r, d_y, d_z, (char*)d_workspace, (hipStream_t)hip_stream)
-      : forward_run<float>(*p, q, d_x, d_w, d_b, d_r, d_y, d_z, (char*)d_workspace, (hipStream_t)hip_stream);
-  return op_hip("abs_linear_forward", e);
+  return forward_call(p, d_x, d_w, d_b, d_r, d_y, d_z, nullptr, d_workspace, workspace_bytes, (hipStream_t)hip_stream);
 }
 
 int abs_linear_backward(const abs_linear* p, const void* d_x, const void* d_w, const void* d_z, const void* d_dy,
@@ -1446,14 +1482,7 @@ int abs_linear_backward(const abs_linear* p, const void* d_x, const void* d_w, c
     if (e == hipSuccess && d_db) { linear_zero_kernel<float><<<few_blocks(p->d_out), 256, 0, s>>>(d_db, p->d_out, 1, p->d_out); e = hipGetLastError(); }
     return op_hip("abs_linear_backward", e);
   }
-  if (!d_dy || (d_dw && !d_x) || (d_dx && !d_w) || (p->act != ABS_ACT_NONE && !d_z)) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
-  const LinearPlan q = linear_plan(*p, true, op_aligned(d_x, 16), op_aligned(d_w, 16), op_aligned(d_dy, 16));
-  if (q.bytes && (!d_workspace || (uintptr_t)d_workspace & 255)) return op_fail(ABS_E_ARG, "linear: d_workspace must be 256-byte aligned");
-  if (workspace_bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "linear: workspace too small");
-  const hipError_t e = p->dtype == ABS_X_BF16
-      ? backward_run<uint16_t>(*p, q, d_x, d_w, d_z, d_dy, d_dx, d_dw, d_db, (char*)d_workspace, s)
-      : backward_run<float>(*p, q, d_x, d_w, d_z, d_dy, d_dx, d_dw, d_db, (char*)d_workspace, s);
-  return op_hip("abs_linear_backward", e);
+  return backward_call(p, d_x, d_w, d_z, d_dy, d_dx, d_dw, d_db, d_workspace, workspace_bytes, s);
 }
 
 }  // extern "C"

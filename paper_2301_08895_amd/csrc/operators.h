@@ -10,6 +10,14 @@ namespace abs_impl {
 int op_fail(int code, const char* text) noexcept;
 int op_hip(const char* what, hipError_t e) noexcept;     // ABS_OK for hipSuccess
 
+// A product left as the fp32 shares of its contraction: element (m, n) is the sum over k < shares of part[k stride + m ld + n], in that order.
+struct OpShares { const float* part; int64_t ld, stride; int shares; };
+// abs_linear_forward's x W left so (in d_workspace, until something else is done there), for sums that are used in fp32 at once.
+// op_linear_shares_size(): what it needs of d_workspace, at any alignment of the operands.
+size_t op_linear_shares_size(const abs_linear* p) noexcept;
+int op_linear_forward_shares(const abs_linear* p, const void* d_x, const void* d_w, void* d_workspace, size_t workspace_bytes, void* hip_stream,
+                             OpShares* product) noexcept;
+
 inline size_t op_round_up(size_t x, size_t m) { return (x + m - 1) / m * m; }
 inline bool op_aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 inline int op_size(int dtype) { return dtype == ABS_X_BF16 ? 2 : 4; }

@@ -179,3 +179,41 @@ def test_bf16_activations_over_their_range(act):
     ou.close(y, value, off + tiny, "value")
     dx, _, _ = lib.linear_backward(z, eye, torch.ones_like(z), act=act, z=z)
     ou.close(dx, slope, off_slope + tiny + 2.0 ** -15 * slope.abs(), "slope")
+
+
+# ---- what the rounds of residual blocks hold in fp32 ----------------------------------------------------
+def _blocks(dims, N=4, B=16, **over):
+    import workloads
+    p = workloads.scaled_preset(3, M=2000, dims=dims, n_classes=dims[-1], N=N, B=B, n_slow=1, lr=0.05, K0=N, k_mode=1, tau_cap=3, **over)
+    p = workloads.with_blocks(p, groups=4, drop=0)
+    return p, workloads.make_split(p, 333)
+
+
+def _last_bias(w0, dims):
+    return w0[w0.size - dims[-1]:]
+
+
+@pytest.mark.parametrize("dims", [[16, 24, 10], [32, 64, 64, 33], [16, 520, 200]])
+def test_logits_closer_than_a_bf16_step(dims):
+    """W_{L-1} = 0: the logits are the biases, 16 and steps of 0.01 above it, where bf16 has steps of 0.125: losses are those of the biases,
+    and a row is a hit where its label is the last class."""
+    import numpy as np
+    p, (train, Xe, ye) = _blocks(dims)
+    C, d = dims[-1], dims[-2]
+    w0 = train["w0"].copy()
+    w0[w0.size - C - d * C:] = 0.0
+    _last_bias(w0, dims)[:] = 16 + 0.01 * np.arange(C)
+    train = dict(train, w0=w0)
+    bias = _last_bias(w0, dims).astype(np.float64)
+    per_class = np.log(np.exp(bias - bias[-1]).sum()) + bias[-1] - bias
+    sim = lib.Simulation(p, train)
+    loss, acc = sim.evaluate(Xe, ye)
+    # a loss is a logarithm of a sum of C exponentials less a difference, each a few half steps of numbers up to log C + 0.01 C
+    tol = 64 * ou.U * (np.log(C) + 0.01 * C + 1)
+    assert abs(loss - per_class[ye].mean()) <= tol
+    assert acc == (ye == C - 1).mean()
+    sim.round(1)
+    rows = np.concatenate([lib.abs_draw_batch_rows(sim.cfg, n, 0) for n in range(p["N"])])
+    got = float(sim.trace()[0][10:11].view(np.float32)[0])
+    assert abs(got - per_class[train["y"][rows]].mean()) <= tol + p["B"] * ou.U * per_class.max()
+    sim.close()
