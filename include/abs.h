@@ -168,8 +168,8 @@ int abs_create(const abs_config* cfg, const void* d_X, const void* d_y, const fl
  *   a_{l+1} = u_l W_l + b_l, plus a_l where residual = 1, l < L - 1 and d_l = d_{l+1},
  * softmax cross-entropy on a_L; held-out evaluation leaves dropout out.  Normalisation is per sample, so it needs
  * nothing from the other workers' data.  Model vector (d_w0, abs_get_model): W_0, b_0, then per layer l >= 1
- * gamma_l [d_l], beta_l [d_l], W_l [d_l, d_{l+1}], b_l.  bf16 operands, activations and matrix gradients (one per
- * model version of a round), fp32 accumulation, statistics, logits and master parameters.  Masks: abs_dropout's with the
+ * gamma_l [d_l], beta_l [d_l], W_l [d_l, d_{l+1}], b_l.  bf16 operands, activations and their gradients; fp32 accumulation,
+ * statistics, logits, gradients of parameters and master parameters.  Masks: abs_dropout's with the
  * handle's seed at offset 8 t + l over round t's stacked minibatches (uploads grouped by model version, oldest first).
  *  groups     of every hidden layer: divides d_1 .. d_{L-1}
  *  act        ABS_ACT_*;  residual 0 / 1;  drop: probability in 65536ths, 0 = none;  eps > 0: of the normalisation

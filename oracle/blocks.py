@@ -3,8 +3,7 @@
   a_1 = x W_0 + b_0,  u_l = dropout(act(group norm(a_l))),  a_{l+1} = u_l W_l + b_l (+ a_l where the widths agree),
 softmax cross-entropy on a_L.  Parameter vector: W_0, b_0, then per layer l >= 1 gamma_l, beta_l, W_l, b_l.
 Rounding points of the bf16 path: matrices; a_l of the hidden layers; the normalised and activated value; after dropout; the logits'
-gradient; every gradient that is handed on (of u_l, after dropout, of a_l); and each version's matrix gradient.  The logits and
-sums are wide.
+gradient; every gradient that is handed on (of u_l, after dropout, of a_l).  The logits, matrix gradients and sums are wide.
 """
 from __future__ import annotations
 
@@ -98,7 +97,7 @@ def gradient(dims, opt, w, X, y, coef, masks=None, rnd=round_bf16):
     params = unpack(dims, np.asarray(w, dtype=np.float64))
     for l in range(len(st) - 1, -1, -1):
         r, (gg, gb, gW, gbias) = st[l], grads[l]
-        gW[:] = rnd(r["u"].T @ da)
+        gW[:] = r["u"].T @ da
         gbias[:] = da.sum(0)
         if not l:
             break

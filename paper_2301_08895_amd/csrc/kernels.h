@@ -240,7 +240,7 @@ struct BlocksPlan {
   size_t off_a[8], off_u[8];          // a_l (l = 0: the gathered rows; the logits a_L have none), u_l: bf16 [N B][d_l]
   size_t off_mean[8], off_rstd[8];
   size_t off_da[2], off_du;           // gradients of a_{l+1} / a_l in turn, of u_l
-  size_t off_dw, off_dv;              // one version's gradient of a matrix (bf16), of vectors (fp32)
+  size_t off_dv;                      // one version's gradient of vectors (fp32; of a matrix: in the product's shares)
   size_t off_rowloss, off_ops, ops_bytes, off_eval, total;
 };
 bool blocks_plan(const abs_config& cfg, const abs_blocks& blocks, BlocksPlan& plan, const char** why);

@@ -3,9 +3,9 @@
 //   a_{l+1} = u_l W_l + b_l (+ a_l where the widths agree),   logits = a_L,   softmax cross-entropy.
 // A round is a chain of the library's own operators over the stacked minibatches, layer by layer; within a layer one
 // call per model version that the round's uploads computed at (their rows are contiguous: the descriptor lists them grouped by
-// version).  Activations and gradients are bf16; the models of the ring, the logits, the sums and the update are fp32, each
-// version's matrices are narrowed to bf16 once.  The bf16 gradient of a version's matrix (coefficients of Eq. 3 in it) is subtracted
-// from the fp32 model, oldest version first.
+// version).  Activations and gradients of activations are bf16, the matrix cores' operands; the models of the ring, the logits, the sums and the update are
+// fp32, each version's matrices are narrowed to bf16 once.  The gradient of a version's matrix (coefficients of Eq. 3 in it) goes from
+// the shares of its product, in fp32, into the fp32 model, oldest version first.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -91,10 +91,33 @@ __global__ __launch_bounds__(128) void blocks_publish_kernel(const float* rowlos
   post_loss(box, k, s / (float)B, stamp);
 }
 
-// next = from - change, for a matrix's bf16 and a vector's fp32 change
-template <typename T>
-__global__ __launch_bounds__(256) void blocks_step_kernel(float* next, const float* from, const T* change, size_t n) {
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) next[i] = from[i] - op_widen(change[i]);
+// next = from - change
+__global__ __launch_bounds__(256) void blocks_step_kernel(float* next, const float* from, const float* change, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) next[i] = from[i] - change[i];
+}
+
+// ... for a matrix, whose change is a product's shares (their rows are whole quads), added in their order
+__global__ __launch_bounds__(256) void blocks_matrix_step_kernel(float* next, const float* from, OpShares d, uint32_t rows, int cols) {
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+  const uint32_t quads = (uint32_t)d.ld / 4, total = rows * quads;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
+    const uint32_t m = i / quads;
+    const int n = (int)(i - m * quads) * 4;
+    const float* const p = d.part + (int64_t)m * d.ld + n;
+    f32x4_t s = *(const f32x4_t*)p;
+#pragma unroll 4
+    for (int k = 1; k < d.shares; ++k) s += *(const f32x4_t*)(p + k * d.stride);
+    const int64_t at = (int64_t)m * cols + n;
+    if (n + 4 <= cols) {
+      Piece<float, 4> w;
+      w.load(from + at);
+      const float f[4] = {w.at(0) - s[0], w.at(1) - s[1], w.at(2) - s[2], w.at(3) - s[3]};
+      w.set(f);
+      w.store(next + at);
+    } else {
+      for (int e = 0; n + e < cols; ++e) next[at + e] = from[at + e] - s[e];
+    }
+  }
 }
 
 __global__ __launch_bounds__(256) void blocks_narrow_kernel(const float* w, size_t rows, int cols, uint16_t* out, int ld) {
@@ -205,17 +228,22 @@ struct Chain {
     hook->end(out.kind);
   }
 
-  // next -= the change of n parameters at `off`; `fresh`: the first one, from the current model
-  template <typename T>
-  void step(float* next, const float* cur, size_t off, const T* change, size_t n, bool fresh) {
-    blocks_step_kernel<T><<<spread(n), 256, 0, s>>>(next + off, (fresh ? cur : next) + off, change, n);
+  // next -= the change of n parameters at `off`, or of matrix l; `fresh`: the first one, from the current model
+  void step(float* next, const float* cur, size_t off, const float* change, size_t n, bool fresh) {
+    if (rc != ABS_OK) return;
+    blocks_step_kernel<<<spread(n), 256, 0, s>>>(next + off, (fresh ? cur : next) + off, change, n);
+    launched();
+  }
+  void step(float* next, const float* cur, int l, const OpShares& change, bool fresh) {
+    if (rc != ABS_OK) return;
+    blocks_matrix_step_kernel<<<spread((size_t)p.d[l] * change.ld / 4), 256, 0, s>>>(next + p.w_off[l], (fresh ? cur : next) + p.w_off[l], change,
+                                                                                   (uint32_t)p.d[l], p.d[l + 1]);
     launched();
   }
 
   void backward(const Group* g, int groups, int64_t rows, int64_t drop_base, uint32_t slot_cur, uint32_t slot_next) {
     float* const next = at<float>(p.off_ring) + (size_t)slot_next * p.slot_stride;
     const float* const cur = model(slot_cur);
-    uint16_t* const dw = at<uint16_t>(p.off_dw);
     float* const dv = at<float>(p.off_dv);
     // the gradient of a_{l+1} is in da[l & 1] (the logits': where the loss left it)
     for (int l = p.L - 1; l >= 0 && rc == ABS_OK; --l) {
@@ -225,9 +253,10 @@ struct Chain {
       for (int i = 0; i < groups; ++i) {
         const abs_linear q = linear_of(p, l, g[i].rows);
         const size_t off = (size_t)g[i].row * p.d[l];
-        did(abs_linear_backward(&q, in(l) + off, narrow(g[i].slot, l), nullptr, dy + (size_t)g[i].row * p.d[l + 1], l ? du + off : nullptr,
-                                dw, dv, at<void>(p.off_ops), p.ops_bytes, s));
-        step(next, cur, p.w_off[l], dw, (size_t)p.d[l] * p.d[l + 1], i == 0);
+        OpShares dw{};
+        did(op_linear_backward_shares(&q, in(l) + off, narrow(g[i].slot, l), nullptr, dy + (size_t)g[i].row * p.d[l + 1], l ? du + off : nullptr,
+                                      dv, at<void>(p.off_ops), p.ops_bytes, s, &dw));
+        step(next, cur, l, dw, i == 0);
         step(next, cur, p.b_off[l], dv, (size_t)p.d[l + 1], i == 0);
       }
       hook->end(KK_BLOCKS_LINEAR);
@@ -293,9 +322,8 @@ bool blocks_plan(const abs_config& c, const abs_blocks& b, BlocksPlan& p, const 
   size_t t = 0;
   auto take = [&](size_t bytes) { const size_t at = t; t = up(t + bytes, 256); return at; };
   const size_t rows = (size_t)p.N * p.B;
-  size_t widest = 0, matrix = 0;
+  size_t widest = 0;
   for (int l = 1; l <= L; ++l) widest = std::max(widest, (size_t)p.d[l]);
-  for (int l = 0; l < L; ++l) matrix = std::max(matrix, (size_t)p.d[l] * p.d[l + 1]);
   p.off_ring = take((size_t)p.R * p.slot_stride * 4);
   p.off_shadow = take((size_t)p.R * p.shadow_stride * 2);
   p.off_label = take(rows * 4);
@@ -307,7 +335,6 @@ bool blocks_plan(const abs_config& c, const abs_blocks& b, BlocksPlan& p, const 
   }
   for (int i = 0; i < 2; ++i) p.off_da[i] = take(rows * widest * 2);
   p.off_du = take(rows * widest * 2);
-  p.off_dw = take(matrix * 2);
   p.off_dv = take(2 * widest * 4);
   p.off_rowloss = take(rows * 4);
   // the operators' own workspace: for any number of uploads of one version, and the last rows of an evaluation
@@ -316,7 +343,7 @@ bool blocks_plan(const abs_config& c, const abs_blocks& b, BlocksPlan& p, const 
     for (int back = 0; back < passes; ++back)
       for (int l = 0; l < L; ++l) {
         const abs_linear q = linear_of(p, l, n);
-        p.ops_bytes = std::max(p.ops_bytes, !back && l == L - 1 ? op_linear_shares_size(&q) : abs_linear_workspace_size(&q, back, 0));
+        p.ops_bytes = std::max(p.ops_bytes, back || l == L - 1 ? op_linear_shares_size(&q, back) : abs_linear_workspace_size(&q, back, 0));
         if (!l) continue;
         const abs_group_norm g = norm_of(p, l, n);
         p.ops_bytes = std::max(p.ops_bytes, abs_group_norm_workspace_size(&g, back));

@@ -1132,7 +1132,7 @@ struct LinearPlan {
   size_t off_x, off_w, off_dz, off_sums, off_part, off_part2, bytes;
 };
 
-// x_ok, w_ok, dy_ok: the pointers are aligned to pieces.  shares: the forward product stays in shares, also where there is one.
+// x_ok, w_ok, dy_ok: the pointers are aligned to pieces.  shares: the forward product, or dW, stays in shares, also where there is one.
 LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok, bool dy_ok, bool shares = false) {
   LinearPlan q{};
   const int size = op_size(p.dtype), piece = 16 / size;
@@ -1164,7 +1164,7 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
       return s;
     };
     q.sa = backward ? split(p.rows, p.d_in, p.d_out, 32, false) : split(p.rows, p.d_out, p.d_in, 32, shares);
-    if (backward) q.sb = split(p.d_in, p.d_out, p.rows, 64, false);
+    if (backward) q.sb = split(p.d_in, p.d_out, p.rows, 64, shares);
     q.off_part = take(q.sa.part_bytes);
     q.off_dz = take(q.sb.part_bytes);
     q.off_sums = take(q.sb.splits > 1 ? (size_t)q.sb.splits * p.d_out * 4 : 0);
@@ -1193,11 +1193,13 @@ LinearPlan linear_plan(const abs_linear& p, bool backward, bool x_ok, bool w_ok,
     double ca, cb;
     q.dx = plan_product(p.rows, p.d_in, p.d_out, p.dtype, &ca);
     q.dw = plan_product(p.d_in, p.d_out, p.rows, p.dtype, &cb);
+    if (shares) q.dw.part_bytes = shares_bytes(q.dw.nsplit, p.d_in, p.d_out);
     q.off_part = take(std::max(q.dx.part_bytes, q.dw.part_bytes));
     q.off_part2 = q.off_part;
     Product a, b;
     if (plan_pair(p, ca + cb, a, b)) {        // (used where both are asked for)
       q.pair = true;
+      if (shares) b.part_bytes = shares_bytes(b.nsplit, p.d_in, p.d_out);
       q.pair_dx = a; q.pair_dw = b;
       q.off_part2 = q.off_part + op_round_up(b.part_bytes, 256);
       o = std::max(o, op_round_up(q.off_part2 + a.part_bytes, 256));
@@ -1336,8 +1338,9 @@ hipError_t forward_run(const abs_linear& p, const LinearPlan& q, const void* x, 
 
 template <typename T>
 hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw,
-                        float* db, char* ws, hipStream_t s) {
+                        OpShares* keep, float* db, char* ws, hipStream_t s) {          // keep: dW's shares in place of dW
   constexpr int V = kPiece<T>;
+  const bool want_dw = dw || keep;
   hipError_t err = hipSuccess;
   if (q.small) {
     SmallArgs<T> g = small_args<T>(p, x, w);
@@ -1348,10 +1351,10 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     Join<T> ja{}, jb{};
     DbShares d{};
     if (dx) g.a = small_part(q.sa, ea, (float*)(ws + q.off_part), p.rows, p.d_in, ja);
-    if (dw || db) {
-      g.b = small_part(q.sb, eb, (float*)(ws + q.off_dz), dw ? p.d_in : 0, p.d_out, jb);
-      if (!dw) g.b.tiles = g.b.nt;                            // (db alone: the first row of dW's tiles)
-      g.dw = dw != nullptr;
+    if (want_dw || db) {
+      g.b = small_part(q.sb, eb, (float*)(ws + q.off_dz), want_dw ? p.d_in : 0, p.d_out, jb, keep);
+      if (!want_dw) g.b.tiles = g.b.nt;                            // (db alone: the first row of dW's tiles)
+      g.dw = want_dw;
       g.db = db && q.sb.splits > 1 ? (float*)(ws + q.off_sums) : db;
       if (db && q.sb.splits > 1) d = DbShares{g.db, q.sb.splits, p.d_out, db};
     }
@@ -1365,7 +1368,7 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
   }
   const T* dz = (const T*)dy;
   int64_t lddz = p.lddy;
-  const bool products = dx || dw;
+  const bool products = dx || want_dw;
   DbShares d{};
   float* sums = db ? (float*)(ws + q.off_sums) : nullptr;
   if ((q.dz && products) || db) {
@@ -1385,16 +1388,16 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     ga.M = p.rows; ga.N = p.d_in; ga.K = p.d_out;
     ga.e.y = (T*)dx; ga.e.ldy = p.lddx;
   }
-  if (err == hipSuccess && dw) {
+  if (err == hipSuccess && want_dw) {
     gb.A = (const T*)x; gb.lda = p.ldx; gb.B = dz; gb.ldb = lddz;
     if (q.pack_x) { gb.A = (const T*)(ws + q.off_x); gb.lda = q.in8; }
     gb.M = p.d_in; gb.N = p.d_out; gb.K = p.rows; gb.mc = q.in8; gb.nc = q.out8;
     gb.e.y = (T*)dw; gb.e.ldy = p.lddw;
   }
-  if (err == hipSuccess) err = pack_operands<T>(p, q, x, w, dw != nullptr, dx != nullptr, ws, s);
+  if (err == hipSuccess) err = pack_operands<T>(p, q, x, w, want_dw, dx != nullptr, ws, s);
   if (err != hipSuccess) return err;
-  if (q.pair && dx && dw) {
-    const Join<T> jb = set_product(q.pair_dw, gb, part), ja = set_product(q.pair_dx, ga, (float*)(ws + q.off_part2));
+  if (q.pair && dx && want_dw) {
+    const Join<T> jb = set_product(q.pair_dw, gb, part, keep), ja = set_product(q.pair_dx, ga, (float*)(ws + q.off_part2));
     const int first = product_blocks(q.pair_dw);
     const dim3 grid((unsigned)(first + product_blocks(q.pair_dx)));
     if (!q.pair_dw.big) linear_tile_pair_kernel<T><<<grid, 256, 0, s>>>(gb, ga, first);
@@ -1403,11 +1406,11 @@ hipError_t backward_run(const abs_linear& p, const LinearPlan& q, const void* x,
     return err == hipSuccess ? launch_join(ja, jb, d, s) : err;
   }
   if (dx) { err = run_product<T, false, false>(q.dx, ga, part, d, nullptr, s); d = DbShares{}; }
-  if (err == hipSuccess && dw) { err = run_product<T, true, true>(q.dw, gb, part, d, nullptr, s); d = DbShares{}; }
+  if (err == hipSuccess && want_dw) { err = run_product<T, true, true>(q.dw, gb, part, d, keep, s); d = DbShares{}; }
   return err == hipSuccess ? launch_join(Join<T>{}, Join<T>{}, d, s) : err;
 }
 
-// Both passes behind their checks of what they write: keep: shares (OpShares) in place of y.
+// Both passes behind their checks of what they write: keep: shares (OpShares) in place of y, or of dW.
 int forward_call(const abs_linear* p, const void* x, const void* w, const float* b, const void* r, void* y, void* z, OpShares* keep, void* ws,
                  size_t bytes, hipStream_t s) {
   if (!x || !w || !(y || keep)) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
@@ -1421,26 +1424,32 @@ int forward_call(const abs_linear* p, const void* x, const void* w, const float*
   return op_hip("abs_linear_forward", e);
 }
 
-int backward_call(const abs_linear* p, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, float* db, void* ws,
-                  size_t bytes, hipStream_t s) {
-  if (!dy || (dw && !x) || (dx && !w) || (p->act != ABS_ACT_NONE && !z)) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
-  const LinearPlan q = linear_plan(*p, true, op_aligned(x, 16), op_aligned(w, 16), op_aligned(dy, 16));
+int backward_call(const abs_linear* p, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, OpShares* keep, float* db,
+                  void* ws, size_t bytes, hipStream_t s) {
+  if (!dy || ((dw || keep) && !x) || (dx && !w) || (p->act != ABS_ACT_NONE && !z)) return op_fail(ABS_E_ARG, "linear: a device pointer is NULL");
+  const LinearPlan q = linear_plan(*p, true, op_aligned(x, 16), op_aligned(w, 16), op_aligned(dy, 16), keep != nullptr);
   if (q.bytes && (!ws || (uintptr_t)ws & 255)) return op_fail(ABS_E_ARG, "linear: d_workspace must be 256-byte aligned");
   if (bytes < q.bytes) return op_fail(ABS_E_WORKSPACE, "linear: workspace too small");
-  const hipError_t e = p->dtype == ABS_X_BF16 ? backward_run<uint16_t>(*p, q, x, w, z, dy, dx, dw, db, (char*)ws, s)
-                                              : backward_run<float>(*p, q, x, w, z, dy, dx, dw, db, (char*)ws, s);
+  const hipError_t e = p->dtype == ABS_X_BF16 ? backward_run<uint16_t>(*p, q, x, w, z, dy, dx, dw, keep, db, (char*)ws, s)
+                                              : backward_run<float>(*p, q, x, w, z, dy, dx, dw, keep, db, (char*)ws, s);
   return op_hip("abs_linear_backward", e);
 }
 
 }  // namespace
 
 // (the library's own calls: operands aligned, pitches checked where the arrays are laid out)
-size_t op_linear_shares_size(const abs_linear* p) noexcept { return linear_plan(*p, false, false, false, false, true).bytes; }
+size_t op_linear_shares_size(const abs_linear* p, int32_t backward) noexcept { return linear_plan(*p, backward != 0, false, false, false, true).bytes; }
 int op_linear_forward_shares(const abs_linear* p, const void* d_x, const void* d_w, void* d_workspace, size_t workspace_bytes, void* hip_stream,
                              OpShares* product) noexcept {
   if (const char* why = linear_problem(p, false)) return op_fail(ABS_E_ARG, why);
   return forward_call(p, d_x, d_w, nullptr, nullptr, nullptr, nullptr, product, d_workspace, workspace_bytes, (hipStream_t)hip_stream);
 }
+int op_linear_backward_shares(const abs_linear* p, const void* d_x, const void* d_w, const void* d_z, const void* d_dy, void* d_dx, float* d_db,
+                              void* d_workspace, size_t workspace_bytes, void* hip_stream, OpShares* dw) noexcept {
+  if (const char* why = linear_problem(p, true)) return op_fail(ABS_E_ARG, why);
+  return backward_call(p, d_x, d_w, d_z, d_dy, d_dx, nullptr, dw, d_db, d_workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
+
 }  // namespace abs_impl
 
 using namespace abs_impl;
@@ -1482,7 +1491,7 @@ int abs_linear_backward(const abs_linear* p, const void* d_x, const void* d_w, c
     if (e == hipSuccess && d_db) { linear_zero_kernel<float><<<few_blocks(p->d_out), 256, 0, s>>>(d_db, p->d_out, 1, p->d_out); e = hipGetLastError(); }
     return op_hip("abs_linear_backward", e);
   }
-  return backward_call(p, d_x, d_w, d_z, d_dy, d_dx, d_dw, d_db, d_workspace, workspace_bytes, s);
+  return backward_call(p, d_x, d_w, d_z, d_dy, d_dx, d_dw, nullptr, d_db, d_workspace, workspace_bytes, s);
 }
 
 }  // extern "C"

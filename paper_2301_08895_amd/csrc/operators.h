@@ -12,11 +12,13 @@ int op_hip(const char* what, hipError_t e) noexcept;     // ABS_OK for hipSucces
 
 // A product left as the fp32 shares of its contraction: element (m, n) is the sum over k < shares of part[k stride + m ld + n], in that order.
 struct OpShares { const float* part; int64_t ld, stride; int shares; };
-// abs_linear_forward's x W left so (in d_workspace, until something else is done there), for sums that are used in fp32 at once.
-// op_linear_shares_size(): what it needs of d_workspace, at any alignment of the operands.
-size_t op_linear_shares_size(const abs_linear* p) noexcept;
+// abs_linear_forward's x W and abs_linear_backward with dW left so (in d_workspace, until something else is done there), for sums that are used in
+// fp32 at once; d_dx and d_db may be NULL.  op_linear_shares_size(): what they need of d_workspace, at any alignment of the operands.
+size_t op_linear_shares_size(const abs_linear* p, int32_t backward) noexcept;
 int op_linear_forward_shares(const abs_linear* p, const void* d_x, const void* d_w, void* d_workspace, size_t workspace_bytes, void* hip_stream,
                              OpShares* product) noexcept;
+int op_linear_backward_shares(const abs_linear* p, const void* d_x, const void* d_w, const void* d_z, const void* d_dy, void* d_dx, float* d_db,
+                              void* d_workspace, size_t workspace_bytes, void* hip_stream, OpShares* dw) noexcept;
 
 inline size_t op_round_up(size_t x, size_t m) { return (x + m - 1) / m * m; }
 inline bool op_aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }

@@ -217,3 +217,19 @@ def test_logits_closer_than_a_bf16_step(dims):
     got = float(sim.trace()[0][10:11].view(np.float32)[0])
     assert abs(got - per_class[train["y"][rows]].mean()) <= tol + p["B"] * ou.U * per_class.max()
     sim.close()
+
+
+@pytest.mark.parametrize("dims,B", [([16, 24, 10], 16), ([64, 128, 128, 50], 40), ([1024, 1096, 200], 128)])
+def test_matrix_gradients_are_not_rounded_on_their_way_into_the_model(dims, B):
+    """From W_{L-1} = 0 the first round's matrix is the gradient, coefficients and signs included: one rounded to bf16 has 16 bits of zeros."""
+    import numpy as np
+    p, (train, _, _) = _blocks(dims, B=B)
+    w0 = train["w0"].copy()
+    C, d = dims[-1], dims[-2]
+    w0[w0.size - C - d * C:] = 0.0
+    sim = lib.Simulation(p, dict(train, w0=w0))
+    sim.round(1)
+    last = sim.model()[w0.size - C - d * C:w0.size - C]
+    low = last.view(np.uint32) & 0xFFFF
+    assert (last != 0).mean() > 0.9 and (low != 0).mean() > 0.9
+    sim.close()
