@@ -233,3 +233,118 @@ def test_matrix_gradients_are_not_rounded_on_their_way_into_the_model(dims, B):
     low = last.view(np.uint32) & 0xFFFF
     assert (last != 0).mean() > 0.9 and (low != 0).mean() > 0.9
     sim.close()
+
+
+# ---- several tiles of a small product in one workgroup: two, four or eight of dW (few rows, wide layers), of the forward product and of dx
+# (many rows, narrow layers), in both dtypes
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,d_in,d_out", [(8, 2048, 2048), (9, 2047, 2045), (60, 2000, 2050), (1, 2900, 1450), (20, 1030, 4095), (30000, 300, 20),
+                                             (30000, 24, 20), (100_000, 64, 64), (70_000, 17, 9), (12_000, 9, 3000), (70_000, 2, 3), (40_000, 130, 33)])
+def test_several_small_tiles_in_a_workgroup(rows, d_in, d_out, dtype):
+    x, w = normal(rows, d_in, dtype), normal(d_in, d_out, dtype, d_in ** -0.5)
+    b, r = torch.randn(d_out, device="cuda"), normal(rows, d_out, dtype)
+    y, z = lib.linear_forward(x, w, b, act=SILU, residual=r, keep_z=True)
+    want, wz, sy, sz = ou.linear(x, w, b, SILU, r)
+    ou.close(z, wz, sz, "z")
+    ou.close(y, want, sy, "y")
+    dy = normal(rows, d_out, dtype)
+    want, slack = ou.linear_gradient(x, w, z, dy, SILU)
+    whole = lib.linear_backward(x, w, dy, act=SILU, z=z)
+    for g, v, s, name in zip(whole, want, slack, ("dx", "dw", "db")):
+        ou.close(g, v, s, name)
+    for only in range(3):
+        one = lib.linear_backward(x, w, dy, act=SILU, z=z, need_dx=only == 0, need_dw=only == 1, need_db=only == 2)
+        assert [g is not None for g in one] == [i == only for i in range(3)]
+        ou.close(one[only], want[only], slack[only], f"{only} alone")        # (not the same bits: without the others its contraction may be cut elsewhere)
+
+
+# ---- dz of small bf16 gradients: two bf16 values
+@pytest.mark.parametrize("act", [SILU, GELU])
+@pytest.mark.parametrize("rows,d_in,d_out", [(64, 48, 64), (300, 200, 130), (2000, 64, 40), (9, 2047, 515)])
+def test_small_bf16_gradients_round_once(rows, d_in, d_out, act):
+    """dz reaches the matrix cores to 2^-15 of itself (its second bf16 value, at most 2^-7 of it, is off by 2^-8 of that), so dx and dW are off by
+    their own rounding and little else; with dz rounded to bf16 once they would not be."""
+    x, w = normal(rows, d_in, BF), normal(d_in, d_out, BF, d_in ** -0.5)
+    z, dy = normal(rows, d_out, BF), normal(rows, d_out, BF)
+    got = lib.linear_backward(x, w, dy, act=act, z=z)
+    want, slack = ou.linear_gradient(x.float(), w.float(), z.float(), dy.float(), act)         # (their slacks without dz's rounding)
+    dz = (dy.double() * ou.slope(z.double(), act))
+    wide, tall = w.double().t().contiguous(), x.double().t().contiguous()
+    sx, sw = slack[0] + 2.0 ** -15 * (dz.abs() @ wide.abs()), slack[1] + 2.0 ** -15 * (tall.abs() @ dz.abs())
+    ou.close(got[0], want[0], sx, "dx")
+    ou.close(got[1], want[1], sw, "dw")
+    once = dz.to(BF).double()
+    for coarse, v, s, length in ((once @ wide, want[0], sx, d_out), (tall @ once, want[1], sw, rows)):
+        if length > 300:
+            continue
+        with pytest.raises(AssertionError):
+            ou.close(coarse.to(BF), v, s)
+
+
+# ---- group norm: pitches of its own for each array of a gradient, results and everything around them
+def _padded(n, S, C, pad, lead, dtype, fill=float("nan")):
+    """([n, S, C] view of normal values in rows that are pad longer, the whole memory, a mask of the rest of it)."""
+    flat = torch.full((lead + n * S * (C + pad),), fill, dtype=dtype, device="cuda")
+    view = flat[lead:].view(n, S, C + pad)[:, :, :C]
+    view.copy_(torch.randn(n, S, C, device="cuda"))
+    rest = torch.ones_like(flat, dtype=torch.bool)
+    rest[lead:].view(n, S, C + pad)[:, :, :C] = False
+    return view, flat, rest
+
+
+# samples whole, in parts, single positions, wide ones, groups of the plain kernel; starts that are no whole piece
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,S,C,G,lead", [(3, 50, 32, 8, 0), (3, 50, 32, 8, 1), (2, 1, 32, 8, 3), (1, 9000, 32, 8, 0), (2, 20000, 12, 3, 1), (300, 1, 264, 1, 0),
+                                          (5, 1, 4096, 1, 8), (40, 9, 224, 32, 0), (3, 4, 1200, 2, 2), (2, 3, 16400, 2, 1)])
+def test_group_norm_gradient_at_pitches_of_its_own(n, S, C, G, lead, dtype):
+    (x, *_), (dy, *_), (res, *_) = (_padded(n, S, C, pad, lead, dtype) for pad in (8, 3, 16))
+    out, flat, rest = _padded(n, S, C, 5, lead, dtype, 7.0)
+    gamma, beta = 1 + 0.3 * torch.randn(C, device="cuda"), 0.3 * torch.randn(C, device="cuda")
+    y, mean, rstd = lib.group_norm_forward(x, gamma, beta, G, act=SILU, out=out)
+    assert y is out and (flat[rest] == 7).all()
+    for g, v, s, name in zip((y, mean, rstd), *ou.norm(x, gamma, beta, G, 1e-5, SILU), ("y", "mean", "rstd")):
+        ou.close(g, v, s, name)
+    for r in (res, None):
+        want, slack = ou.norm_gradient(x, gamma, beta, mean, rstd, dy, r, SILU)
+        got = lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=SILU, residual=r, out=out)
+        assert got[0] is out and (flat[rest] == 7).all()
+        for g, v, s, name in zip(got, want, slack, ("dx", "dgamma", "dbeta")):
+            ou.close(g, v, s, name)
+    over, flat, rest = _padded(n, S, C, 5, lead, dtype, 7.0)
+    want, slack = ou.norm_gradient(x, gamma, beta, mean, rstd, dy, over.clone(), SILU)
+    got = lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=SILU, residual=over, out=over)
+    assert (flat[rest] == 7).all()
+    for g, v, s, name in zip(got, want, slack, ("dx over the residual", "dgamma", "dbeta")):
+        ou.close(g, v, s, name)
+
+
+# ---- rounds of residual blocks whose products run on tiles: whole pieces, copied operands, several versions a round
+@pytest.mark.parametrize("over", [dict(dims=[64, 1536, 1536, 100], groups=32, K0=8), dict(dims=[72, 1530, 1530, 37], groups=5, K0=8, act=1),
+                                  dict(dims=[64, 1400, 1400, 1400, 10], groups=7, K0=5)])
+def test_wide_blocks_follow_the_oracle(over):
+    import numpy as np
+    import workloads
+    from test_gpu_blocks import TOL, oracle_rounds, preset, tensors
+    from oracle import blocks as ob
+    from oracle.bf16 import bits_to_f64
+    p = preset(N=8, B=160, **over)
+    d, Xe, ye = workloads.make_split(p, 1500)
+    sim = lib.Simulation(p, d)
+    T = 3
+    got = [sim.model()]
+    for _ in range(T):
+        sim.round(1)
+        got.append(sim.model())
+    want, losses = oracle_rounds(p, d, sim, T)
+    trace = sim.trace()
+    for t in range(T):
+        gl = float(trace[t][10:11].view(np.float32)[0])
+        assert abs(gl - losses[t]) <= TOL * max(1.0, losses[t]), t
+    for t in (1, T):
+        for name, s in tensors(p):
+            up, back = got[t][s].astype(np.float64) - got[0][s], want[t][s] - want[0][s]
+            assert np.linalg.norm(up - back) <= TOL * max(np.linalg.norm(back), 1e-12), (t, name)
+    loss, _ = sim.evaluate(Xe, ye)
+    per_row, _ = ob.loss_of(ob.forward(p["dims"], p["blocks"], sim.model(), bits_to_f64(Xe))[0], ye)
+    assert abs(loss - per_row.mean()) <= TOL * max(1.0, per_row.mean())
+    sim.close()
