@@ -348,3 +348,34 @@ def test_wide_blocks_follow_the_oracle(over):
     per_row, _ = ob.loss_of(ob.forward(p["dims"], p["blocks"], sim.model(), bits_to_f64(Xe))[0], ye)
     assert abs(loss - per_row.mean()) <= TOL * max(1.0, per_row.mean())
     sim.close()
+
+
+# ---- the ends of the documented ranges
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,d_in,d_out", [(1, 1 << 20, 3), (2, 3, 1 << 20), (1, 1, 1 << 20), (1, 1 << 20, 1), ((1 << 22) + 3, 1, 1), ((1 << 22) + 3, 2, 2),
+                                             ((1 << 21) + 1, 3, 1)])
+def test_linear_at_the_ends_of_its_range(rows, d_in, d_out, dtype):
+    x, w = normal(rows, d_in, dtype), normal(d_in, d_out, dtype, d_in ** -0.5)
+    b = torch.randn(d_out, device="cuda")
+    y, z = lib.linear_forward(x, w, b, act=SILU, keep_z=True)
+    want, wz, sy, sz = ou.linear(x, w, b, SILU, None)
+    ou.close(z, wz, sz, "z")
+    ou.close(y, want, sy, "y")
+    dy = normal(rows, d_out, dtype)
+    for g, v, s, name in zip(lib.linear_backward(x, w, dy, act=SILU, z=z), *ou.linear_gradient(x, w, z, dy, SILU), ("dx", "dw", "db")):
+        ou.close(g, v, s, name)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,S,C,G", [(2, 1, 1 << 20, 1), (2, 1, 1 << 20, 1 << 20), (1, 1 << 22, 1, 1), (1 << 22, 1, 2, 1), (1 << 20, 3, 2, 2), (1, 2, 1 << 20, 1 << 10)])
+def test_group_norm_at_the_ends_of_its_range(n, S, C, G, dtype):
+    x, dy = normal(n * S, C, dtype).view(n, S, C), normal(n * S, C, dtype).view(n, S, C)
+    gamma, beta = 1 + 0.3 * torch.randn(C, device="cuda"), 0.3 * torch.randn(C, device="cuda")
+    # (groups of one or two values: eps keeps the reciprocal deviation, and with it every error, near 1)
+    got = lib.group_norm_forward(x, gamma, beta, G, eps=1.0, act=SILU)
+    for g, v, s, name in zip(got, *ou.norm(x, gamma, beta, G, 1.0, SILU), ("y", "mean", "rstd")):
+        ou.close(g, v, s, name)
+    _, mean, rstd = got
+    want, slack = ou.norm_gradient(x, gamma, beta, mean, rstd, dy, None, SILU)
+    for g, v, s, name in zip(lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=SILU), want, slack, ("dx", "dgamma", "dbeta")):
+        ou.close(g, v, s, name)
