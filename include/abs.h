@@ -370,7 +370,8 @@ int abs_calibrate_mfma(int32_t data_mode, int32_t iters, int32_t workgroups, flo
  * fp32).  Any size, pitch and alignment that the elements allow is taken (a large product of matrices whose rows'
  * length, pitch or start are not multiples of 16 bytes copies them into the workspace first).  What lies between a
  * row's end and the next row is neither read nor written.  Sums, statistics and products are held in fp32 and
- * rounded once to the output's dtype; they have a fixed order (no float atomics): two calls give the same bits.
+ * rounded once to the output's dtype; they have a fixed order (no float atomics): two calls give the same bits.  silu, gelu and
+ * their slopes are off by a few half steps of fp32 behind fp32 elements, by little against bf16's own step behind bf16 ones.
  *
  * Every call enqueues on hip_stream (of the device that is current) and returns; nothing is allocated, copied to
  * the host or waited for, so calls can be captured into a HIP graph.  d_workspace: at least *_workspace_size()

@@ -935,8 +935,11 @@ __global__ __launch_bounds__(512, 2) void linear_small_kernel(SmallArgs<T> g) {
 
 // ---------------------------------------------------------------------- dz = dy act'(z), and its column sums
 // 256 threads: 32 pieces of columns, 8 rows at a time; a workgroup's shares of the column sums leave in `sums` [gridDim.y][N].  Rows of dz
-// are whole pieces (lddz), zeros from N on.  Bound by memory: 8192 x 2048 bf16 19 us, 5.3 TB/s, a large copy's rate (WHOLE: N is whole
-// pieces; with the ends' branch 23).
+// are whole pieces (lddz), zeros from N on.  Bound by memory: 8192 x 2048 bf16 18 us, 5.6 TB/s, a large copy's rate and more (WHOLE: N is whole
+// pieces; with the ends' branch 23).  bf16: silu's and gelu's dz is rounded once here, for products whose operands go from memory to LDS
+// as they are.  dx and dW are then off by 2.3e-3 in the norm, their own rounding alone by 1.65e-3 (which is what two_parts leaves small products).  Two values here
+// would make both contractions twice as long: 8192 x 2048 x 2048, dx 61 -> 104 us and dW 92 -> 143, where the whole pass takes 165.
+// relu's dz, and dy itself, are bf16 values already.
 template <bool WHOLE, typename T>
 __device__ __forceinline__ void load_columns(Piece<T, kPiece<T>>& v, const T* p, int count) {
   constexpr int V = kPiece<T>;

@@ -195,9 +195,9 @@ __device__ __forceinline__ void place_work(uint32_t b, uint32_t per_sample, uint
 // Forward.  APPLY: one part holds the sample (parts == 1) and the result is written; else only the part's mean and squared
 // distances are left.  NP positions per lane.  Addresses are a uniform base and a 32-bit
 // offset that walks, so that they cost two registers and not two per piece (with 64 registers of values that decides whether
-// anything spills).  bf16 64 x 4096 x 256 in 32 groups with silu: 67 to 72 us, 3.7 to 4.0 TB/s where a copy moves 5.1: about 40 us
-// of vector instructions (19 an element, two of them transcendental) that a workgroup as large as its CU's registers hides only in
-// part.  In 512 lanes, two workgroups on a CU and 32 bytes of a position each, 99 us.
+// anything spills).  bf16 64 x 4096 x 256 in 32 groups with silu: 67 to 73 us, 3.7 to 4.0 TB/s where a copy moves 5.1: the vector units are
+// busy 48 % of the time (18 instructions an element, two of them transcendental), which a workgroup as large as its CU's registers hides
+// only in part.  In 512 lanes, two workgroups on a CU and 32 bytes of a position each, 99 us.
 template <typename T, int V, int NP, bool APPLY, bool TAIL>
 __global__ __launch_bounds__(1024) void norm_forward_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
@@ -429,8 +429,9 @@ __device__ __forceinline__ void norm_dh(const Piece<T, V>& x, const Piece<T, V>&
 // dh stays in fp32 registers between the sums and dx.  What is added per element are dh and dh d alone, per channel of the lane's piece:
 // with s = gamma rstd the group's two sums are S1 = sum_c s_c sum dh and S2 = sum_c s_c sum (dh d), a channel's share of dgamma is
 // rstd sum (dh d), and dx = s dh - S1 / N - d rstd^2 S2 / N.  bf16 with silu: 32 x 1024 x 512 in 32 groups 37 us + 5 for the shares,
-// 8192 x 2048 with residual 38 + 5; the bytes alone 20 and 26: half of the rest is vector instructions, half loads, sums and stores of
-// a share one after the other (two workgroups on a CU, and with single positions the next share's loads, cover some of it).
+// 8192 x 2048 with residual 38 + 5; the bytes alone 17 and 22.  The vector units are busy 41 and 51 % of the time (41 and 48 instructions an element),
+// a wavefront waits 43 and 46 % of its: loads, sums and stores of a share come one after the other (two workgroups on a CU, and with single
+// positions the next share's loads, cover some of it), and a workgroup of the first asks for 32 bytes of a position, a quarter of a line.
 template <typename T, int V, int NP, bool APPLY, bool TAIL>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs<T> a) {
   typedef Piece<T, V> Vec;
@@ -696,7 +697,7 @@ __global__ __launch_bounds__(1024) void norm_backward_apply_kernel(NormArgs<T> a
 // Backward, single positions of wide groups, like norm_row_kernel: a workgroup takes every row_count-th sample of one group, so that its
 // channels' sums add up in registers.  gamma and beta are read again for every sample (they are in the caches).  Groups of whole pieces
 // alone: the registers do not hold a partial piece's handling too (4096 x 4099 fp32 125 -> 139 us).  4096 x 8192 bf16 in one group 61 us
-// (79 in norm_backward_kernel, floor 39), x 16384 127 (366 in the plain kernel, floor 78), fp32 4096 x 4096 57 (130); 4096 x 2048
+// (79 in norm_backward_kernel, floor 39), x 16384 127 (366 in the plain kernel, floor 78), fp32 4096 x 4096 51 (130); 4096 x 2048
 // bf16 34 against 30 there, hence the rule.
 template <typename T, int V>
 __global__ __launch_bounds__(1024) void norm_row_backward_kernel(NormArgs<T> a) {

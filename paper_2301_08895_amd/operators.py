@@ -6,8 +6,9 @@ Tensors are on one GPU; a matrix is the last dimension times the others flattene
 distance apart (a slice of columns is fine, a transposed or expanded view is refused).  Operands are all
 float32 or all bfloat16; biases, gamma, beta, saved statistics and their gradients are float32.  The
 work goes to torch's current stream of the tensors' device; outputs and workspaces come from torch's
-allocator on that stream, so calls can be captured into a graph.  Nothing here records gradients: a
-backward pass is a call of its own.
+allocator on that stream, so calls can be captured into a graph.  Nothing here records gradients, also
+where a tensor requires one (what comes back is cut off from its graph): a backward pass is a call of
+its own.
 """
 from __future__ import annotations
 
