@@ -379,3 +379,20 @@ def test_group_norm_at_the_ends_of_its_range(n, S, C, G, dtype):
     want, slack = ou.norm_gradient(x, gamma, beta, mean, rstd, dy, None, SILU)
     for g, v, s, name in zip(lib.group_norm_backward(x, gamma, beta, mean, rstd, dy, act=SILU), want, slack, ("dx", "dgamma", "dbeta")):
         ou.close(g, v, s, name)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_losses_of_blocks_that_are_not_finite_end_the_round(value):
+    """A logit that is not finite in one class: the round is refused and not counted, and the model stays; held-out losses say so too."""
+    import numpy as np
+    p, (train, Xe, ye) = _blocks([16, 24, 10])
+    w0 = train["w0"].copy()
+    _last_bias(w0, p["dims"])[3] = value
+    sim = lib.Simulation(p, dict(train, w0=w0))
+    with pytest.raises(lib.AbsError) as e:
+        sim.round(1)
+    assert e.value.code == -5 and lib.abs_rounds_done(sim.handle) == 0
+    assert np.array_equal(sim.model(), w0, equal_nan=True)
+    loss, _ = sim.evaluate(Xe, ye)
+    assert not np.isfinite(loss)
+    sim.close()
